@@ -258,6 +258,61 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
                                int grad_replica, float eta, void* stream);
 
 /*
+ * The loss at the end of a chain of peers, and the gradient that its backward begins with: softmax cross entropy of
+ * every token against a vocabulary, over the head's product z = x w^T.
+ *   x         device bf16 [T, d], rows ldx elements apart: the last block's output.  d a multiple of 64, up to 16384.
+ *   w         device bf16 [V, d], rows ldw elements apart, one per token of the vocabulary (as an embedding that is
+ *             shared with the input has them).  1 <= V <= 2^24, any number; V * ldw below 2^31.
+ *   label     device int64 [T].  A label outside [0, V) takes its row out of the batch (prompts, padding): its loss, lse
+ *             and dx are zero and what the row of x holds reaches nothing.
+ *   loss      device fp32 [T]: lse_t - z[t, label_t], natural logarithm.     lse  device fp32 [T] or NULL: ln sum exp z[t].
+ * Of rv_loss_step alone, with g_t = scale * row_scale[t] (row_scale device fp32 [T], NULL: ones) the weight of a token's loss,
+ * dz[t, v] = g_t (softmax(z_t)[v] - [v = label_t]):
+ *   dx        device bf16 [T, d], rows lddx apart, or NULL: dz w, the grad_out of the last peer's backward.  May be x.
+ *   dw        device bf16 [V, d] without gaps, or NULL: dz^T x.
+ *   master, master_out, version, eta   all three or none, in place of dw, device [V, d] without gaps: the update of Eq. 2 in the
+ *             same call, master_out = master - eta * dz^T x (fp32), version = its bf16 rounding.  The product's fp32 sums are used,
+ *             not their rounding.  master_out may be master, version may be w.
+ * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16.
+ *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 64): bounds the work
+ *             memory at about 2 V * rows bytes; with several such pieces dw is added up in fp32, 4 V d bytes more.
+ *             0: as many as 2 GiB hold.  Outputs do not depend on it but for the order of those sums.
+ *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).
+ *             Nothing in it has to be kept between calls; calls that may run at one time need one each, and so do graphs
+ *             that may be replayed at one time.
+ * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8.  Outputs must not share memory
+ * with inputs or one another but as said.  Allocates nothing; RV_E_INVAL, before anything is enqueued, on what is not covered.
+ */
+typedef struct {
+  const void* x;
+  int64_t ldx;
+  const void* w;
+  int64_t ldw;
+  const int64_t* label;
+  int32_t T, d, V, rows;
+  float scale;
+  const float* row_scale;
+  float* loss;
+  float* lse;
+  void* dx;
+  int64_t lddx;
+  void* dw;
+  const float* master;
+  float* master_out;
+  void* version;
+  float eta;
+  void* work;
+  size_t work_bytes;
+  void* stream;
+} rv_loss_desc;
+
+rv_status rv_loss_work(int T, int d, int V, int64_t ldw, int rows, int gradients, size_t* bytes);
+/* Loss and lse alone (evaluation): one product. */
+rv_status rv_loss_forward(const rv_loss_desc* desc);
+/* Loss and gradients in one call: three products. */
+rv_status rv_loss_step(const rv_loss_desc* desc);
+
+/*
  * Measurement aid (no part of the method): while on, a decoder stage brackets every launch of
  * the work that dominates its step - the grouped weight-gradient products dW2 | dW1 | dWo | dWqkv,
  * of one block in one to three launches, or of up to four small blocks in one - with HIP events on the stream

@@ -17,6 +17,14 @@ class StageDesc(ctypes.Structure):
                 ("eta", c_float), ("ln_eps", c_float), ("stream", c_void_p)]
 
 
+class LossDesc(ctypes.Structure):
+    _fields_ = [("x", c_void_p), ("ldx", c_int64), ("w", c_void_p), ("ldw", c_int64), ("label", c_void_p),
+                ("T", c_int32), ("d", c_int32), ("V", c_int32), ("rows", c_int32), ("scale", c_float),
+                ("row_scale", c_void_p), ("loss", c_void_p), ("lse", c_void_p), ("dx", c_void_p), ("lddx", c_int64),
+                ("dw", c_void_p), ("master", c_void_p), ("master_out", c_void_p), ("version", c_void_p),
+                ("eta", c_float), ("work", c_void_p), ("work_bytes", c_size_t), ("stream", c_void_p)]
+
+
 # every symbol include/rv.h declares: name -> (restype, argtypes)
 SYMBOLS = {
     "rv_stage_create": (c_int, [ctypes.POINTER(StageDesc), ctypes.POINTER(c_void_p)]),
@@ -43,6 +51,9 @@ SYMBOLS = {
                                    c_void_p, c_int, c_float, c_void_p]),
     "rv_cluster_average_v": (c_int, [ctypes.POINTER(c_void_p), c_int, c_size_t, ctypes.POINTER(c_int64), c_int,
                                      c_void_p, c_int, c_void_p, c_int, c_float, c_void_p]),
+    "rv_loss_work": (c_int, [c_int, c_int, c_int, c_int64, c_int, c_int, ctypes.POINTER(c_size_t)]),
+    "rv_loss_forward": (c_int, [ctypes.POINTER(LossDesc)]),
+    "rv_loss_step": (c_int, [ctypes.POINTER(LossDesc)]),
     "rv_stage_profile": (c_int, [c_void_p, c_int]),
     "rv_stage_profile_read": (c_int, [c_void_p, ctypes.POINTER(c_int), ctypes.POINTER(c_float)]),
     "rv_strerror": (ctypes.c_char_p, [c_int]),

@@ -223,3 +223,78 @@ def cluster_average(replicas, R, mean_out=None, write_back=False, grad=None, gra
     _check(_lib.lib().rv_cluster_average(arr, C, n, R, _ptr(mean_out), 1 if write_back else 0, _ptr(grad),
                                          grad_replica, eta, _stream_handle(stream)))
     return mean_out
+
+
+def _rows(t, dtype, shape):
+    """A device matrix whose last dimension has no gaps; the pitch of its rows."""
+    assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
+    assert t.shape[1] == 1 or t.stride(1) == 1, "the columns of a row have to be neighbours"
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _flat(t, dtype, shape):
+    assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
+    return t
+
+
+def _on(stream, *tensors):
+    """The stream for a call on these tensors (the current one of their device if none is given)."""
+    devices = {t.device for t in tensors if t is not None}
+    assert len(devices) == 1, "tensors of several devices: %s" % sorted(map(str, devices))
+    device = devices.pop()
+    stream = torch.cuda.current_stream(device) if stream is None else stream
+    assert stream.device == device, "a stream of %s for tensors of %s" % (stream.device, device)
+    return stream
+
+
+def _loss(x, w, label, rows, gradients, call, stream, **more):
+    """Fills in what both calls share; scratch and outputs come from the call's own stream."""
+    T, d = x.shape
+    V = w.shape[0]
+    a = _lib.LossDesc(x=_ptr(x), ldx=_rows(x, torch.bfloat16, (T, d)), w=_ptr(w), ldw=_rows(w, torch.bfloat16, (V, d)),
+                      label=_ptr(_flat(label, torch.int64, (T,))), T=T, d=d, V=V, rows=rows, stream=_stream_handle(stream), **more)
+    n = ctypes.c_size_t(0)
+    _check(_lib.lib().rv_loss_work(T, d, V, a.ldw, rows, gradients, ctypes.byref(n)))
+    work = torch.empty(n.value, dtype=torch.uint8, device=x.device)
+    a.work, a.work_bytes = _ptr(work), n.value
+    _check(call(ctypes.byref(a)))
+
+
+def loss_forward(x, w, label, rows=0, stream=None):
+    """rv_loss_forward: (loss, lse), fp32 [T], of x bf16 [T, d] against the vocabulary w bf16 [V, d] and label int64 [T]; a label outside
+    [0, V) takes its row out (loss and lse 0)."""
+    stream = _on(stream, x, w, label)
+    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+        loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        lse = torch.empty_like(loss)
+        _loss(x, w, label, rows, 0, _lib.lib().rv_loss_forward, stream, loss=_ptr(loss), lse=_ptr(lse))
+    return loss, lse
+
+
+def loss_step(x, w, label, scale=1.0, row_scale=None, master=None, eta=0.0, master_out=None, version=None, dx=None, dw=None,
+              want_dx=True, want_dw=True, rows=0, stream=None):
+    """rv_loss_step: loss and gradients of sum_t scale * row_scale[t] * loss_t in one call.  Returns (loss, dx, dw), or, with the fp32
+    `master` of w, (loss, dx, master_out, version): the weights after w <- w - eta * dw (master_out may be master, version may be
+    w).  Outputs that are not given are allocated; want_dx, want_dw false leave one out (None in its place)."""
+    stream = _on(stream, x, w, label, row_scale, master, master_out, version, dx, dw)
+    assert master is not None or (master_out is None and version is None), "an update needs the master weights"
+    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+        loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        if dx is None and want_dx:
+            dx = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+        more = dict(scale=scale, loss=_ptr(loss), dx=_ptr(dx), lddx=_rows(dx, torch.bfloat16, x.shape) if dx is not None else 0)
+        if row_scale is not None:
+            more["row_scale"] = _ptr(_flat(row_scale, torch.float32, loss.shape))
+        if master is not None:
+            assert dw is None, "dw or the update"
+            master_out = torch.empty_like(master) if master_out is None else master_out
+            version = torch.empty(w.shape, dtype=torch.bfloat16, device=w.device) if version is None else version
+            more.update(master=_ptr(_flat(master, torch.float32, w.shape)), master_out=_ptr(_flat(master_out, torch.float32, w.shape)),
+                        version=_ptr(_flat(version, torch.bfloat16, w.shape)), eta=eta)
+        else:
+            if dw is None and want_dw:
+                dw = torch.empty(w.shape, dtype=torch.bfloat16, device=w.device)
+            if dw is not None:
+                more["dw"] = _ptr(_flat(dw, torch.bfloat16, w.shape))
+        _loss(x, w, label, rows, 1, _lib.lib().rv_loss_step, stream, **more)
+    return (loss, dx, dw) if master is None else (loss, dx, master_out, version)

@@ -1,0 +1,238 @@
+"""The loss at a chain's end and its gradients against the definition in 64 bits on the same bf16 operands.
+
+Tolerances, element by element, from the roundings that the kernels make (a bf16 rounding is off by at most 2^-8 of the value):
+  logits    fp32 accumulation of d products: (d + 8) 2^-24 sum |x w| at most
+  loss, lse that of the logits, and a softmax sum of exp2 (2 ulp) in up to 64 + V / 64 additions of a chain, and their log
+  dx, dw    the exponential and dz are rounded to bf16 once each, (1 + 2^-8)^2 - 1 < 2^-7 + 2^-15, and an error of the logits, of the
+            lse and of an exponential, `slack`, moves dz by a factor of exp(slack) < 1 + 2 slack: |dz| (2^-7 + 2^-15 + 2 slack),
+            through a product of absolute values; then the result's own rounding.  The label's column has p - 1 from fp32: its error is that of z, absolute.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2401_01728_amd as rv
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(seed, T, d, V, out=0.0, sure=6.0):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randn(V, d, generator=g) * 0.05
+    label = torch.randint(0, V, (T,), generator=g)
+    x = torch.randn(T, d, generator=g) + torch.rand(T, 1, generator=g) * sure / (0.05 * d) * (w[label] / 0.05)
+    gone = torch.randperm(T, generator=g)[:int(T * out)]
+    label[gone] = torch.tensor([-1, V, -100, 1 << 40])[torch.arange(len(gone)) % 4]
+    x = x.to(torch.bfloat16)
+    x[gone] = float("nan")
+    return x, w.to(torch.bfloat16), label, w
+
+
+def _reference(x, w, label, g):
+    """loss, lse, dz [T, V], and the bound of the logits' error, in 64 bits; rows out of the batch are zero"""
+    T, d = x.shape
+    V = w.shape[0]
+    takes = (label >= 0) & (label < V)
+    x64, w64 = torch.where(takes[:, None], x.double(), 0.0), w.double()
+    z = x64 @ w64.T
+    lse = torch.logsumexp(z, 1)
+    y = torch.where(takes, label, 0)
+    at = z.gather(1, y[:, None])[:, 0]
+    p = torch.exp(z - lse[:, None])
+    hot = torch.zeros_like(z)
+    hot[torch.arange(T), y] = 1.0
+    gt = torch.where(takes, g.double(), 0.0)[:, None]
+    dz = (p - hot) * gt
+    zerr = (d + 8) * 2.0 ** -24 * float((x64.abs() @ w64.abs().T).max())
+    zero = torch.zeros_like(lse)
+    return torch.where(takes, lse - at, zero), torch.where(takes, lse, zero), dz, zerr, x64, w64, y, takes
+
+
+def _check(x, w, label, g, got_loss, got_lse, dx=None, dw=None, master=None, eta=0.0, new=None, version=None):
+    loss, lse, dz, zerr, x64, w64, y, takes = _reference(x, w, label, g)
+    V = w.shape[0]
+    slack = 2 * zerr + (80 + V / 64) * 2.0 ** -24 + 2.0 ** -22 * float(lse.abs().max())
+    for got, ref in ((got_loss, loss), (got_lse, lse)):
+        if got is not None:
+            assert float((got.cpu().double() - ref).abs().max()) <= slack
+    # what dz may be off by: relative, but absolute (times the row's weight) at the label
+    off = dz.abs() * (2.0 ** -7 + 2.0 ** -15 + 2 * slack)
+    rows = torch.arange(len(y))
+    off[rows, y] = dz[rows, y].abs() * 2.0 ** -8 + torch.where(takes, g.double().abs(), 0.0) * slack
+    fp32 = 2.0 ** -24 * (x.shape[0] + V)      # accumulation of the products of dz, relative to the sums of absolute values
+    if dx is not None:
+        ref = dz @ w64
+        bound = (off + dz.abs() * fp32) @ w64.abs()
+        assert bool(((dx.cpu().double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
+        assert not dx.cpu()[~takes].any()
+    ref = dz.T @ x64
+    bound = (off + dz.abs() * fp32).T @ x64.abs()
+    if dw is not None:
+        assert bool(((dw.cpu().double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
+    if new is not None:
+        want = master.cpu().double() - eta * ref
+        assert bool(((new.cpu().double() - want).abs() <= eta * bound + 2.0 ** -23 * (want.abs() + eta * ref.abs())).all())
+        assert torch.equal(version, new.to(torch.bfloat16))
+
+
+# one row, one token of vocabulary, less than a strip, ends inside a strip and a tile, more than one tile each way, rows that end inside
+# a tile of 32, widths of one and of several tiles; few and many rows
+SIZES = [(1, 64, 1), (1, 64, 5), (2, 128, 33), (3, 128, 63), (31, 64, 64), (33, 192, 65), (65, 64, 1000), (130, 448, 257), (257, 128, 2049),
+         (300, 320, 4097), (129, 192, 513), (513, 256, 1031), (96, 1024, 5000), (700, 1600, 777)]
+
+
+@pytest.mark.parametrize("T,d,V", SIZES)
+@pytest.mark.parametrize("out", [0.0, 0.4])
+def test_loss_and_gradients(T, d, V, out):
+    x, w, label, _ = _inputs(T + d + V, T, d, V, out)
+    g = torch.full((T,), 1.0 / T)
+    loss, lse = rv.loss_forward(x.cuda(), w.cuda(), label.cuda())
+    _check(x, w, label, g, loss, lse)
+    loss2, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=1.0 / T)
+    _check(x, w, label, g, loss2, None, dx, dw)
+
+
+@pytest.mark.parametrize("T,d,V,rows", [(300, 128, 777, 64), (300, 320, 1031, 128), (1100, 192, 513, 512), (65, 64, 100, 1)])
+@pytest.mark.parametrize("out", [0.0, 0.6])
+def test_pieces_of_rows(T, d, V, rows, out):
+    x, w, label, master = _inputs(7, T, d, V, out)
+    g = torch.full((T,), 0.25)
+    loss, lse = rv.loss_forward(x.cuda(), w.cuda(), label.cuda(), rows=rows)
+    _check(x, w, label, g, loss, lse)
+    loss, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.25, rows=rows)
+    _check(x, w, label, g, loss, None, dx, dw)
+    loss, dx, new, version = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.25, rows=rows, master=master.cuda(), eta=0.1)
+    _check(x, w, label, g, loss, None, dx, None, master, 0.1, new, version)
+
+
+@pytest.mark.parametrize("T,d,V", [(1, 64, 3), (40, 128, 130), (300, 320, 4097), (200, 1024, 16500)])
+def test_update_and_row_weights(T, d, V):
+    x, w, label, master = _inputs(11, T, d, V, 0.25)
+    row = torch.rand(T, generator=torch.Generator().manual_seed(5)) - 0.3
+    takes = (label >= 0) & (label < V)
+    row[~takes] = float("nan")
+    xs, ws, m = x.cuda(), w.cuda(), master.cuda()
+    loss, dx, new, version = rv.loss_step(xs, ws, label.cuda(), scale=0.5, row_scale=row.cuda(), master=m, eta=0.3)
+    _check(x, w, label, torch.where(takes, row, 0.0) * 0.5, loss, None, dx, None, master, 0.3, new, version)
+    # in place: the same values
+    loss2, dx2, m2, w2 = rv.loss_step(xs, ws, label.cuda(), scale=0.5, row_scale=row.cuda(), master=m, eta=0.3, master_out=m, version=ws, dx=xs)
+    assert dx2 is xs and m2 is m and w2 is ws
+    for a, b in ((loss2, loss), (dx2, dx), (m2, new), (w2, version)):
+        assert torch.equal(a, b)
+
+
+def test_no_row_takes_part():
+    T, d, V = 70, 128, 300
+    x, w, label, master = _inputs(3, T, d, V, 1.0)
+    loss, lse = rv.loss_forward(x.cuda(), w.cuda(), label.cuda())
+    assert not loss.any() and not lse.any()
+    for rows in (0, 64):
+        loss, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), rows=rows)
+        assert not loss.any() and not dx.any() and not dw.any()
+        _, _, new, version = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), rows=rows, master=master.cuda(), eta=0.5)
+        assert torch.equal(new, master.cuda()) and torch.equal(version, master.cuda().to(torch.bfloat16))
+
+
+def test_strides_and_one_gradient_alone():
+    T, d, V = 150, 192, 515
+    x, w, label, _ = _inputs(4, T, d, V, 0.2)
+    xs = torch.full((T, d + 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((V, d + 8), float("nan"), dtype=torch.bfloat16, device="cuda")
+    dxs = torch.full((T, d + 24), 7.0, dtype=torch.bfloat16, device="cuda")
+    xs[:, 64:] = x.cuda()
+    ws[:, :d] = w.cuda()
+    ref = rv.loss_step(x.cuda(), w.cuda(), label.cuda())
+    got = rv.loss_step(xs[:, 64:], ws[:, :d], label.cuda(), dx=dxs[:, :d])
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+    assert bool((dxs[:, d:] == 7.0).all())
+    only = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), want_dw=False)
+    assert only[2] is None and torch.equal(only[1], ref[1])
+    only = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), want_dx=False)
+    assert only[1] is None and torch.equal(only[2], ref[2])
+
+
+def test_large_and_infinite_values():
+    """Logits of +-1e4 (their exponentials span the whole range), a column of weights that gives -inf, a row that gives NaN alone."""
+    T, d, V = 40, 64, 200
+    x, w, label, _ = _inputs(6, T, d, V)
+    label[:] = torch.arange(T) % 100
+    w[:, 1:] *= 4e4
+    w[:, 0] = 0.0
+    w[150, 0] = -3e38
+    x[:, 0] = 1.0
+    x[7] = float("nan")
+    x[8, 0] = 100.0        # -3e40: -inf in fp32
+    loss, lse = rv.loss_forward(x.cuda(), w.cuda(), label.cuda())
+    z = x.double() @ w.double().T
+    ref_lse = torch.logsumexp(z, 1)
+    ref = ref_lse - z[torch.arange(T), label]
+    keep = torch.arange(T) != 7
+    tol = 80 * 2.0 ** -24 * float((x[keep].double()[:, 1:].abs() @ w.double()[:, 1:].abs().T).max())
+    assert bool(torch.isnan(loss.cpu()[7])) and bool(torch.isnan(lse.cpu()[7]))
+    assert float((loss.cpu().double() - ref)[keep].abs().max()) <= tol
+    assert float((lse.cpu().double() - ref_lse)[keep].abs().max()) <= tol
+    _, dx, _ = rv.loss_step(x.cuda(), w.cuda(), label.cuda())
+    assert bool(torch.isfinite(dx.cpu()[keep & (torch.arange(T) != 8)].float()).all())
+
+
+def test_gradient_against_differences():
+    """dx . u and dw . u against central differences of the summed loss, formed in 64 bits by the definition: the directions are whole
+    tensors, so the roundings of single elements average out; 2^-7 of the sum of absolute terms bounds them."""
+    T, d, V = 20, 128, 90
+    x, w, label, _ = _inputs(9, T, d, V, 0.2)
+    _, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda())
+    takes = label >= 0
+    takes &= label < V
+    x64, w64 = torch.where(takes[:, None], x.double(), 0.0), w.double()
+
+    def total(xx, ww):
+        z = xx @ ww.T
+        at = z.gather(1, torch.where(takes, label, 0)[:, None])[:, 0]
+        return float(torch.where(takes, torch.logsumexp(z, 1) - at, 0.0).sum())
+
+    g = torch.Generator().manual_seed(1)
+    for which, grad in (("x", dx), ("w", dw)):
+        u = torch.randn(grad.shape, generator=g, dtype=torch.float64)
+        if which == "x":
+            u[~takes] = 0.0
+        h = 1e-5
+        num = (total(x64 + h * u, w64) - total(x64 - h * u, w64)) / (2 * h) if which == "x" else (total(x64, w64 + h * u) - total(x64, w64 - h * u)) / (2 * h)
+        terms = grad.cpu().double() * u
+        assert abs(float(terms.sum()) - num) <= 2.0 ** -6 * float(terms.abs().sum())
+
+
+def test_other_stream_and_captured_graph():
+    T, d, V = 200, 128, 700
+    x, w, label, master = _inputs(12, T, d, V, 0.3)
+    x, w, label, master = x.cuda(), w.cuda(), label.cuda(), master.cuda()
+    ref = rv.loss_step(x, w, label, master=master, eta=0.1)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = rv.loss_step(x, w, label, master=master, eta=0.1, stream=side)
+    side.synchronize()
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = rv.loss_step(x, w, label, master=master, eta=0.1)
+        fwd = rv.loss_forward(x, w, label)
+    for k in range(4):
+        fresh, _, fresh_label, _ = _inputs(20 + k, T, d, V, 0.2 * k)
+        x.copy_(fresh)
+        label.copy_(fresh_label)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got + fwd, rv.loss_step(x, w, label, master=master, eta=0.1) + rv.loss_forward(x, w, label)):
+            assert torch.equal(a, b)
+
+
+def test_same_bits_every_time():
+    x, w, label, _ = _inputs(15, 900, 512, 3001, 0.1)
+    x, w, label = x.cuda(), w.cuda(), label.cuda()
+    ref = rv.loss_step(x, w, label)
+    for _ in range(3):
+        for a, b in zip(rv.loss_step(x, w, label), ref):
+            assert torch.equal(a, b)
