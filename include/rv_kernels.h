@@ -1,7 +1,8 @@
 /*
  * rv_kernels.h - per-kernel entry points of librv.so, for parity tests and profiling of
  * the individual steps of the decoder stage.  The product API is rv.h; these calls expose
- * the same kernels the stage launches, one at a time.  All pointers are device memory,
+ * the same kernels the stage launches, one at a time.  Cross-attention (at the end) is an operator that a peer's owner
+ * runs between stages; no stage launches it.  All pointers are device memory,
  * 16-byte aligned; every call enqueues on `stream` and returns without synchronising;
  * RV_E_INVAL on shapes the kernels do not cover.
  */
@@ -157,6 +158,32 @@ rv_status rv_k_attention_bwd(const void* qkv, const void* out, const void* dout,
 rv_status rv_k_attention_bwd_static(const void* qkv, const void* out, const void* dout, const float* lse2,
                                     void* dqkv, int microbatch, int seq, int d_model, int n_heads,
                                     void* stream);
+
+/*
+ * Attention of a decoder's tokens to an encoder's states of another length (no causal mask).
+ *   q, out, dout, dq   bf16, token i of sequence b at row b * Sq + i, rows ldq, ldo, lddo, lddq elements apart, head h at columns
+ *                      h * d_head on (n_heads of them).
+ *   k, v, dk, dv       bf16, key j of sequence b at row b * Sk + j, n_kv_heads heads likewise; k and v may be columns of one matrix.
+ *                      n_kv_heads divides n_heads: query head h reads key/value head h / (n_heads / n_kv_heads).
+ *   klen               device int32 [B]: keys of each sequence, taken as 0 below 0 and as Sk above; NULL: Sk for all.  What lies behind a
+ *                      sequence's keys is not read.  A sequence without keys gives out 0, lse2 -inf and dq 0.
+ *   lse2               fp32 [B, n_heads, Sq]: log2 of the softmax denominator in the scaled base-2 domain (kept for the backward).
+ * d_head is 64 or 128; the scale is 1 / sqrt(d_head); B, Sq, Sk are at least 1, of any size (B <= 2^20, Sq and Sk <= 2^24,
+ * n_heads <= 2^16).  Pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (lse2, klen: 4).  The backward writes all of dq, dk
+ * and dv, zeros for keys behind a sequence's; out and lse2 are the forward's.  Outputs must not share memory with inputs or one
+ * another (but dk and dv may be columns of one matrix, and so may dq of a matrix with others).  No atomics: results do not vary.
+ *   work               device, 256-byte aligned, rv_k_cross_attention_work bytes (0 in some forwards: NULL is fine then); nothing in it is
+ *                      kept between calls, calls that may run at one time need one each.
+ */
+rv_status rv_k_cross_attention_work(int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, int backward, size_t* bytes);
+rv_status rv_k_cross_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                   const int32_t* klen, void* out, int64_t ldo, float* lse2, int B, int Sq, int Sk, int n_heads,
+                                   int n_kv_heads, int d_head, void* work, size_t work_bytes, void* stream);
+rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                   const int32_t* klen, const void* out, int64_t ldo, const void* dout, int64_t lddo,
+                                   const float* lse2, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, int B,
+                                   int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, void* work, size_t work_bytes,
+                                   void* stream);
 
 #ifdef __cplusplus
 }

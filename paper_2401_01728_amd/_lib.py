@@ -84,6 +84,11 @@ KERNEL_SYMBOLS = {
     "rv_k_attention_fwd": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p]),
     "rv_k_attention_bwd": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                    c_int, c_void_p]),
+    "rv_k_cross_attention_work": (c_int, [c_int] * 7 + [ctypes.POINTER(c_size_t)]),
+    "rv_k_cross_attention_fwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p, c_void_p, c_int64, c_void_p] + [c_int] * 6
+                                 + [c_void_p, c_size_t, c_void_p]),
+    "rv_k_cross_attention_bwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p] + [c_void_p, c_int64] * 2 + [c_void_p]
+                                 + [c_void_p, c_int64] * 3 + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]),
     "rv_k_attention_bwd_static": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                           c_int, c_void_p]),
 }

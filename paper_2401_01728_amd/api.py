@@ -229,7 +229,7 @@ def _rows(t, dtype, shape):
     """A device matrix whose last dimension has no gaps; the pitch of its rows."""
     assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
     assert t.shape[1] == 1 or t.stride(1) == 1, "the columns of a row have to be neighbours"
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _flat(t, dtype, shape):

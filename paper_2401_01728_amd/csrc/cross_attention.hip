@@ -1,0 +1,777 @@
+// Attention of a decoder's tokens to an encoder's states of another length, forward and backward: bf16 operands, fp32 scores, softmax
+// statistics and sums.
+//
+//   s = q k^T / sqrt(dh),  p = softmax over the keys of the sequence,  o = p v
+//   dv = p^T do,  ds = p (do v^T - rowsum(do o)),  dq = ds k / sqrt(dh),  dk = ds^T q / sqrt(dh)
+//
+// The `share` query heads of a key/value head see the same keys: their tokens are taken as ONE list of share * Sq rows, row r being
+// token r % Sq of head r / Sq.  So a key/value head is streamed once for all of them, the gradients of a shared head are sums over
+// one list in one workgroup, without atomics, and a single token of eight heads is eight rows of a matrix product.
+//
+// Scores are formed transposed to the side that a wave owns, as in attention.hip: the owned index (32 rows, or 32 keys in the dK/dV
+// kernel) is the lane, the streamed one runs over the 16 registers of an accumulator; row statistics are scalars of a lane and the
+// probabilities are already the B operand of the second product.  The streamed side goes global -> LDS directly, in tiles of 64 rows,
+// through a ring of slots with one barrier a tile; 16-byte chunks are permuted by row (swizzle) so that ONE copy of a tile serves both
+// the reads of whole rows and the transposing reads without bank conflicts.
+// Keys behind a sequence's length are never read: a tile's rows are clamped to the last key, whose repeats are masked by a select.
+// The work is cut along the streamed side where the rows alone do not fill the chip; the parts' sums (with their maxima, in the
+// forward) are joined by a second kernel in a fixed order.
+#include <math.h>
+#include "gemm_core.h"
+
+namespace {
+
+constexpr int TILE = 64;                 // streamed rows
+constexpr int OWN = 32;                  // rows or keys a wave owns
+
+struct CrossArgs {
+  const uint16_t* q; const uint16_t* k; const uint16_t* v;
+  int64_t ldq, ldk, ldv;
+  const int* klen;                       // device [B] or null
+  uint16_t* out; int64_t ldo;
+  float* lse2;                           // [B][Hkv][R]
+  // backward
+  const uint16_t* o; const uint16_t* dout; int64_t lddo;
+  uint16_t* dq; uint16_t* dk; uint16_t* dv;
+  int64_t lddq, lddk, lddv;
+  float* stat_lse; float* stat_d;        // [B][Hkv][Rp], +inf and 0 behind the last row
+  float* part; float2* part_ml;          // sums of the parts
+  int B, Sq, Sk, share, Hkv, R, Rp, parts;
+  float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
+};
+
+__device__ __forceinline__ int keys_of(const CrossArgs& a, int b) {
+  if (!a.klen) return a.Sk;
+  const int n = __builtin_amdgcn_readfirstlane(a.klen[b]);
+  return n < 0 ? 0 : n < a.Sk ? n : a.Sk;
+}
+// element offset of row r of (b, hkv) in a matrix of tokens whose rows are ld apart, heads of DH columns
+template <int DH>
+__device__ __forceinline__ int64_t row_at(const CrossArgs& a, int b, int h, int r, int64_t ld) {
+  const int g = r / a.Sq, t = r - g * a.Sq;
+  return ((int64_t)b * a.Sq + t) * ld + (h * a.share + g) * DH;
+}
+
+// Workgroup -> (sequence, key/value head, part, block): ids go to the 8 XCDs in turn; each takes a contiguous range of a list in which the
+// blocks of one (head, sequence), which read the same keys, are neighbours, and the sequences of one head follow one another - their
+// lengths differ, and a range of heads of every sequence is as long as any other.
+struct Where { int b, h, part, block, unit; };
+__device__ __forceinline__ Where where(const CrossArgs& a, int blocks) {
+  const int total = gridDim.x, base = total / 8, rem = total % 8;
+  const int g = blockIdx.x % 8, v = g * base + (g < rem ? g : rem) + blockIdx.x / 8;
+  Where w;
+  w.block = v % blocks;
+  const int x = v / blocks;
+  w.part = x % a.parts;
+  const int u = x / a.parts;
+  w.b = u % a.B; w.h = u / a.B;
+  w.unit = w.b * a.Hkv + w.h;
+  return w;
+}
+
+typedef __bf16 Frag __attribute__((ext_vector_type(8)));
+
+// row of a tile -> what its chunk indexes are xor-ed with.  Rows of 128 columns (16 chunks, one bank line of 256 bytes): a permutation of 16
+// over 16 rows, for the reads of one chunk of 16 rows, whose upper two bits differ among four neighbouring rows, for the transposing reads of 64
+// bytes of four rows.  64 columns: two rows to a line, so eight values over 16 rows and one bit among the rows of a parity.
+template <int DH>
+__device__ __forceinline__ int swizzle(int row) {
+  return DH == 128 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+template <int DH> constexpr int kTileBytes = TILE * DH * 2;
+
+// A fragment, rows row0 + lane % 32, columns 16 kk + 8 (lane / 32) .. + 7
+template <int DH>
+__device__ __forceinline__ Frag frag_rows(const char* lds, int row0, int kk) {
+  const int l = threadIdx.x & 63, row = row0 + (l & 31);
+  return *reinterpret_cast<const Frag*>(lds + row * (DH * 2) + (((kk * 2 + (l >> 5)) ^ swizzle<DH>(row)) << 4));
+}
+// A fragment of the transposed tile: m = column col0 + lane % 32, its eight k the rows row0 + 4 g + (0 .. 3) and row0 + 8 + 4 g + (0 .. 3) of
+// lane group g = lane / 32 - those of a lane's accumulator registers
+template <int DH>
+__device__ __forceinline__ Frag frag_cols(const char* lds, int row0, int col0) {
+  const int l = threadIdx.x & 63, q = l >> 4, i = l & 15;
+  const int row = row0 + 4 * (q >> 1) + (i >> 2), col = col0 + 16 * (q & 1) + 4 * (i & 3);
+  auto at = [&](int r) {
+    return (s16x4 __attribute__((address_space(3)))*)(lds + r * (DH * 2) + (((col >> 3) ^ swizzle<DH>(r)) << 4) + (col & 7) * 2);
+  };
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row + 8));
+  return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// registers 8 ks .. 8 ks + 7 of an accumulator, rounded: a B fragment
+__device__ __forceinline__ Frag pack_frag(const f32x16& a, int ks) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = rv_pack_bf16x2(a[8 * ks + 2 * i], a[8 * ks + 2 * i + 1]);
+  return __builtin_bit_cast(Frag, r);
+}
+// streamed row (of 32) of accumulator register r in lane group g
+__device__ __forceinline__ int acc_row(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
+
+template <int N>
+__device__ __forceinline__ void clear(f32x16 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
+}
+
+// waits that later LDS reads are not moved in front of
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// A wave's share of a tile of keys: TILE rows from k0 on, clamped to the last key.
+template <int DH, int NW, int ROWS = TILE>
+struct KeyLoads {
+  static constexpr int N = ROWS * DH / 8 / 64 / NW;      // loads per lane
+  int row[N];
+  unsigned col[N];                                       // bytes
+  int wave;
+  __device__ __forceinline__ explicit KeyLoads(int w) : wave(w) {
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = (i * NW + wave) * 64 + l;
+      row[i] = slot / (DH / 8);
+      col[i] = (unsigned)((slot % (DH / 8)) ^ swizzle<DH>(row[i])) * 16;
+    }
+  }
+  __device__ __forceinline__ void issue(const uint16_t* base, int64_t ld, int k0, int n, char* lds) const {
+    const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)lds + wave * 1024);
+    const uint16_t* from = base + (int64_t)k0 * ld;
+    const int last = n - 1 - k0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row[i] < last ? row[i] : last;
+      dtl_load_s(from, (unsigned)r * (unsigned)(ld * 2) + col[i], m0v + i * NW * 1024);
+    }
+  }
+};
+// The same of rows of the list of a key/value head's query rows (out of the last row: clamped to it).
+template <int DH, int NW>
+struct RowLoads {
+  static constexpr int N = TILE * DH / 8 / 64 / NW;
+  int row[N];
+  int col[N];                                            // elements
+  int wave;
+  __device__ __forceinline__ explicit RowLoads(int w) : wave(w) {
+    const int l = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = (i * NW + wave) * 64 + l;
+      row[i] = slot / (DH / 8);
+      col[i] = ((slot % (DH / 8)) ^ swizzle<DH>(row[i])) * 8;
+    }
+  }
+  __device__ __forceinline__ void issue(const CrossArgs& a, int b, int h, const uint16_t* q, int64_t ldq, const uint16_t* o, int64_t ldo, int r0, char* lds_q,
+                                        char* lds_o) const {
+    const int mq = __builtin_amdgcn_readfirstlane((int)(size_t)lds_q + wave * 1024), mo = __builtin_amdgcn_readfirstlane((int)(size_t)lds_o + wave * 1024);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int r = r0 + row[i];
+      r = r < a.R ? r : a.R - 1;
+      const int g = r / a.Sq, t = r - g * a.Sq;
+      const int64_t tok = (int64_t)b * a.Sq + t;
+      const int c = (h * a.share + g) * DH + col[i];
+      const uint16_t* pq = q + tok * ldq + c;
+      const uint16_t* po = o + tok * ldo + c;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pq), "s"(mq + i * NW * 1024) : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(po), "s"(mo + i * NW * 1024) : "memory", "m0");
+    }
+  }
+};
+// 64 floats -> LDS
+__device__ __forceinline__ void load_floats(const float* from, char* lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               : : "v"((threadIdx.x & 63) * 4), "s"(from), "s"(__builtin_amdgcn_readfirstlane((int)(size_t)lds)) : "memory", "m0");
+}
+
+// a wave's owned rows as B fragments
+template <int DH>
+__device__ __forceinline__ void load_owned(Frag (&f)[DH / 16], const uint16_t* row) {
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int kk = 0; kk < DH / 16; ++kk) f[kk] = *reinterpret_cast<const Frag*>(row + kk * 16 + (l >> 5) * 8);
+}
+// acc^T (lane = row) as bf16, or as it is
+template <int DH>
+__device__ __forceinline__ void store_owned(const f32x16 (&acc)[DH / 32], float mul, uint16_t* row) {
+  const int grp = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg) {
+      u32x2 o;
+      o.x = rv_pack_bf16x2(acc[dt][4 * rg] * mul, acc[dt][4 * rg + 1] * mul);
+      o.y = rv_pack_bf16x2(acc[dt][4 * rg + 2] * mul, acc[dt][4 * rg + 3] * mul);
+      *reinterpret_cast<u32x2*>(row + dt * 32 + 8 * rg + 4 * grp) = o;
+    }
+}
+template <int DH>
+__device__ __forceinline__ void store_owned32(const f32x16 (&acc)[DH / 32], float* row) {
+  const int grp = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg)
+      *reinterpret_cast<f32x4*>(row + dt * 32 + 8 * rg + 4 * grp) =
+          f32x4{acc[dt][4 * rg], acc[dt][4 * rg + 1], acc[dt][4 * rg + 2], acc[dt][4 * rg + 3]};
+}
+
+// Softmax of a tile of scores s (SUBS x 32 keys from k0 on) with the running maximum m and sum l of a lane's row, in base 2: s becomes
+// exp2(s c2 - m); the factor for what was summed before is returned.
+template <int SUBS>
+__device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, int k0, int n, float& m, float& lsum) {
+  const int grp = (threadIdx.x & 63) >> 5;
+  if (k0 + SUBS * 32 > n) {            // (wave-uniform) only the last tile ends inside
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (k0 + sub * 32 + acc_row(r, grp) >= n) s[sub][r] = -INFINITY;
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  const float mn = fmaxf(m, mx * c2), base = mn == -INFINITY ? 0.f : mn;   // (scores of -inf alone: no probability, no NaN)
+  const float alpha = __builtin_amdgcn_exp2f(m - base);
+  m = mn;
+  float ps = 0.f;
+#pragma unroll
+  for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[sub][r], c2, -base));
+      s[sub][r] = p;
+      ps += p;
+    }
+  lsum = lsum * alpha + ps;
+  return alpha;
+}
+
+// ---- forward ----------------------------------------------------------------------------------
+template <int DH, int NW, int NS>
+__global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a) {
+  char* smem = dtl_smem;
+  constexpr int SLOT = 2 * kTileBytes<DH>;               // keys, values
+  const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
+  const Where w = where(a, blocks);
+  const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
+  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
+  const int r = w.block * OWN * NW + wave * OWN + (l & 31);
+  const bool active = w.block * OWN * NW + wave * OWN < a.R;
+  const int rc = r < a.R ? r : a.R - 1;
+  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
+  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
+
+  Frag qf[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
+  f32x16 o[DH / 32];
+  clear(o);
+  float m = -INFINITY, lsum = 0.f;
+
+  const KeyLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * KeyLoads<DH, NW>::N;
+  auto issue = [&](int t) {
+    char* to = smem + (t - t0) % NS * SLOT;
+    loads.issue(K, a.ldk, t * TILE, n, to);
+    loads.issue(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  for (int t = t0; t < t1; ++t) {
+    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
+    __syncthreads();                                     // tile t is there, and everyone has left tile t - 1
+    if (t + NS - 1 < t1) issue(t + NS - 1);
+    if (!active) continue;
+    const char* Ks = smem + (t - t0) % NS * SLOT;
+    const char* Vs = Ks + kTileBytes<DH>;
+    f32x16 s[2];
+    clear(s);
+#pragma unroll
+    for (int kk = 0; kk < DH / 16; ++kk)
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, sub * 32, kk), qf[kk], s[sub], 0, 0, 0);
+    const float alpha = softmax_tile(s, a.c2, t * TILE, n, m, lsum);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {    // maxima that have settled leave the sums as they are
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
+    }
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const Frag p = pack_frag(s[sub], ks);
+#pragma unroll
+        for (int dt = 0; dt < DH / 32; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Vs, sub * 32 + ks * 16, dt * 32), p, o[dt], 0, 0, 0);
+      }
+  }
+  if (!active || r >= a.R) return;
+  const float tot = lsum + __shfl_xor(lsum, 32, 64);
+  if (a.parts == 1) {
+    store_owned<DH>(o, tot == 0.f ? 0.f : 1.0f / tot, a.out + row_at<DH>(a, w.b, w.h, r, a.ldo));
+    if (grp == 0) a.lse2[(int64_t)w.unit * a.R + r] = m + __builtin_amdgcn_logf(tot);     // v_log_f32 is log2
+  } else {
+    const int64_t at = ((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r;
+    store_owned32<DH>(o, a.part + at * DH);
+    if (grp == 0) a.part_ml[at] = float2{m, tot};
+  }
+}
+
+// Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the four waves walks over tiles of 32
+// keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.
+constexpr int TOKEN_KEYS = 32, TOKEN_NW = 4;
+template <int DH> constexpr int kTokenSlots = DH == 128 ? 2 : 4;
+template <int DH> constexpr int kTokenRing = kTokenSlots<DH> * 2 * TOKEN_KEYS * DH * 2;
+template <int DH>
+__global__ __launch_bounds__(64 * TOKEN_NW) void cross_token_kernel(CrossArgs a) {
+  constexpr int NS = kTokenSlots<DH>, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
+  const Where w = where(a, 1);
+  const int n = keys_of(a, w.b), nt = (n + TOKEN_KEYS - 1) / TOKEN_KEYS;
+  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5, r = l & 31;
+  char* ring = dtl_smem + wave * kTokenRing<DH>;
+  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
+  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
+  Frag qf[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, r < a.R ? r : a.R - 1, a.ldq));
+  f32x16 o[DH / 32];
+  clear(o);
+  float m = -INFINITY, lsum = 0.f;
+  const KeyLoads<DH, 1, TOKEN_KEYS> loads(0);
+  constexpr int LPT = 2 * KeyLoads<DH, 1, TOKEN_KEYS>::N;
+  const int mine = t1 - t0 > wave ? (t1 - t0 - wave + TOKEN_NW - 1) / TOKEN_NW : 0;      // tiles t0 + wave, + TOKEN_NW, ...
+  auto issue = [&](int i) {
+    char* to = ring + i % NS * SLOT;
+    const int k0 = (t0 + wave + i * TOKEN_NW) * TOKEN_KEYS;
+    loads.issue(K, a.ldk, k0, n, to);
+    loads.issue(V, a.ldv, k0, n, to + HALF);
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (i < mine) issue(i);
+  for (int i = 0; i < mine; ++i) {
+    // the slot that is filled next was read a tile ago; its reads have come back before the load goes out
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    if (i + NS - 1 < mine) { issue(i + NS - 1); wait_loads<LPT * (NS - 1)>(); }
+    else wait_loads<0>();
+    const char* Ks = ring + i % NS * SLOT;
+    const char* Vs = Ks + HALF;
+    f32x16 s[1];
+    clear(s);
+#pragma unroll
+    for (int kk = 0; kk < DH / 16; ++kk) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, 0, kk), qf[kk], s[0], 0, 0, 0);
+    const float alpha = softmax_tile(s, a.c2, (t0 + wave + i * TOKEN_NW) * TOKEN_KEYS, n, m, lsum);
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const Frag p = pack_frag(s[0], ks);
+#pragma unroll
+      for (int dt = 0; dt < DH / 32; ++dt)
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Vs, ks * 16, dt * 32), p, o[dt], 0, 0, 0);
+    }
+  }
+  lsum += __shfl_xor(lsum, 32, 64);
+  // four waves' sums: registers through LDS, a quarter of them to each wave
+  __syncthreads();
+  float* image = reinterpret_cast<float*>(dtl_smem);     // [wave][DH / 2][64], then the pairs
+  float2* ml = reinterpret_cast<float2*>(image + TOKEN_NW * (DH / 2) * 64);
+#pragma unroll
+  for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) image[(wave * (DH / 2) + dt * 16 + x) * 64 + l] = o[dt][x];
+  if (grp == 0) ml[wave * 32 + r] = float2{m, lsum};
+  __syncthreads();
+  float top = -INFINITY, tot = 0.f, f[TOKEN_NW];
+#pragma unroll
+  for (int i = 0; i < TOKEN_NW; ++i) top = fmaxf(top, ml[i * 32 + r].x);
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < TOKEN_NW; ++i) {
+    f[i] = __builtin_amdgcn_exp2f(ml[i * 32 + r].x - base);
+    tot += ml[i * 32 + r].y * f[i];
+  }
+  if (r >= a.R) return;
+  const int64_t at = ((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r;
+  constexpr int PER = DH / 2 / TOKEN_NW;                 // registers: 8 or 16
+#pragma unroll
+  for (int x = 0; x < PER; x += 4) {
+    const int reg = wave * PER + x;
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < TOKEN_NW; ++i) v[e] += image[(i * (DH / 2) + reg + e) * 64 + l] * f[i];
+    }
+    *reinterpret_cast<f32x4*>(a.part + at * DH + (reg >> 4) * 32 + acc_row(reg & 15, grp)) = v;
+  }
+  if (wave == 0 && grp == 0) a.part_ml[at] = float2{top, tot};
+}
+
+// parts -> out, lse2: eight columns to a lane
+template <int DH>
+__global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (DH / 8);
+  const int c = (int)(i % (DH / 8)) * 8;
+  if (row >= rows) return;
+  float m = -INFINITY, tot = 0.f;
+  f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  for (int s = 0; s < a.parts; ++s) {
+    const int64_t at = s * rows + row;
+    const float2 ml = a.part_ml[at];
+    const f32x4* p = reinterpret_cast<const f32x4*>(a.part + at * DH + c);
+    const float mn = fmaxf(m, ml.x), base = mn == -INFINITY ? 0.f : mn;
+    const float was = __builtin_amdgcn_exp2f(m - base), f = __builtin_amdgcn_exp2f(ml.x - base);
+    v[0] = v[0] * was + p[0] * f;
+    v[1] = v[1] * was + p[1] * f;
+    tot = tot * was + ml.y * f;
+    m = mn;
+  }
+  const float inv = tot == 0.f ? 0.f : 1.0f / tot;
+  v[0] *= inv; v[1] *= inv;
+  const int unit = (int)(row / a.R), r = (int)(row - (int64_t)unit * a.R);
+  *reinterpret_cast<u32x4*>(a.out + row_at<DH>(a, unit / a.Hkv, unit % a.Hkv, r, a.ldo) + c) = f32_to_bf16x8(v);
+  if (c == 0) a.lse2[row] = m + __builtin_amdgcn_logf(tot);
+}
+
+// ---- backward ----------------------------------------------------------------------------------
+// rowsum(do o) and the lse of every row, in the order of the list; behind the last row an lse of +inf, which makes its probabilities zero,
+// and so for a row without keys or with scores of -inf alone
+template <int DH>
+__global__ __launch_bounds__(256) void cross_stat_kernel(CrossArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (DH / 8);
+  const int c = (int)(i % (DH / 8)) * 8;
+  if (row >= (int64_t)a.B * a.Hkv * a.Rp) return;         // (whole rows: DH / 8 lanes go together)
+  const int unit = (int)(row / a.Rp), r = (int)(row - (int64_t)unit * a.Rp);
+  float d = 0.f, lse = INFINITY;
+  if (r < a.R) {
+    const int b = unit / a.Hkv, h = unit % a.Hkv;
+    f32x4 x[2], y[2];
+    bf16x8_to_f32(x, *reinterpret_cast<const u32x4*>(a.o + row_at<DH>(a, b, h, r, a.ldo) + c));
+    bf16x8_to_f32(y, *reinterpret_cast<const u32x4*>(a.dout + row_at<DH>(a, b, h, r, a.lddo) + c));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) d = __fmaf_rn(x[k >> 2][k & 3], y[k >> 2][k & 3], d);
+    lse = a.lse2[(int64_t)unit * a.R + r];
+    if (lse == -INFINITY) lse = INFINITY;
+  }
+#pragma unroll
+  for (int o = 1; o < DH / 8; o *= 2) d += __shfl_xor(d, o, 64);
+  if (c == 0) { a.stat_lse[row] = lse; a.stat_d[row] = lse == INFINITY ? 0.f : d; }
+}
+
+// dQ: a wave owns 32 rows, keys and values stream.
+template <int DH, int NW, int NS>
+__global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs a) {
+  char* smem = dtl_smem;
+  constexpr int SLOT = 2 * kTileBytes<DH>;
+  const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
+  const Where w = where(a, blocks);
+  const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
+  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
+  const int r = w.block * OWN * NW + wave * OWN + (l & 31);
+  const bool active = w.block * OWN * NW + wave * OWN < a.R;
+  const int rc = r < a.R ? r : a.R - 1;
+  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
+  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
+  Frag qf[DH / 16], of[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
+  load_owned<DH>(of, a.dout + row_at<DH>(a, w.b, w.h, rc, a.lddo));
+  const float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
+  f32x16 dq[DH / 32];
+  clear(dq);
+  const KeyLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * KeyLoads<DH, NW>::N;
+  auto issue = [&](int t) {
+    char* to = smem + (t - t0) % NS * SLOT;
+    loads.issue(K, a.ldk, t * TILE, n, to);
+    loads.issue(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  for (int t = t0; t < t1; ++t) {
+    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
+    __syncthreads();
+    if (t + NS - 1 < t1) issue(t + NS - 1);
+    if (!active) continue;
+    const char* Ks = smem + (t - t0) % NS * SLOT;
+    const char* Vs = Ks + kTileBytes<DH>;
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      f32x16 s[1], dp[1];
+      clear(s); clear(dp);
+#pragma unroll
+      for (int kk = 0; kk < DH / 16; ++kk) {
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, sub * 32, kk), qf[kk], s[0], 0, 0, 0);
+        dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Vs, sub * 32, kk), of[kk], dp[0], 0, 0, 0);
+      }
+      const int k0 = t * TILE + sub * 32;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) dp[0][x] = __builtin_amdgcn_exp2f(__fmaf_rn(s[0][x], a.c2, -lse)) * (dp[0][x] - D);
+      if (k0 + 32 > n) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (k0 + acc_row(x, grp) >= n) dp[0][x] = 0.f;
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const Frag ds = pack_frag(dp[0], ks);
+#pragma unroll
+        for (int dt = 0; dt < DH / 32; ++dt)
+          dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Ks, sub * 32 + ks * 16, dt * 32), ds, dq[dt], 0, 0, 0);
+      }
+    }
+  }
+  if (!active || r >= a.R) return;
+  if (a.parts == 1) store_owned<DH>(dq, a.scale, a.dq + row_at<DH>(a, w.b, w.h, r, a.lddq));
+  else store_owned32<DH>(dq, a.part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r) * DH);
+}
+
+// dK, dV: a wave owns 32 keys, the rows (queries and do) stream.
+template <int DH, int NW, int NS>
+__global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_kv_kernel(CrossArgs a) {
+  char* smem = dtl_smem;
+  constexpr int SLOT = 2 * kTileBytes<DH> + 2 * TILE * 4;   // queries, do, lse, D
+  const int blocks = (a.Sk + OWN * NW - 1) / (OWN * NW);
+  const Where w = where(a, blocks);
+  const int n = keys_of(a, w.b), j0 = w.block * OWN * NW;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
+  const int j = j0 + wave * OWN + (l & 31);
+  const int nt = j0 < n ? (a.R + TILE - 1) / TILE : 0;      // keys behind the sequence: zeros
+  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const bool active = j0 + wave * OWN < n;
+  Frag kf[DH / 16], vf[DH / 16];
+  f32x16 dk[DH / 32], dv[DH / 32];
+  clear(dk); clear(dv);
+  if (active) {
+    const int jc = j < n ? j : n - 1;
+    load_owned<DH>(kf, a.k + ((int64_t)w.b * a.Sk + jc) * a.ldk + w.h * DH);
+    load_owned<DH>(vf, a.v + ((int64_t)w.b * a.Sk + jc) * a.ldv + w.h * DH);
+  }
+  const RowLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * RowLoads<DH, NW>::N + 1;
+  const float* stat = (wave & 1 ? a.stat_d : a.stat_lse) + (int64_t)w.unit * a.Rp;   // (even waves bring the lse, odd ones D)
+  auto issue = [&](int t) {
+    char* to = smem + (t - t0) % NS * SLOT;
+    loads.issue(a, w.b, w.h, a.q, a.ldq, a.dout, a.lddo, t * TILE, to, to + kTileBytes<DH>);
+    load_floats(stat + t * TILE, to + 2 * kTileBytes<DH> + (wave & 1) * TILE * 4);
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  for (int t = t0; t < t1; ++t) {
+    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
+    __syncthreads();
+    if (t + NS - 1 < t1) issue(t + NS - 1);
+    if (!active) continue;
+    const char* Qs = smem + (t - t0) % NS * SLOT;
+    const char* Os = Qs + kTileBytes<DH>;
+    const float* lse = reinterpret_cast<const float*>(Os + kTileBytes<DH>);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      f32x16 s[1], dp[1];
+      clear(s); clear(dp);
+#pragma unroll
+      for (int kk = 0; kk < DH / 16; ++kk) {
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Qs, sub * 32, kk), kf[kk], s[0], 0, 0, 0);
+        dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Os, sub * 32, kk), vf[kk], dp[0], 0, 0, 0);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse + sub * 32 + 8 * q + 4 * grp);
+        const f32x4 D = *reinterpret_cast<const f32x4*>(lse + TILE + sub * 32 + 8 * q + 4 * grp);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[0][4 * q + x], a.c2, -ls[x]));
+          s[0][4 * q + x] = p;
+          dp[0][4 * q + x] = p * (dp[0][4 * q + x] - D[x]);
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const Frag p = pack_frag(s[0], ks), ds = pack_frag(dp[0], ks);
+#pragma unroll
+        for (int dt = 0; dt < DH / 32; ++dt) {
+          dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Os, sub * 32 + ks * 16, dt * 32), p, dv[dt], 0, 0, 0);
+          dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Qs, sub * 32 + ks * 16, dt * 32), ds, dk[dt], 0, 0, 0);
+        }
+      }
+    }
+  }
+  if (j >= a.Sk) return;
+  if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
+  if (a.parts == 1) {
+    store_owned<DH>(dk, a.scale, a.dk + ((int64_t)w.b * a.Sk + j) * a.lddk + w.h * DH);
+    store_owned<DH>(dv, 1.0f, a.dv + ((int64_t)w.b * a.Sk + j) * a.lddv + w.h * DH);
+  } else {
+    float* to = a.part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.Sk + j) * 2 * DH;
+    store_owned32<DH>(dk, to);
+    store_owned32<DH>(dv, to + DH);
+  }
+}
+// parts -> dq (KV false), or dk and dv
+template <int DH, bool KV>
+__global__ __launch_bounds__(256) void cross_bwd_join_kernel(CrossArgs a) {
+  constexpr int W = KV ? 2 * DH : DH;
+  const int per = KV ? a.Sk : a.R;
+  const int64_t rows = (int64_t)a.B * a.Hkv * per;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
+  const int c = (int)(i % (W / 8)) * 8;
+  if (row >= rows) return;
+  f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  for (int s = 0; s < a.parts; ++s) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(a.part + (s * rows + row) * W + c);
+    v[0] += p[0]; v[1] += p[1];
+  }
+  const int unit = (int)(row / per), r = (int)(row - (int64_t)unit * per), b = unit / a.Hkv, h = unit % a.Hkv;
+  const bool values = KV && c >= DH;
+  if (!values) { v[0] *= a.scale; v[1] *= a.scale; }
+  uint16_t* to = !KV ? a.dq + row_at<DH>(a, b, h, r, a.lddq) + c
+                 : values ? a.dv + ((int64_t)b * a.Sk + r) * a.lddv + h * DH + c - DH : a.dk + ((int64_t)b * a.Sk + r) * a.lddk + h * DH + c;
+  *reinterpret_cast<u32x4*>(to) = f32_to_bf16x8(v);
+}
+
+// ---- host ----------------------------------------------------------------------------------
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int kMostParts = 64;
+
+// Parts of the streamed side: as many as give `want` workgroups, each with `least` tiles or more.
+int parts_for(int64_t blocks, int64_t tiles, int64_t want, int64_t least) {
+  int64_t p = want / (blocks > 0 ? blocks : 1);
+  if (p > tiles / least) p = tiles / least;
+  return (int)(p < 1 ? 1 : p > kMostParts ? kMostParts : p);
+}
+
+struct CrossPlan {
+  bool token;                              // up to 32 rows to a key/value head
+  int R, Rp, fwd_parts, q_parts, kv_parts;
+  size_t fwd_ml, fwd_bytes;                // forward: [sums][pairs]
+  size_t d, part, bwd_bytes;               // backward: [lse][D][sums]
+};
+bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh) {
+  if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128)) return false;
+  if (B > (1 << 20) || Sq > (1 << 24) || Sk > (1 << 24) || H > (1 << 16)) return false;
+  const int64_t U = B * Hkv, R = H / Hkv * Sq;
+  if (R > (1ll << 30) || U * up(R, OWN) > (1ll << 30) || U * up(Sk, OWN) > (1ll << 30) || U * R * dh / 8 > (1ll << 38) || U * Sk * dh / 8 > (1ll << 38)) return false;
+  p.R = (int)R; p.Rp = (int)(up(R, TILE) * TILE);
+  p.token = R <= OWN;
+  p.fwd_parts = p.token ? parts_for(U, up(Sk, TOKEN_KEYS), 512, 8) : parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
+  p.q_parts = parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
+  p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(R, TILE), 512, 4);
+  auto round = [](size_t b) { return (b + 255) / 256 * 256; };
+  const bool parts = p.token || p.fwd_parts > 1;
+  p.fwd_ml = parts ? round((size_t)4 * p.fwd_parts * U * R * dh) : 0;
+  p.fwd_bytes = parts ? p.fwd_ml + round((size_t)8 * p.fwd_parts * U * R) : 0;
+  p.d = round((size_t)4 * U * p.Rp);
+  p.part = 2 * p.d;
+  const size_t q = p.q_parts > 1 ? (size_t)4 * p.q_parts * U * R * dh : 0, kv = p.kv_parts > 1 ? (size_t)8 * p.kv_parts * U * Sk * dh : 0;
+  p.bwd_bytes = p.part + round(q > kv ? q : kv);
+  return true;
+}
+
+template <auto Kern>
+rv_status launch(const CrossArgs& a, int64_t grid, int threads, int lds, hipStream_t st) {
+  static const hipError_t done = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (done != hipSuccess || grid > 0x7FFFFFFF) return RV_E_DEVICE;
+  hipLaunchKernelGGL(Kern, dim3((unsigned)grid), dim3(threads), lds, st, a);
+  return rv_launch_status();
+}
+
+bool bad(const void* p, uintptr_t to) { return !p || ((uintptr_t)p & (to - 1)); }
+bool bad_pitch(int64_t ld, int64_t cols) { return ld < cols || ld % 8 || ld > (1 << 24); }
+
+CrossArgs common_args(const CrossPlan& p, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* klen, int B, int Sq,
+                      int Sk, int H, int Hkv, int dh) {
+  CrossArgs a{};
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+  a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.klen = klen;
+  a.B = B; a.Sq = Sq; a.Sk = Sk; a.share = H / Hkv; a.Hkv = Hkv; a.R = p.R; a.Rp = p.Rp; a.parts = 1;
+  a.scale = 1.0f / sqrtf((float)dh);
+  a.c2 = 1.4426950408889634f * a.scale;
+  return a;
+}
+
+template <int DH>
+rv_status forward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
+  const int64_t U = (int64_t)a.B * a.Hkv;
+  a.parts = p.fwd_parts;
+  a.part = (float*)work; a.part_ml = (float2*)(work + p.fwd_ml);
+  if (p.token) {
+    constexpr int ring = TOKEN_NW * kTokenRing<DH>, image = TOKEN_NW * (DH / 2 * 64 * 4 + 32 * 8);
+    RV_TRY((launch<cross_token_kernel<DH>>(a, U * a.parts, 64 * TOKEN_NW, ring > image ? ring : image, st)));
+  } else {
+    RV_TRY((launch<cross_fwd_kernel<DH, 4, 2>>(a, U * a.parts * up(a.R, OWN * 4), 256, 2 * 2 * kTileBytes<DH>, st)));
+  }
+  if (p.token || a.parts > 1) RV_TRY((launch<cross_join_kernel<DH>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
+  return RV_OK;
+}
+template <int DH>
+rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
+  const int64_t U = (int64_t)a.B * a.Hkv;
+  a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.part = (float*)(work + p.part);
+  RV_TRY((launch<cross_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
+  a.parts = p.q_parts;
+  RV_TRY((launch<cross_bwd_q_kernel<DH, 4, 2>>(a, U * a.parts * up(a.R, OWN * 4), 256, 2 * 2 * kTileBytes<DH>, st)));
+  if (a.parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
+  a.parts = p.kv_parts;
+  RV_TRY((launch<cross_bwd_kv_kernel<DH, 4, 2>>(a, U * a.parts * up(a.Sk, OWN * 4), 256, 2 * (2 * kTileBytes<DH> + 2 * TILE * 4), st)));
+  if (a.parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
+  return RV_OK;
+}
+
+}  // namespace
+
+extern "C" rv_status rv_k_cross_attention_work(int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, int backward, size_t* bytes) {
+  CrossPlan p;
+  if (!bytes || !make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  *bytes = backward ? p.bwd_bytes : p.fwd_bytes;
+  return RV_OK;
+}
+
+extern "C" rv_status rv_k_cross_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* klen,
+                                              void* out, int64_t ldo, float* lse2, int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head,
+                                              void* work, size_t work_bytes, void* stream) {
+  CrossPlan p;
+  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  const int64_t cols = (int64_t)n_heads * d_head, kcols = (int64_t)n_kv_heads * d_head;
+  if (bad(q, 16) || bad(k, 16) || bad(v, 16) || bad(out, 16) || bad(lse2, 4) || ((uintptr_t)klen & 3)) return RV_E_INVAL;
+  if (bad_pitch(ldq, cols) || bad_pitch(ldk, kcols) || bad_pitch(ldv, kcols) || bad_pitch(ldo, cols)) return RV_E_INVAL;
+  if (p.fwd_bytes && (bad(work, 256) || work_bytes < p.fwd_bytes)) return RV_E_INVAL;
+  CrossArgs a = common_args(p, q, ldq, k, ldk, v, ldv, klen, B, Sq, Sk, n_heads, n_kv_heads, d_head);
+  a.out = (uint16_t*)out; a.ldo = ldo; a.lse2 = lse2;
+  return d_head == 64 ? forward<64>(a, p, (char*)work, (hipStream_t)stream) : forward<128>(a, p, (char*)work, (hipStream_t)stream);
+}
+
+extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* klen,
+                                              const void* out, int64_t ldo, const void* dout, int64_t lddo, const float* lse2, void* dq, int64_t lddq,
+                                              void* dk, int64_t lddk, void* dv, int64_t lddv, int B, int Sq, int Sk, int n_heads, int n_kv_heads,
+                                              int d_head, void* work, size_t work_bytes, void* stream) {
+  CrossPlan p;
+  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  const int64_t cols = (int64_t)n_heads * d_head, kcols = (int64_t)n_kv_heads * d_head;
+  if (bad(q, 16) || bad(k, 16) || bad(v, 16) || bad(out, 16) || bad(dout, 16) || bad(lse2, 4) || bad(dq, 16) || bad(dk, 16) || bad(dv, 16) ||
+      ((uintptr_t)klen & 3)) return RV_E_INVAL;
+  if (bad_pitch(ldq, cols) || bad_pitch(ldk, kcols) || bad_pitch(ldv, kcols) || bad_pitch(ldo, cols) || bad_pitch(lddo, cols) || bad_pitch(lddq, cols) ||
+      bad_pitch(lddk, kcols) || bad_pitch(lddv, kcols)) return RV_E_INVAL;
+  if (bad(work, 256) || work_bytes < p.bwd_bytes) return RV_E_INVAL;
+  CrossArgs a = common_args(p, q, ldq, k, ldk, v, ldv, klen, B, Sq, Sk, n_heads, n_kv_heads, d_head);
+  a.o = (const uint16_t*)out; a.ldo = ldo; a.dout = (const uint16_t*)dout; a.lddo = lddo; a.lse2 = (float*)lse2;
+  a.dq = (uint16_t*)dq; a.lddq = lddq; a.dk = (uint16_t*)dk; a.lddk = lddk; a.dv = (uint16_t*)dv; a.lddv = lddv;
+  return d_head == 64 ? backward<64>(a, p, (char*)work, (hipStream_t)stream) : backward<128>(a, p, (char*)work, (hipStream_t)stream);
+}

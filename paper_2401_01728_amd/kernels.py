@@ -4,7 +4,7 @@ import ctypes
 import torch
 
 from . import _lib
-from .api import _check, _ptr, _stream_handle
+from .api import _check, _flat, _on, _ptr, _stream_handle
 
 EPI_BF16, EPI_BF16_BIAS, EPI_F32_BIAS_RESID, EPI_BF16_BIAS_GELU, EPI_BF16_DGELU, EPI_F32, EPI_F32_BIAS_RESID_BF16 = range(7)
 
@@ -130,3 +130,54 @@ def attention_bwd_static(qkv, out, dout, lse2, dqkv, mb, S, d, H, stream=None):
     _check(_lib.lib().rv_k_attention_bwd_static(_ptr(qkv), _ptr(out), _ptr(dout), _ptr(lse2), _ptr(dqkv), mb, S, d,
                                                 H, _stream_handle(stream)))
     return dqkv
+
+
+def _tokens(t, B, S, cols):
+    """bf16 [B, S, cols], sequences one behind the other; the pitch of a token's row."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (B, S, cols), (t.dtype, tuple(t.shape), (B, S, cols))
+    ld = t.stride(1) if S > 1 else t.stride(0) if B > 1 else cols
+    assert t.stride(2) == 1 and (B == 1 or t.stride(0) == S * ld), "tokens one pitch apart, columns neighbours: strides %s" % (t.stride(),)
+    return ld
+
+
+def _cross_sizes(q, k, n_heads, n_kv_heads):
+    B, Sq, cols = q.shape
+    assert n_heads >= 1 and cols % n_heads == 0, (cols, n_heads)
+    return B, Sq, k.shape[1], n_heads, n_kv_heads, cols // n_heads
+
+
+def _cross_work(sizes, backward, device):
+    n = ctypes.c_size_t(0)
+    _check(_lib.lib().rv_k_cross_attention_work(*sizes, backward, ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None, n.value
+
+
+def cross_attention_fwd(q, k, v, n_heads, n_kv_heads, klen=None, out=None, stream=None):
+    """rv_k_cross_attention_fwd: q bf16 [B, Sq, n_heads * d_head], k and v bf16 [B, Sk, n_kv_heads * d_head] (columns of a wider matrix
+    or not), klen int32 [B] or None -> (out like q, lse2 fp32 [B, n_heads, Sq])."""
+    sizes = B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
+    stream = _on(stream, q, k, v, klen, out)
+    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+        out = torch.empty(B, Sq, H * dh, dtype=torch.bfloat16, device=q.device) if out is None else out
+        lse2 = torch.empty(B, H, Sq, dtype=torch.float32, device=q.device)
+        work, n = _cross_work(sizes, 0, q.device)
+        _check(_lib.lib().rv_k_cross_attention_fwd(
+            _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
+            _ptr(_flat(klen, torch.int32, (B,)) if klen is not None else None), _ptr(out), _tokens(out, B, Sq, H * dh), _ptr(lse2), *sizes,
+            _ptr(work), n, _stream_handle(stream)))
+    return out, lse2
+
+
+def cross_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, klen=None, dq=None, dk=None, dv=None, stream=None):
+    """rv_k_cross_attention_bwd: (dq, dk, dv) of the above; out and lse2 are the forward's."""
+    sizes = B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
+    stream = _on(stream, q, k, v, klen, out, dout, lse2, dq, dk, dv)
+    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+        dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v)))
+        work, n = _cross_work(sizes, 1, q.device)
+        _check(_lib.lib().rv_k_cross_attention_bwd(
+            _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
+            _ptr(_flat(klen, torch.int32, (B,)) if klen is not None else None), _ptr(out), _tokens(out, B, Sq, H * dh),
+            _ptr(dout), _tokens(dout, B, Sq, H * dh), _ptr(_flat(lse2, torch.float32, (B, H, Sq))), _ptr(dq), _tokens(dq, B, Sq, H * dh),
+            _ptr(dk), _tokens(dk, B, Sk, Hkv * dh), _ptr(dv), _tokens(dv, B, Sk, Hkv * dh), *sizes, _ptr(work), n, _stream_handle(stream)))
+    return dq, dk, dv

@@ -1,0 +1,202 @@
+"""Cross-attention and its gradients against the definition in 64 bits on the same bf16 operands.
+
+Tolerances, element by element; a bf16 rounding is off by at most 2^-8 of the value, and the fp32 steps in front of it (scores of dh
+products, an exponential, sums over the keys) are kept together as `slack`, relative to a probability:
+  out   each probability is rounded once, the result once:       (2^-8 + slack) sum p |v| + 2^-8 |out|
+  dv    the same over the rows:                                  (2^-8 + slack) sum p |do| + 2^-8 |dv|
+  dq    ds = p (dp - D), rounded once; D = rowsum(do o) with the o given, rounded when it was written, so off by 2^-8 sum |do o|, and dp
+        by fp32 alone: per element of ds (2^-8 + slack) |ds| + p (2^-8 sum |do o| + slack sum |do| |v|), through |k|, then 2^-8 |dq|
+  dk    the same through |q|
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2401_01728_amd import kernels
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(seed, B, Sq, Sk, H, Hkv, dh, klen):
+    g = torch.Generator().manual_seed(seed)
+    q = (torch.randn(B, Sq, H * dh, generator=g) * 1.3).to(torch.bfloat16)
+    kv = torch.randn(B, Sk, 2 * Hkv * dh, generator=g).to(torch.bfloat16)
+    do = (torch.randn(B, Sq, H * dh, generator=g) * 0.02).to(torch.bfloat16)
+    n = [Sk] * B if klen is None else [max(0, min(Sk, x)) for x in klen]
+    for b in range(B):
+        kv[b, n[b]:] = float("nan")
+    return q, kv[..., :Hkv * dh], kv[..., Hkv * dh:], do, n
+
+
+def _reference(q, k, v, do, n, H, Hkv, o_given=None):
+    B, Sq, _ = q.shape
+    Sk = k.shape[1]
+    dh = q.shape[2] // H
+    f64 = dict(dtype=torch.float64)
+    out, lse2 = torch.zeros(q.shape, **f64), torch.full((B, H, Sq), -math.inf, **f64)
+    dq, dk, dv = torch.zeros(q.shape, **f64), torch.zeros(k.shape, **f64), torch.zeros(k.shape, **f64)
+    e_out, e_dq, e_dk, e_dv = (torch.zeros_like(t) for t in (out, dq, dk, dv))
+    for b in range(B):
+        if n[b] == 0:
+            continue
+        for h in range(H):
+            c, kc = slice(h * dh, (h + 1) * dh), slice(h // (H // Hkv) * dh, (h // (H // Hkv) + 1) * dh)
+            qh, kh, vh, doh = q[b, :, c].double(), k[b, :n[b], kc].double(), v[b, :n[b], kc].double(), do[b, :, c].double()
+            s = qh @ kh.T / math.sqrt(dh)
+            lse = torch.logsumexp(s, 1, keepdim=True)
+            p = torch.exp(s - lse)
+            out[b, :, c], lse2[b, h] = p @ vh, lse[:, 0] / math.log(2.0)
+            slack = (dh + 8) * 2.0 ** -24 * float((qh.abs() @ kh.abs().T).max()) / math.sqrt(dh) * 2 + (n[b] / 32 + 64) * 2.0 ** -24
+            r = 2.0 ** -8 + slack
+            e_out[b, :, c] = r * (p @ vh.abs()) + 2.0 ** -8 * out[b, :, c].abs()
+            dp = doh @ vh.T
+            D = (doh * out[b, :, c]).sum(1, keepdim=True)
+            ds = p * (dp - D)
+            e_ds = r * ds.abs() + p * (2.0 ** -8 * (doh * out[b, :, c]).abs().sum(1, keepdim=True) + slack * (doh.abs() @ vh.abs().T))
+            dq[b, :, c] = ds @ kh / math.sqrt(dh)
+            e_dq[b, :, c] = e_ds @ kh.abs() / math.sqrt(dh) + 2.0 ** -8 * dq[b, :, c].abs()
+            dk[b, :n[b], kc] += ds.T @ qh / math.sqrt(dh)
+            e_dk[b, :n[b], kc] += e_ds.T @ qh.abs() / math.sqrt(dh)
+            dv[b, :n[b], kc] += p.T @ doh
+            e_dv[b, :n[b], kc] += r * (p.T @ doh.abs())
+    e_dk += 2.0 ** -8 * dk.abs()
+    e_dv += 2.0 ** -8 * dv.abs()
+    # second order: a rounding of what is already off
+    return (out, lse2, dq, dk, dv), tuple(e * (1 + 2.0 ** -7) + 1e-30 for e in (e_out, e_dq, e_dk, e_dv))
+
+
+def _near(got, ref, bound):
+    got = got.cpu().double()
+    assert bool(torch.isfinite(got).all())
+    over = (got - ref).abs() / bound
+    assert bool((over <= 1.0).all()), "off by %.3g of the bound at %s" % (float(over.max()), int(over.argmax()))
+
+
+def _check(B, Sq, Sk, H, Hkv, dh, klen, seed=0):
+    q, k, v, do, n = _inputs(seed, B, Sq, Sk, H, Hkv, dh, klen)
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    # k and v stay columns of one matrix
+    kv = torch.cat([k, v], -1).cuda()
+    kd, vd = kv[..., :Hkv * dh], kv[..., Hkv * dh:]
+    length = torch.tensor(klen, dtype=torch.int32).cuda() if klen is not None else None
+    got_out, got_lse = kernels.cross_attention_fwd(q.cuda(), kd, vd, H, Hkv, length)
+    _near(got_out, out, e_out)
+    got_lse = got_lse.cpu().double()
+    assert torch.equal(got_lse == -math.inf, lse2 == -math.inf)
+    there = lse2 != -math.inf
+    assert float((got_lse - lse2)[there].abs().max() if there.any() else 0.0) <= 2.0 ** -12
+    got = kernels.cross_attention_bwd(q.cuda(), kd, vd, got_out, do.cuda(), got_lse.float().cuda(), H, Hkv, length)
+    for a, ref, bound in zip(got, (dq, dk, dv), (e_dq, e_dk, e_dv)):
+        _near(a, ref, bound)
+
+
+# single tokens and few rows (one wave's worth and one more), lengths around a tile of 32 and 64 and a workgroup's 128, long walks that are cut
+# into parts on either side, shared heads, both widths of a head
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh", [
+    (1, 1, 1, 1, 1, 64), (1, 1, 1, 1, 1, 128), (2, 1, 31, 2, 1, 64), (1, 1, 33, 8, 1, 128), (3, 1, 700, 4, 4, 64), (1, 4, 1000, 8, 1, 128),
+    (1, 1, 5000, 3, 3, 128), (2, 3, 65, 33, 3, 64), (1, 2, 97, 32, 2, 64), (1, 33, 64, 1, 1, 64), (2, 32, 63, 1, 1, 128), (1, 63, 129, 2, 2, 64),
+    (2, 65, 31, 2, 1, 128), (1, 128, 128, 1, 1, 64), (1, 129, 257, 3, 1, 128), (2, 200, 1, 2, 2, 64), (1, 40, 1500, 6, 2, 64), (1, 300, 77, 12, 12, 64),
+    (1, 1030, 70, 2, 2, 128), (1, 7, 400, 20, 4, 128), (8, 70, 200, 16, 16, 64)])
+def test_forward_and_backward(B, Sq, Sk, H, Hkv, dh):
+    _check(B, Sq, Sk, H, Hkv, dh, None)
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh,klen", [
+    (3, 1, 200, 4, 2, 64, [200, 0, 65]), (4, 1, 130, 4, 1, 128, [1, 130, 0, 64]), (4, 70, 130, 2, 1, 64, [0, 63, 64, 129]),
+    (3, 150, 300, 4, 2, 128, [1, 257, 300]), (2, 40, 90, 3, 3, 64, [0, 0]), (3, 33, 100, 2, 2, 128, [-5, 1000, 32]), (2, 20, 2000, 2, 2, 64, [1999, 3])])
+def test_lengths(B, Sq, Sk, H, Hkv, dh, klen):
+    """Sequences of their own lengths, none among them; what lies behind is not a number."""
+    _check(B, Sq, Sk, H, Hkv, dh, klen, seed=1)
+
+
+def test_strides_and_what_lies_beside():
+    B, Sq, Sk, H, Hkv, dh = 2, 70, 100, 4, 2, 64
+    q, k, v, do, _ = _inputs(2, B, Sq, Sk, H, Hkv, dh, None)
+    length = torch.tensor([100, 37], dtype=torch.int32).cuda()
+    ref = kernels.cross_attention_fwd(q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), H, Hkv, length)
+    grads = kernels.cross_attention_bwd(q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), ref[0], do.cuda(), ref[1], H, Hkv, length)
+
+    def within(t, extra, fill):
+        w = torch.full((*t.shape[:2], t.shape[2] + extra), fill, dtype=torch.bfloat16, device="cuda")
+        w[..., 8:8 + t.shape[2]] = t.cuda()
+        return w, w[..., 8:8 + t.shape[2]]
+
+    nan = float("nan")
+    qs, ks, vs, dos = (within(t, e, nan)[1] for t, e in ((q, 24), (k, 16), (v, 40), (do, 8)))
+    wide, out = within(torch.zeros_like(q), 32, 5.0)
+    got = kernels.cross_attention_fwd(qs, ks, vs, H, Hkv, length, out=out)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    assert bool((wide[..., :8] == 5.0).all()) and bool((wide[..., 8 + H * dh:] == 5.0).all())
+    wides = [within(torch.zeros_like(t), 16, 5.0) for t in (q, k, v)]
+    got = kernels.cross_attention_bwd(qs, ks, vs, out, dos, ref[1], H, Hkv, length, *(t for _, t in wides))
+    for a, b, (w, t) in zip(got, grads, wides):
+        assert a is t and torch.equal(a, b)
+        assert bool((w[..., :8] == 5.0).all()) and bool((w[..., -8:] == 5.0).all())
+
+
+def test_scores_without_bounds():
+    """Scores of thousands: the running maximum moves late and far; a key that nobody else comes near takes all."""
+    B, Sq, Sk, H, dh = 1, 50, 500, 2, 64
+    q, k, v, do, n = _inputs(3, B, Sq, Sk, H, H, dh, None)
+    k = k.clone()
+    k[:, 411] *= 600.0
+    k[:, 70] *= 100.0
+    (out, _, _, _, _), _ = _reference(q, k, v, do, n, H, H)
+    got, lse2 = kernels.cross_attention_fwd(q.cuda(), k.cuda(), v.cuda().contiguous(), H, H)
+    # a probability next to another may be off by the error of a score of thousands: (dh + 8) 2^-24 sum |q k| / sqrt(dh)
+    err = (dh + 8) * 2.0 ** -24 * float((q.double().abs().max() ** 2 * 0 + (q[0].double().abs() @ k[0].double().abs().T).max())) / math.sqrt(dh)
+    assert float((got.cpu().double() - out).abs().max()) <= (2.0 ** -7 + 2 * err) * float(v.double().abs().max())
+    assert bool(torch.isfinite(lse2).all())
+
+
+def test_gradient_against_differences():
+    B, Sq, Sk, H, Hkv, dh = 1, 10, 70, 2, 1, 64
+    q, k, v, do, n = _inputs(4, B, Sq, Sk, H, Hkv, dh, [50])
+    length = torch.tensor([50], dtype=torch.int32).cuda()
+    out, lse2 = kernels.cross_attention_fwd(q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), H, Hkv, length)
+    grads = kernels.cross_attention_bwd(q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), out, do.cuda(), lse2, H, Hkv, length)
+
+    def total(t):
+        o = torch.cat([torch.softmax(t[0][0, :, h * dh:(h + 1) * dh] @ t[1][0, :50].T / math.sqrt(dh), -1) @ t[2][0, :50] for h in range(H)], -1)
+        return float((o * do[0].double()).sum())
+
+    base = [q.double(), k.double(), v.double()]
+    g = torch.Generator().manual_seed(8)
+    for i, grad in enumerate(grads):
+        u = torch.randn(grad.shape, generator=g, dtype=torch.float64)
+        if i:
+            u[:, 50:] = 0.0
+        plus, minus = ([t + e * u if x == i else t for x, t in enumerate(base)] for e in (1e-5, -1e-5))
+        plus, minus = ([torch.nan_to_num(t) for t in s] for s in (plus, minus))
+        num = (total(plus) - total(minus)) / 2e-5
+        terms = grad.cpu().double() * u
+        assert abs(float(terms.sum()) - num) <= 2.0 ** -6 * float(terms.abs().sum())
+
+
+def test_other_stream_and_captured_graph():
+    B, Sq, Sk, H, Hkv, dh = 2, 40, 900, 4, 2, 64
+    q, k, v, do, _ = _inputs(5, B, Sq, Sk, H, Hkv, dh, None)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    length = torch.tensor([900, 411], dtype=torch.int32).cuda()
+    both = lambda st=None: (lambda o: (*o, *kernels.cross_attention_bwd(q, k, v, o[0], do, o[1], H, Hkv, length, stream=st)))(  # noqa: E731
+        kernels.cross_attention_fwd(q, k, v, H, Hkv, length, stream=st))
+    ref = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = both(side)
+    side.synchronize()
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+        token = kernels.cross_attention_fwd(q[:, :1].contiguous(), k, v, H, Hkv, length)
+    for seed in range(4):
+        for t, fresh in zip((q, k, v, do), _inputs(30 + seed, B, Sq, Sk, H, Hkv, dh, None)):
+            t.copy_(fresh)
+        length.copy_(torch.tensor([900 - seed, 64 * seed], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*got, *token), (*both(), *kernels.cross_attention_fwd(q[:, :1].contiguous(), k, v, H, Hkv, length))):
+            assert torch.equal(a, b)
