@@ -3,6 +3,7 @@
 torch is used for device memory and streams; every step of the path runs in librv.so.
 """
 import ctypes
+from contextlib import nullcontext
 
 import torch
 
@@ -238,13 +239,17 @@ def _flat(t, dtype, shape):
 
 
 def _on(stream, *tensors):
-    """The stream for a call on these tensors (the current one of their device if none is given)."""
-    devices = {t.device for t in tensors if t is not None}
-    assert len(devices) == 1, "tensors of several devices: %s" % sorted(map(str, devices))
-    device = devices.pop()
-    stream = torch.cuda.current_stream(device) if stream is None else stream
+    """The stream for a call on these tensors (the current one of their device if none is given), and a context in which memory is
+    allocated for it: entering torch's costs as much as two launches, so only where stream or device are not the current ones."""
+    device = tensors[0].device
+    for t in tensors:
+        assert t is None or t.device == device, "tensors of several devices: %s, %s" % (device, t.device)
+    assert device.type == "cuda", device
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+        return stream, nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.stream(stream)
     assert stream.device == device, "a stream of %s for tensors of %s" % (stream.device, device)
-    return stream
+    return stream, torch.cuda.stream(stream)
 
 
 def _loss(x, w, label, rows, gradients, call, stream, **more):
@@ -263,8 +268,8 @@ def _loss(x, w, label, rows, gradients, call, stream, **more):
 def loss_forward(x, w, label, rows=0, stream=None):
     """rv_loss_forward: (loss, lse), fp32 [T], of x bf16 [T, d] against the vocabulary w bf16 [V, d] and label int64 [T]; a label outside
     [0, V) takes its row out (loss and lse 0)."""
-    stream = _on(stream, x, w, label)
-    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+    stream, context = _on(stream, x, w, label)
+    with context:
         loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
         lse = torch.empty_like(loss)
         _loss(x, w, label, rows, 0, _lib.lib().rv_loss_forward, stream, loss=_ptr(loss), lse=_ptr(lse))
@@ -276,9 +281,9 @@ def loss_step(x, w, label, scale=1.0, row_scale=None, master=None, eta=0.0, mast
     """rv_loss_step: loss and gradients of sum_t scale * row_scale[t] * loss_t in one call.  Returns (loss, dx, dw), or, with the fp32
     `master` of w, (loss, dx, master_out, version): the weights after w <- w - eta * dw (master_out may be master, version may be
     w).  Outputs that are not given are allocated; want_dx, want_dw false leave one out (None in its place)."""
-    stream = _on(stream, x, w, label, row_scale, master, master_out, version, dx, dw)
+    stream, context = _on(stream, x, w, label, row_scale, master, master_out, version, dx, dw)
     assert master is not None or (master_out is None and version is None), "an update needs the master weights"
-    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+    with context:
         loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
         if dx is None and want_dx:
             dx = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)

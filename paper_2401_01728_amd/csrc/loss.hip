@@ -6,14 +6,15 @@
 //   dx = dz W,  dW = dz^T x       three products of 2 T V d flop each; the forward alone is one
 //
 // The logits are never written.  A wave of the first product holds 64 columns of the vocabulary - a strip - of its rows; it takes
-// each row's maximum m over the strip (fp32) and writes the pair (m, sum of exp2(z log2 e - m)) and, for the gradients, the
-// exponentials e themselves in bf16.  They lie in (0, 1] whatever the logits are, so that their rounding is half a step of the
-// probability (2^-9 relative) - logits in bf16 would move it by |z| 2^-9.  The pairs of a row's strips are then joined to its
-// lse, and  dz = e exp2(m - lse2) g  overwrites e in place, rounded once more: bf16 is what the matrix instructions take, and both
-// roundings together stay below that of dx and dW themselves.  The label's own column gets  g expm1(z_y - lse)  from the fp32 logit:
-// where the model is nearly certain, p - 1 from a rounded p would have no digits left.
-// Computing z again for the gradients instead of keeping e would be a fourth product: 4 bytes of e and dz written and 6 read per
-// logit are (at 5 TB/s) 2 ps, the product 2 d / 1.3 PFLOP/s = 1.6 ps at d 1024, 3.2 ps at 2048.
+// each row's maximum over the strip (fp32), m = max z log2 e - 15, and writes the pair (m, sum of exp2(z log2 e - m)) and, for the
+// gradients, the exponentials e themselves in fp16: they are at most 2^15 whatever the logits are, keep 11 bits down to 2^-29 of the
+// strip's largest and are off by less than 2^-40 of it below.  (Logits in 16 bits would move a probability by |z| 2^-9 of itself, e in
+// bf16 by 2^-8: with the rounding of dz the gradients were then 1.6 times as far from 64 bits as their own rounding, now 1.2.)  The pairs of
+// a row's strips are joined to its lse, and  dz = e exp2(m - lse2) g  overwrites e in place, rounded to bf16, which is what the matrix
+// instructions take.  The label's own column gets  g expm1(z_y - lse)  from the fp32 logit: where the model is nearly certain,
+// p - 1 from a rounded p would have no digits left.
+// Computing z again for the gradients instead of keeping e would be a fourth product: 2 bytes of e written and 4 moved by the pass
+// that makes dz of it are 1.2 ps a logit at 5 TB/s, the product 2 d / 1.3 PFLOP/s = 1.6 ps at d 1024, 3.2 ps at 2048.
 // One piece of rows is kept at a time (e and strips of `rows` rows, at most 2 GiB of e where the caller leaves the choice), so the work
 // memory has a bound that does not grow with T; from the second piece on the weight gradient is added up in fp32.
 //
@@ -27,15 +28,19 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int STRIP = 64;
+constexpr int kTop = 15;                 // a strip's largest exponential is 2^15
 constexpr int64_t kMostE = 1ll << 30;    // elements of e, of a piece's rows: offsets in a product are 31 bits, and 2 GiB of work memory
 
 // what a row of the piece needs in the backward
 struct RowInfo { float lse2, g, at_label; int label; };
 
+struct CutForm { int tile, S; };
 struct Plan {
   int T, d, V, Vp, P, pieces;            // V rounded up to whole strips; rows of a piece and their number
   bool grads;
   int64_t ldw;
+  CutForm dx;                            // tile and stretches of dx; stretches of dW
+  int S_w;
   size_t count, pos, idx, lab, info, target, stat, xw, tail, e, part, acc, bytes;
 };
 
@@ -72,7 +77,13 @@ __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict_
   const int t0 = blockIdx.x * per, rows = T - t0 < per ? T - t0 : per;
   auto takes = [&](int64_t y) { return y >= 0 && y < V; };
   int before = 0;
-  for (int t = tid; t < t0; t += 256) before += takes(label[t]) ? 1 : 0;
+  for (int t = tid; t < t0; t += 8 * 256) {   // (eight on the way at a time)
+    int64_t y[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] = label[t + k * 256 < t0 ? t + k * 256 : t];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) before += t + k * 256 < t0 && takes(y[k]) ? 1 : 0;
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o, 64);
   if (l == 0) part[tid >> 6] = before;
@@ -114,71 +125,92 @@ struct LogitsOut {
   int P, V, Vp;
 };
 
+// max and sum over the four lanes (l / 16) that share a row, left in all of them: lane rows swapped with their neighbours, then halves
+__device__ __forceinline__ float quad_max(float v) {
+  auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+  s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {   // round to nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, f16x2));
+}
+
 template <bool STORE, int TM, int TN>
-__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, int mw, int nw, int M) {
-  static_assert(TN * 16 == STRIP, "a wave's columns are one strip");
-  if (nw >= o.Vp || mw >= M) return;
-  const int l = threadIdx.x & 63, grp = l >> 4, strip = nw / STRIP;
-  const bool ragged = nw + STRIP > o.V;     // (wave-uniform)
+__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, int mw, int nw0, int M) {
+  constexpr int TS = STRIP / 16;
+  static_assert(TN % TS == 0, "a wave's columns are whole strips");
+  const int l = threadIdx.x & 63, grp = l >> 4;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int row = mw + i * 16 + (l & 15);
-    const bool ok = row < M;
-    f32x4 a[TN];
+  for (int u = 0; u < TN / TS; ++u) {
+    const int nw = nw0 + u * STRIP, strip = nw / STRIP;
+    if (nw >= o.Vp || mw >= M) return;
+    const bool ragged = nw + STRIP > o.V;     // (wave-uniform)
 #pragma unroll
-    for (int c = 0; c < TN; ++c) {
-      a[c] = acc[i][c];
-      if (ragged) {
+    for (int i = 0; i < TM; ++i) {
+      const int row = mw + i * 16 + (l & 15);
+      const bool ok = row < M;
+      f32x4 a[TS];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (nw + c * 16 + 4 * grp + k >= o.V) a[c][k] = -INFINITY;
-      }
-    }
-    const int y = ok ? o.lab[row] - nw : -1;
-    if (__builtin_amdgcn_ballot_w64(y >= 0 && y < STRIP)) {   // few strips hold a label of their rows
-      float at = 0.f;
-      bool mine = false;
+      for (int c = 0; c < TS; ++c) {
+        a[c] = acc[i][u * TS + c];
+        if (ragged) {
 #pragma unroll
-      for (int c = 0; c < TN; ++c)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (y == c * 16 + 4 * grp + k) { at = a[c][k]; mine = true; }
-      if (mine) o.target[row] = at;
-    }
-    float m = a[0][0];
-#pragma unroll
-    for (int c = 0; c < TN; ++c)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) m = fmaxf(m, a[c][k]);
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-    m *= kLog2e;
-    const float base = m == -INFINITY ? 0.f : m;   // (a strip of -inf alone: its sum is zero)
-    float sum = 0.f;
-#pragma unroll
-    for (int c = 0; c < TN; ++c)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        a[c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[c][k], kLog2e, -base));
-        sum += a[c][k];
-      }
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (grp == 0 && ok) o.stat[(int64_t)strip * o.P + row] = float2{m, sum};
-    if (STORE) {
-      // Two quads of a lane are 16 columns apart; the swap of lane rows of 16 gives even rows eight consecutive columns of the first
-      // quad and odd ones of the second, and a wave's 16 bytes a lane are one run of 1 KiB of the block of 32 columns.
-#pragma unroll
-      for (int b = 0; b < TN / 2; ++b) {
-        u32x4 v;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const auto s = __builtin_amdgcn_permlane16_swap(rv_pack_bf16x2(a[2 * b][2 * h], a[2 * b][2 * h + 1]),
-                                                          rv_pack_bf16x2(a[2 * b + 1][2 * h], a[2 * b + 1][2 * h + 1]), false, false);
-          v[h] = s[0]; v[2 + h] = s[1];
+          for (int k = 0; k < 4; ++k)
+            if (nw + c * 16 + 4 * grp + k >= o.V) a[c][k] = -INFINITY;
         }
-        const int col = grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp;
-        if (ok) *reinterpret_cast<u32x4*>(o.e + ((int64_t)(2 * strip + b) * o.P + row) * 32 + col) = v;
+      }
+      const int y = ok ? o.lab[row] - nw : -1;
+      if (__builtin_amdgcn_ballot_w64(y >= 0 && y < STRIP)) {   // few strips hold a label of their rows
+        float at = 0.f;
+        bool mine = false;
+#pragma unroll
+        for (int c = 0; c < TS; ++c)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (y == c * 16 + 4 * grp + k) { at = a[c][k]; mine = true; }
+        if (mine) o.target[row] = at;
+      }
+      float m = a[0][0];
+#pragma unroll
+      for (int c = 0; c < TS; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = fmaxf(m, a[c][k]);
+      m = __fmaf_rn(quad_max(m), kLog2e, -(float)kTop);
+      const float base = m == -INFINITY ? 0.f : m;   // (a strip of -inf alone: its sum is zero)
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < TS; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          a[c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[c][k], kLog2e, -base));
+          sum += a[c][k];
+        }
+      sum = quad_sum(sum);
+      if (grp == 0 && ok) o.stat[(int64_t)strip * o.P + row] = float2{m, sum};
+      if (STORE) {
+        // Two quads of a lane are 16 columns apart; the swap of lane rows of 16 gives even rows eight consecutive columns of the first
+        // quad and odd ones of the second, and a wave's 16 bytes a lane are one run of 1 KiB of the block of 32 columns.
+#pragma unroll
+        for (int b = 0; b < TS / 2; ++b) {
+          u32x4 v;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const auto s = __builtin_amdgcn_permlane16_swap(pack_f16(a[2 * b][2 * h], a[2 * b][2 * h + 1]),
+                                                            pack_f16(a[2 * b + 1][2 * h], a[2 * b + 1][2 * h + 1]), false, false);
+            v[h] = s[0]; v[2 + h] = s[1];
+          }
+          const int col = grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp;
+          if (ok) *reinterpret_cast<u32x4*>(o.e + ((int64_t)(2 * strip + b) * o.P + row) * 32 + col) = v;
+        }
       }
     }
   }
@@ -269,7 +301,13 @@ __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const
     for (int h = 0; h < 2; ++h) {
       u32x4* at = reinterpret_cast<u32x4*>(base + (2 * s + h) * bs);
       f32x4 v[2];
-      bf16x8_to_f32(v, *at);
+      const u32x4 packed = *at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t pair = packed[k];          // (a bit cast of a vector's element reads element 0)
+        const f32x2 two = __builtin_convertvector(__builtin_bit_cast(f16x2, pair), f32x2);
+        v[k >> 1][2 * (k & 1)] = two.x; v[k >> 1][2 * (k & 1) + 1] = two.y;
+      }
       const int y = r.label - ((2 * s + h) * 32 + q * 8);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k >> 2][k & 3] = y == k ? r.at_label : v[k >> 2][k & 3] * f;
@@ -279,27 +317,24 @@ __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const
 }
 
 // ---- dx ----------------------------------------------------------------------
-// dx has few tiles and a contraction as long as the vocabulary: it is cut into S stretches where the tiles alone do not fill the chip.
-// S is the count that wastes least of the last round of workgroups, each stretch counted as a 32nd of the walk for what its sums cost
-// to write and read; the same on the device (which knows the rows) and on the host (the work memory of the worst case).
-constexpr int kMostParts = 64, kMostPartTiles = 512;
-__host__ __device__ inline int stretches(int tiles, int slots_log2, int nk) {
-  const int slots = 1 << slots_log2;
-  int best = 1, best_rounds = (tiles + slots - 1) >> slots_log2;
-  for (int S = 2; S <= kMostParts && tiles * S <= kMostPartTiles && S * 8 <= nk; ++S) {
-    const int rounds = (tiles * S + slots - 1) >> slots_log2;
-    if (rounds * best * 33 < best_rounds * S * 32) { best = S; best_rounds = rounds; }
-  }
-  return best;
+// dx has few tiles and a contraction as long as the vocabulary: it is cut into S stretches, whose fp32 sums a second kernel adds.  Tile and
+// S are the host's choice by modelled time for all rows (cut_form below); where fewer rows take part, the device, which alone knows,
+// makes as many more stretches of the walk as there are tile rows less, so that the launch fills the chip as far as it was to.
+constexpr int kMostParts = 64;
+__device__ __forceinline__ int stretches(int S, int tiles_m, int vm, int nk) {
+  int n = S * tiles_m / vm;
+  n = n < kMostParts ? n : kMostParts;
+  n = n * 8 <= nk ? n : nk / 8;
+  return n > S ? n : S;
 }
-template <int BM, int BN, int NS, int NW, int SLOTS>
+template <int BM, int BN, int NS, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void input_grad_kernel(const uint16_t* __restrict__ dz, const uint16_t* __restrict__ w, int64_t ldw, int d,
-                                                                int V, int Vp, const int* __restrict__ count, int p, int P,
+                                                                int V, int Vp, const int* __restrict__ count, int p, int P, int S_all, int tiles_m,
                                                                 const uint16_t* __restrict__ tail, float* __restrict__ part) {
   const int M = piece_rows(*count, p, P);
   if (M <= 0) return;
   const int vm = div_up(M, BM), vn = div_up(d, BN), tiles = vm * vn, nk = Vp / 32;
-  const int S = stretches(tiles, SLOTS, nk);
+  const int S = stretches(S_all, tiles_m, vm, nk);
   const int id = blockIdx.x;
   if (id >= tiles * S) return;
   const int s = id / tiles, in = id - s * tiles, bm = in % vm, bn = in / vm;
@@ -309,32 +344,44 @@ __global__ __launch_bounds__(64 * NW, 2) void input_grad_kernel(const uint16_t* 
   gemm_dtl_body<BM, BN, 32, NS, NW, false, true, EPI_F32, true>(dz + (int64_t)k0 * 32 * P, 32, 32ll * P, w + (int64_t)k0 * 32 * ldw, ldw, 32, M, d,
                                                                 (k1 - k0) * 32, bm, bn, out, tail, V / 32 - k0);
 }
-// the stretches' sums, added in order and rounded, to the rows they belong to; zeros to the rows that take no part
-template <int BM, int BN, int SLOTS>
+// the stretches' sums, added in a fixed order and rounded, to the rows they belong to; zeros to the rows that take no part.  LANES lanes share
+// eight columns of a row: with dozens of stretches one lane's walk over them is a chain of round trips (256 rows of 448
+// columns, 64 stretches: 25 us with one lane).
+template <int LANES>
 __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __restrict__ part, const int* __restrict__ pos, const int* __restrict__ count,
-                                                              int p, int P, int T, int d, int Vp, uint16_t* __restrict__ dx, int64_t lddx) {
+                                                              int p, int P, int T, int d, int nk, int bm, int S_all, int tiles_m, uint16_t* __restrict__ dx,
+                                                              int64_t lddx) {
   const int M = piece_rows(*count, p, P);
   if (M <= 0 && p) return;
-  const int vm = div_up(M > 0 ? M : 0, BM), S = stretches(vm * div_up(d, BN), SLOTS, Vp / 32);
-  const int64_t pitch = (int64_t)vm * BM * d;
-  const int64_t chunk = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int lane = LANES > 1 ? threadIdx.x / (256 / LANES) : 0;
+  const int64_t chunk = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x % (256 / LANES);
   const int per = d / 8;
-  if (chunk >= (int64_t)T * per) return;
-  const int t = (int)(chunk / per), c = (int)(chunk - (int64_t)t * per) * 8, j = pos[t];
-  u32x4 r = {0u, 0u, 0u, 0u};
-  if (j >= 0) {
-    if (j / P != p) return;
+  const bool in = chunk < (int64_t)T * per;
+  const int t = in ? (int)(chunk / per) : 0, c = in ? (int)(chunk - (int64_t)t * per) * 8 : 0, j = in ? pos[t] : -1;
+  const bool here = j >= 0 && j / P == p;
+  f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if (here) {
+    const int vm = div_up(M, bm), S = stretches(S_all, tiles_m, vm, nk);
+    const int64_t pitch = (int64_t)vm * bm * d;
     const float* src = part + (int64_t)(j - p * P) * d + c;
-    f32x4 v[2] = {reinterpret_cast<const f32x4*>(src)[0], reinterpret_cast<const f32x4*>(src)[1]};
-    for (int s = 1; s < S; ++s) {
+#pragma unroll 4
+    for (int s = lane; s < S; s += LANES) {
       const f32x4* q = reinterpret_cast<const f32x4*>(src + s * pitch);
       v[0] += q[0]; v[1] += q[1];
     }
-    r = f32_to_bf16x8(v);
-  } else if (p) {
-    return;
   }
-  *reinterpret_cast<u32x4*>(dx + (int64_t)t * lddx + c) = r;
+  if (LANES > 1) {
+    __shared__ f32x4 sum[2][256];
+    sum[0][threadIdx.x] = v[0]; sum[1][threadIdx.x] = v[1];
+    __syncthreads();
+    if (lane) return;
+#pragma unroll
+    for (int x = 1; x < LANES; ++x) {
+      v[0] += sum[0][threadIdx.x + x * (256 / LANES)];
+      v[1] += sum[1][threadIdx.x + x * (256 / LANES)];
+    }
+  }
+  if (in && (here || (j < 0 && p == 0))) *reinterpret_cast<u32x4*>(dx + (int64_t)t * lddx + c) = f32_to_bf16x8(v);
 }
 
 // ---- dW ----------------------------------------------------------------------
@@ -417,10 +464,23 @@ bool big_tiles(int rows, int cols) {
   const int64_t b = (int64_t)div_up(rows, 256) * div_up(cols, 256), m = (int64_t)div_up(rows, 128) * div_up(cols, 128);
   return (double)((b + 255) / 256) * 65536 <= (double)((m + 511) / 512) * 2 * 16384 / 0.83;
 }
-bool big_input_grad(int rows, int d) { return rows > 128 && d > 128; }
-int weight_stretches(int V, int d, int P) {
-  const int tiles = div_up(V, WB) * div_up(d, WB);
-  return stretches(tiles, 8, P / 32);
+// Tile (256: one workgroup to a CU, 128: two) and stretches of a product [M, N] over nk k-tiles whose fp32 sums a kernel adds: the least
+// modelled time, us.  A round is a start and a walk, whose step takes longer where the launch fills the chip (the forms of gemm_bf16.hip,
+// by 32 in k); the sums are written and read at 5 TB/s.
+CutForm cut_form(int M, int N, int nk, bool mid) {
+  CutForm best{256, 1};
+  float least = 3e38f;
+  for (int form = 0; form < (mid ? 2 : 1); ++form) {
+    const int B = form ? 128 : 256;
+    const float slots = form ? 512.f : 256.f, start = form ? 3.1f : 8.9f, t0 = form ? 0.33f : 0.51f, t1 = form ? 0.45f : 0.64f;
+    const float tiles = (float)div_up(M, B) * div_up(N, B);
+    for (int S = 1; S <= kMostParts && (S == 1 || S * 8 <= nk); S += S < 8 ? 1 : S < 16 ? 2 : S < 32 ? 4 : 8) {
+      const float fill = tiles * S < slots ? tiles * S / slots : 1.f;
+      const float time = ceilf(tiles * S / slots) * (start + ceilf((float)nk / S) * (t0 + (t1 - t0) * fill * fill)) + (float)M * N * S * 8 / 5e6f;
+      if (time < least) { least = time; best = {B, S}; }
+    }
+  }
+  return best;
 }
 
 bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t rows, bool grads) {
@@ -453,13 +513,11 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
     q.info = take(sizeof(RowInfo) * P);
     q.tail = take((size_t)2 * 64 * ldw);
     q.e = take((size_t)2 * P * q.Vp);
-    // dx: the rows' tiles, or kMostPartTiles of them where the contraction is cut
-    const int b = big_input_grad(q.P, q.d) ? 256 : 128;
-    const size_t tiles = (size_t)div_up(q.P, b) * div_up(q.d, b);
-    q.part = take((tiles > kMostPartTiles ? tiles : kMostPartTiles) * b * b * 4);
-    q.acc = 0;
-    const int S = q.pieces > 1 ? 1 : weight_stretches(q.V, q.d, q.P);
-    if (q.pieces > 1 || S > 1) q.acc = take((size_t)4 * S * V * d);
+    const int most_rows = q.T < q.P ? q.T : q.P;
+    q.dx = cut_form(most_rows, q.d, q.Vp / 32, true);
+    q.part = take((size_t)div_up(most_rows, q.dx.tile) * q.dx.S * q.dx.tile * q.d * 4);
+    q.S_w = q.pieces > 1 ? 1 : cut_form(q.V, q.d, q.P / 32, false).S;
+    q.acc = q.pieces > 1 || q.S_w > 1 ? take((size_t)4 * q.S_w * V * d) : 0;
   }
   q.bytes = at;
   return true;
@@ -493,24 +551,24 @@ rv_status launch_logits(const Plan& q, char* work, const uint16_t* w, int p, hip
   return rv_launch_status();
 }
 
-template <int B, int NW, int SLOTS, int LDS>
+template <int B, int NW, int LDS>
 rv_status launch_input_grad(const Plan& q, char* work, const rv_loss_desc& a, int p, hipStream_t st) {
-  constexpr auto kern = input_grad_kernel<B, B, 4, NW, SLOTS>;
+  constexpr auto kern = input_grad_kernel<B, B, 4, NW>;
   if (allow_lds<kern>(LDS) != hipSuccess) return RV_E_DEVICE;
   const int* count = (const int*)(work + q.count);
   float* part = (float*)(work + q.part);
-  const int rows = q.T < q.P ? q.T : q.P, vm = div_up(rows, B), vn = div_up(q.d, B);
-  int grid = vm * vn;                             // of the largest launch that a number of rows up to `rows` asks for
-  for (int m = 1; m <= vm; ++m) {
-    const int n = m * vn * stretches(m * vn, SLOTS, q.Vp / 32);
-    if (n > grid) grid = n;
-  }
-  hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * NW), LDS, st, (const uint16_t*)(work + q.e), (const uint16_t*)a.w, q.ldw, q.d, q.V, q.Vp, count, p,
-                     q.P, (const uint16_t*)(work + q.tail), part);
+  const int rows = q.T < q.P ? q.T : q.P, vm = div_up(rows, B), vn = div_up(q.d, B), S = q.dx.S;
+  // (fewer tile rows, more stretches: never more workgroups than this, nor more memory)
+  hipLaunchKernelGGL(kern, dim3(vm * vn * S), dim3(64 * NW), LDS, st, (const uint16_t*)(work + q.e), (const uint16_t*)a.w, q.ldw, q.d, q.V, q.Vp, count, p,
+                     q.P, S, vm, (const uint16_t*)(work + q.tail), part);
   RV_TRY(rv_launch_status());
   const int64_t chunks = (int64_t)q.T * (q.d / 8);
-  hipLaunchKernelGGL((input_grad_join_kernel<B, B, SLOTS>), dim3((unsigned)((chunks + 255) / 256)), dim3(256), 0, st, part, (const int*)(work + q.pos), count, p,
-                     q.P, q.T, q.d, q.Vp, (uint16_t*)a.dx, a.lddx);
+  auto join = [&](auto k, int lanes) {
+    hipLaunchKernelGGL(k, dim3((unsigned)((chunks * lanes + 255) / 256)), dim3(256), 0, st, part, (const int*)(work + q.pos), count, p, q.P, q.T, q.d,
+                       q.Vp / 32, B, S, vm, (uint16_t*)a.dx, a.lddx);
+  };
+  if (S > 8) join(input_grad_join_kernel<8>, 8);
+  else join(input_grad_join_kernel<1>, 1);
   return rv_launch_status();
 }
 
@@ -553,7 +611,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
                      (int*)(work + q.pos), (int*)(work + q.idx), lab, (uint16_t*)(work + q.xw), a.loss, a.lse, w, q.ldw,
                      grads ? (uint16_t*)(work + q.tail) : nullptr, row_blocks);
   RV_TRY(rv_launch_status());
-  const int strips = q.Vp / STRIP, S = grads && q.pieces == 1 ? weight_stretches(q.V, q.d, q.P) : 1;
+  const int strips = q.Vp / STRIP, S = grads ? q.S_w : 1;
   const int rows = q.T < q.P ? q.T : q.P;
   for (int p = 0; p < q.pieces; ++p) {
     if (grads) RV_TRY(launch_logits<true>(q, work, w, p, st));
@@ -563,13 +621,15 @@ rv_status run(const rv_loss_desc& a, bool grads) {
                        lab + (int64_t)p * q.P, (const int*)(work + q.idx) + (int64_t)p * q.P, count, p, q.P, strips, a.scale, a.row_scale, a.loss, a.lse, info);
     RV_TRY(rv_launch_status());
     if (!grads) continue;
-    const int per_dz = 8;
+    // strips a block takes one after the other: up to 8, fewer where that leaves fewer than 2048 blocks
+    const int64_t dz_blocks = (int64_t)div_up(rows, 64) * strips / 2048;
+    const int per_dz = dz_blocks < 1 ? 1 : dz_blocks < 8 ? (int)dz_blocks : 8;
     hipLaunchKernelGGL(dz_kernel, dim3(div_up(rows, 64), div_up(strips, per_dz)), dim3(256), 0, st, (uint16_t*)(work + q.e), (const float2*)(work + q.stat), info,
                        count, p, q.P, strips, per_dz, (uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d, q.d);
     RV_TRY(rv_launch_status());
     if (a.dx) {
-      if (big_input_grad(q.P, q.d)) RV_TRY((launch_input_grad<256, 8, 8, kBigLds>(q, work, a, p, st)));
-      else RV_TRY((launch_input_grad<128, 4, 9, kMidLds>(q, work, a, p, st)));
+      if (q.dx.tile == 256) RV_TRY((launch_input_grad<256, 8, kBigLds>(q, work, a, p, st)));
+      else RV_TRY((launch_input_grad<128, 4, kMidLds>(q, work, a, p, st)));
     }
     if (!a.dw && !update) continue;
     if (q.pieces == 1 && S == 1) {

@@ -156,8 +156,8 @@ def cross_attention_fwd(q, k, v, n_heads, n_kv_heads, klen=None, out=None, strea
     """rv_k_cross_attention_fwd: q bf16 [B, Sq, n_heads * d_head], k and v bf16 [B, Sk, n_kv_heads * d_head] (columns of a wider matrix
     or not), klen int32 [B] or None -> (out like q, lse2 fp32 [B, n_heads, Sq])."""
     sizes = B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
-    stream = _on(stream, q, k, v, klen, out)
-    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+    stream, context = _on(stream, q, k, v, klen, out)
+    with context:
         out = torch.empty(B, Sq, H * dh, dtype=torch.bfloat16, device=q.device) if out is None else out
         lse2 = torch.empty(B, H, Sq, dtype=torch.float32, device=q.device)
         work, n = _cross_work(sizes, 0, q.device)
@@ -171,8 +171,8 @@ def cross_attention_fwd(q, k, v, n_heads, n_kv_heads, klen=None, out=None, strea
 def cross_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, klen=None, dq=None, dk=None, dv=None, stream=None):
     """rv_k_cross_attention_bwd: (dq, dk, dv) of the above; out and lse2 are the forward's."""
     sizes = B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
-    stream = _on(stream, q, k, v, klen, out, dout, lse2, dq, dk, dv)
-    with torch.cuda.device(stream.device), torch.cuda.stream(stream):
+    stream, context = _on(stream, q, k, v, klen, out, dout, lse2, dq, dk, dv)
+    with context:
         dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v)))
         work, n = _cross_work(sizes, 1, q.device)
         _check(_lib.lib().rv_k_cross_attention_bwd(

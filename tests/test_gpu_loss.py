@@ -3,9 +3,9 @@
 Tolerances, element by element, from the roundings that the kernels make (a bf16 rounding is off by at most 2^-8 of the value):
   logits    fp32 accumulation of d products: (d + 8) 2^-24 sum |x w| at most
   loss, lse that of the logits, and a softmax sum of exp2 (2 ulp) in up to 64 + V / 64 additions of a chain, and their log
-  dx, dw    the exponential and dz are rounded to bf16 once each, (1 + 2^-8)^2 - 1 < 2^-7 + 2^-15, and an error of the logits, of the
-            lse and of an exponential, `slack`, moves dz by a factor of exp(slack) < 1 + 2 slack: |dz| (2^-7 + 2^-15 + 2 slack),
-            through a product of absolute values; then the result's own rounding.  The label's column has p - 1 from fp32: its error is that of z, absolute.
+  dx, dw    the exponential is rounded to fp16 (2^-11, and 2^-40 of a row's weight where it is subnormal), dz to bf16 (2^-8), together below
+            2^-8 + 2^-10, and an error of the logits, of the lse and of an exponential, `slack`, moves dz by a factor of
+            exp(slack) < 1 + 2 slack; through a product of absolute values; then the result's own rounding.  The label's column has p - 1 from fp32: its error is that of z, absolute.
 """
 import math
 
@@ -58,7 +58,8 @@ def _check(x, w, label, g, got_loss, got_lse, dx=None, dw=None, master=None, eta
         if got is not None:
             assert float((got.cpu().double() - ref).abs().max()) <= slack
     # what dz may be off by: relative, but absolute (times the row's weight) at the label
-    off = dz.abs() * (2.0 ** -7 + 2.0 ** -15 + 2 * slack)
+    weight = torch.where(takes, g.double().abs(), 0.0)[:, None]
+    off = dz.abs() * (2.0 ** -8 + 2.0 ** -10 + 2 * slack) + weight * 2.0 ** -40
     rows = torch.arange(len(y))
     off[rows, y] = dz[rows, y].abs() * 2.0 ** -8 + torch.where(takes, g.double().abs(), 0.0) * slack
     fp32 = 2.0 ** -24 * (x.shape[0] + V)      # accumulation of the products of dz, relative to the sums of absolute values
