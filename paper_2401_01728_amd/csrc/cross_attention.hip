@@ -34,9 +34,10 @@ struct CrossArgs {
   const uint16_t* o; const uint16_t* dout; int64_t lddo;
   uint16_t* dq; uint16_t* dk; uint16_t* dv;
   int64_t lddq, lddk, lddv;
-  float* stat_lse; float* stat_d;        // [B][Hkv][Rp], +inf and 0 behind the last row
-  float* part; float2* part_ml;          // sums of the parts
-  int B, Sq, Sk, share, Hkv, R, Rp, parts;
+  float* stat_lse; float* stat_d;        // [B][Hkv][Rp]: see cross_stat_kernel
+  float* part; float2* part_ml;          // forward: sums of the parts
+  float* q_part; float* kv_part;         // backward
+  int B, Sq, Sk, share, Hkv, R, Rp, parts, q_parts, kv_parts, kv_grid;
   float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
 };
 
@@ -56,14 +57,14 @@ __device__ __forceinline__ int64_t row_at(const CrossArgs& a, int b, int h, int 
 // blocks of one (head, sequence), which read the same keys, are neighbours, and the sequences of one head follow one another - their
 // lengths differ, and a range of heads of every sequence is as long as any other.
 struct Where { int b, h, part, block, unit; };
-__device__ __forceinline__ Where where(const CrossArgs& a, int blocks) {
-  const int total = gridDim.x, base = total / 8, rem = total % 8;
-  const int g = blockIdx.x % 8, v = g * base + (g < rem ? g : rem) + blockIdx.x / 8;
+__device__ __forceinline__ Where where(const CrossArgs& a, int blocks, int parts, int id, int total) {
+  const int base = total / 8, rem = total % 8;
+  const int g = id % 8, v = g * base + (g < rem ? g : rem) + id / 8;
   Where w;
   w.block = v % blocks;
   const int x = v / blocks;
-  w.part = x % a.parts;
-  const int u = x / a.parts;
+  w.part = x % parts;
+  const int u = x / parts;
   w.b = u % a.B; w.h = u / a.B;
   w.unit = w.b * a.Hkv + w.h;
   return w;
@@ -120,59 +121,43 @@ __device__ __forceinline__ void clear(f32x16 (&v)[N]) {
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 
-// A wave's share of a tile of keys: TILE rows from k0 on, clamped to the last key.
+// A wave's share of the loads of a tile of ROWS rows: load i of lane l is chunk (i NW + wave) 64 + l of the tile in LDS.  A load brings STEP rows
+// further than the one before; where that is a multiple of the swizzle's period all of a lane's loads have one column.
 template <int DH, int NW, int ROWS = TILE>
-struct KeyLoads {
-  static constexpr int N = ROWS * DH / 8 / 64 / NW;      // loads per lane
-  int row[N];
-  unsigned col[N];                                       // bytes
+struct TileLoads {
+  static constexpr int N = ROWS * DH / 8 / 64 / NW, STEP = NW * 64 / (DH / 8);
+  static constexpr bool kOneColumn = STEP % 16 == 0;
+  int row, col[kOneColumn ? 1 : N];                      // first row; columns in elements
   int wave;
-  __device__ __forceinline__ explicit KeyLoads(int w) : wave(w) {
-    const int l = threadIdx.x & 63;
+  __device__ __forceinline__ explicit TileLoads(int w) : wave(w) {
+    const int slot = wave * 64 + (threadIdx.x & 63);
+    row = slot / (DH / 8);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int slot = (i * NW + wave) * 64 + l;
-      row[i] = slot / (DH / 8);
-      col[i] = (unsigned)((slot % (DH / 8)) ^ swizzle<DH>(row[i])) * 16;
-    }
+    for (int i = 0; i < (kOneColumn ? 1 : N); ++i) col[i] = ((slot % (DH / 8)) ^ swizzle<DH>(row + i * STEP)) * 8;
   }
-  __device__ __forceinline__ void issue(const uint16_t* base, int64_t ld, int k0, int n, char* lds) const {
+  __device__ __forceinline__ int column(int i) const { return col[kOneColumn ? 0 : i]; }
+  // keys k0 .. of a sequence of n, clamped to the last one
+  __device__ __forceinline__ void keys(const uint16_t* base, int64_t ld, int k0, int n, char* lds) const {
     const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)lds + wave * 1024);
     const uint16_t* from = base + (int64_t)k0 * ld;
     const int last = n - 1 - k0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = row[i] < last ? row[i] : last;
-      dtl_load_s(from, (unsigned)r * (unsigned)(ld * 2) + col[i], m0v + i * NW * 1024);
+      const int r = row + i * STEP < last ? row + i * STEP : last;
+      dtl_load_s(from, (unsigned)r * (unsigned)(ld * 2) + column(i) * 2, m0v + i * NW * 1024);
     }
   }
-};
-// The same of rows of the list of a key/value head's query rows (out of the last row: clamped to it).
-template <int DH, int NW>
-struct RowLoads {
-  static constexpr int N = TILE * DH / 8 / 64 / NW;
-  int row[N];
-  int col[N];                                            // elements
-  int wave;
-  __device__ __forceinline__ explicit RowLoads(int w) : wave(w) {
-    const int l = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int slot = (i * NW + wave) * 64 + l;
-      row[i] = slot / (DH / 8);
-      col[i] = ((slot % (DH / 8)) ^ swizzle<DH>(row[i])) * 8;
-    }
-  }
-  __device__ __forceinline__ void issue(const CrossArgs& a, int b, int h, const uint16_t* q, int64_t ldq, const uint16_t* o, int64_t ldo, int r0, char* lds_q,
-                                        char* lds_o) const {
+  // rows r0 .. of the list of a key/value head's query rows, clamped to the last one, of two matrices
+  __device__ __forceinline__ void rows(const CrossArgs& a, int b, int h, const uint16_t* q, int64_t ldq, const uint16_t* o, int64_t ldo, int r0, char* lds_q,
+                                       char* lds_o) const {
     const int mq = __builtin_amdgcn_readfirstlane((int)(size_t)lds_q + wave * 1024), mo = __builtin_amdgcn_readfirstlane((int)(size_t)lds_o + wave * 1024);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      int r = r0 + row[i];
+      int r = r0 + row + i * STEP;
       r = r < a.R ? r : a.R - 1;
       const int g = r / a.Sq, t = r - g * a.Sq;
       const int64_t tok = (int64_t)b * a.Sq + t;
-      const int c = (h * a.share + g) * DH + col[i];
+      const int c = (h * a.share + g) * DH + column(i);
       const uint16_t* pq = q + tok * ldq + c;
       const uint16_t* po = o + tok * ldo + c;
       asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(pq), "s"(mq + i * NW * 1024) : "memory", "m0");
@@ -258,7 +243,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH>;               // keys, values
   const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks);
+  const Where w = where(a, blocks, a.parts, blockIdx.x, gridDim.x);
   const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
   const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
@@ -274,12 +259,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
   clear(o);
   float m = -INFINITY, lsum = 0.f;
 
-  const KeyLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * KeyLoads<DH, NW>::N;
+  const TileLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * TileLoads<DH, NW>::N;
   auto issue = [&](int t) {
     char* to = smem + (t - t0) % NS * SLOT;
-    loads.issue(K, a.ldk, t * TILE, n, to);
-    loads.issue(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
+    loads.keys(K, a.ldk, t * TILE, n, to);
+    loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
@@ -328,13 +313,21 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
 
 // Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the four waves walks over tiles of 32
 // keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.
-constexpr int TOKEN_KEYS = 32, TOKEN_NW = 4;
-template <int DH> constexpr int kTokenSlots = DH == 128 ? 2 : 4;
-template <int DH> constexpr int kTokenRing = kTokenSlots<DH> * 2 * TOKEN_KEYS * DH * 2;
+#ifndef TOK_NW
+#define TOK_NW(DH) (DH == 128 ? 2 : 4)
+#define TOK_NS(DH) 2
+#endif
+#ifndef BWD_NW
+#define BWD_NW 4
+#endif
+constexpr int TOKEN_KEYS = 32;
+template <int DH> constexpr int kTokenWaves = TOK_NW(DH);
+template <int DH> constexpr int kTokenSlots = TOK_NS(DH);
+template <int DH> constexpr int kTokenRing = kTokenSlots<DH> * 2 * TOKEN_KEYS * DH * 2;   // of a wave
 template <int DH>
-__global__ __launch_bounds__(64 * TOKEN_NW) void cross_token_kernel(CrossArgs a) {
-  constexpr int NS = kTokenSlots<DH>, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
-  const Where w = where(a, 1);
+__global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(CrossArgs a) {
+  constexpr int TOKEN_NW = kTokenWaves<DH>, NS = kTokenSlots<DH>, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
+  const Where w = where(a, 1, a.parts, blockIdx.x, gridDim.x);
   const int n = keys_of(a, w.b), nt = (n + TOKEN_KEYS - 1) / TOKEN_KEYS;
   const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5, r = l & 31;
@@ -346,14 +339,14 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void cross_token_kernel(CrossArgs a)
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
-  const KeyLoads<DH, 1, TOKEN_KEYS> loads(0);
-  constexpr int LPT = 2 * KeyLoads<DH, 1, TOKEN_KEYS>::N;
+  const TileLoads<DH, 1, TOKEN_KEYS> loads(0);
+  constexpr int LPT = 2 * TileLoads<DH, 1, TOKEN_KEYS>::N;
   const int mine = t1 - t0 > wave ? (t1 - t0 - wave + TOKEN_NW - 1) / TOKEN_NW : 0;      // tiles t0 + wave, + TOKEN_NW, ...
   auto issue = [&](int i) {
     char* to = ring + i % NS * SLOT;
     const int k0 = (t0 + wave + i * TOKEN_NW) * TOKEN_KEYS;
-    loads.issue(K, a.ldk, k0, n, to);
-    loads.issue(V, a.ldv, k0, n, to + HALF);
+    loads.keys(K, a.ldk, k0, n, to);
+    loads.keys(V, a.ldv, k0, n, to + HALF);
   };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
@@ -420,26 +413,44 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void cross_token_kernel(CrossArgs a)
   if (wave == 0 && grp == 0) a.part_ml[at] = float2{top, tot};
 }
 
-// parts -> out, lse2: eight columns to a lane
-template <int DH>
+// parts -> out, lse2.  Eight columns to a lane; LANES lanes share the parts of one (a chain of up to 64 round trips else: single tokens of 8
+// heads over 32 parts took 20 us with one lane).
+template <int DH, int LANES>
 __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
+  constexpr int W = 256 / LANES;                         // column groups of a block
+  static_assert(W % (DH / 8) == 0, "whole rows");
+  __shared__ f32x4 sums[2][256];
+  __shared__ float2 pairs[256];
   const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (DH / 8);
+  const int lane = threadIdx.x / W;
+  const int64_t i = (int64_t)blockIdx.x * W + threadIdx.x % W, row = i / (DH / 8);
   const int c = (int)(i % (DH / 8)) * 8;
-  if (row >= rows) return;
   float m = -INFINITY, tot = 0.f;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  for (int s = 0; s < a.parts; ++s) {
-    const int64_t at = s * rows + row;
-    const float2 ml = a.part_ml[at];
-    const f32x4* p = reinterpret_cast<const f32x4*>(a.part + at * DH + c);
+  auto add = [&](float2 ml, f32x4 x, f32x4 y) {
     const float mn = fmaxf(m, ml.x), base = mn == -INFINITY ? 0.f : mn;
     const float was = __builtin_amdgcn_exp2f(m - base), f = __builtin_amdgcn_exp2f(ml.x - base);
-    v[0] = v[0] * was + p[0] * f;
-    v[1] = v[1] * was + p[1] * f;
+    v[0] = v[0] * was + x * f;
+    v[1] = v[1] * was + y * f;
     tot = tot * was + ml.y * f;
     m = mn;
+  };
+  if (row < rows) {
+#pragma unroll 4
+    for (int s = lane; s < a.parts; s += LANES) {
+      const int64_t at = s * rows + row;
+      const f32x4* p = reinterpret_cast<const f32x4*>(a.part + at * DH + c);
+      add(a.part_ml[at], p[0], p[1]);
+    }
   }
+  if (LANES > 1) {
+    sums[0][threadIdx.x] = v[0]; sums[1][threadIdx.x] = v[1]; pairs[threadIdx.x] = float2{m, tot};
+    __syncthreads();
+    if (lane) return;
+#pragma unroll
+    for (int x = 1; x < LANES; ++x) add(pairs[threadIdx.x + x * W], sums[0][threadIdx.x + x * W], sums[1][threadIdx.x + x * W]);
+  }
+  if (row >= rows) return;
   const float inv = tot == 0.f ? 0.f : 1.0f / tot;
   v[0] *= inv; v[1] *= inv;
   const int unit = (int)(row / a.R), r = (int)(row - (int64_t)unit * a.R);
@@ -448,8 +459,9 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
 }
 
 // ---- backward ----------------------------------------------------------------------------------
-// rowsum(do o) and the lse of every row, in the order of the list; behind the last row an lse of +inf, which makes its probabilities zero,
-// and so for a row without keys or with scores of -inf alone
+// What the accumulators of the scores and of do v^T begin with, for every row in the order of the list: -lse / c2, so that a probability is
+// exp2(c2 acc), and -D = -rowsum(do o), so that acc is dp - D.  Behind the last row, for a row without keys and for one with scores of -inf
+// alone -inf, which makes the probabilities zero, and 0.
 template <int DH>
 __global__ __launch_bounds__(256) void cross_stat_kernel(CrossArgs a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (DH / 8);
@@ -465,22 +477,23 @@ __global__ __launch_bounds__(256) void cross_stat_kernel(CrossArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) d = __fmaf_rn(x[k >> 2][k & 3], y[k >> 2][k & 3], d);
     lse = a.lse2[(int64_t)unit * a.R + r];
-    if (lse == -INFINITY) lse = INFINITY;
+    lse = lse == -INFINITY ? INFINITY : lse / a.c2;
   }
 #pragma unroll
   for (int o = 1; o < DH / 8; o *= 2) d += __shfl_xor(d, o, 64);
-  if (c == 0) { a.stat_lse[row] = lse; a.stat_d[row] = lse == INFINITY ? 0.f : d; }
+  if (c == 0) { a.stat_lse[row] = -lse; a.stat_d[row] = lse == INFINITY ? 0.f : -d; }
 }
 
 // dQ: a wave owns 32 rows, keys and values stream.
 template <int DH, int NW, int NS>
-__global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs a) {
+__device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH>;
   const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks);
+  const Where w = where(a, blocks, a.q_parts, id, grid);
+  const int parts = a.q_parts;
   const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
-  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int r = w.block * OWN * NW + wave * OWN + (l & 31);
   const bool active = w.block * OWN * NW + wave * OWN < a.R;
@@ -493,12 +506,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs 
   const float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
   f32x16 dq[DH / 32];
   clear(dq);
-  const KeyLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * KeyLoads<DH, NW>::N;
+  const TileLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * TileLoads<DH, NW>::N;
   auto issue = [&](int t) {
     char* to = smem + (t - t0) % NS * SLOT;
-    loads.issue(K, a.ldk, t * TILE, n, to);
-    loads.issue(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
+    loads.keys(K, a.ldk, t * TILE, n, to);
+    loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
@@ -514,7 +527,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs 
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
       f32x16 s[1], dp[1];
-      clear(s); clear(dp);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) { s[0][x] = lse; dp[0][x] = D; }
 #pragma unroll
       for (int kk = 0; kk < DH / 16; ++kk) {
         s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, sub * 32, kk), qf[kk], s[0], 0, 0, 0);
@@ -522,7 +536,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs 
       }
       const int k0 = t * TILE + sub * 32;
 #pragma unroll
-      for (int x = 0; x < 16; ++x) dp[0][x] = __builtin_amdgcn_exp2f(__fmaf_rn(s[0][x], a.c2, -lse)) * (dp[0][x] - D);
+      for (int x = 0; x < 16; ++x) dp[0][x] *= __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       if (k0 + 32 > n) {
 #pragma unroll
         for (int x = 0; x < 16; ++x)
@@ -538,22 +552,23 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_q_kernel(CrossArgs 
     }
   }
   if (!active || r >= a.R) return;
-  if (a.parts == 1) store_owned<DH>(dq, a.scale, a.dq + row_at<DH>(a, w.b, w.h, r, a.lddq));
-  else store_owned32<DH>(dq, a.part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r) * DH);
+  if (parts == 1) store_owned<DH>(dq, a.scale, a.dq + row_at<DH>(a, w.b, w.h, r, a.lddq));
+  else store_owned32<DH>(dq, a.q_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r) * DH);
 }
 
 // dK, dV: a wave owns 32 keys, the rows (queries and do) stream.
 template <int DH, int NW, int NS>
-__global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_kv_kernel(CrossArgs a) {
+__device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH> + 2 * TILE * 4;   // queries, do, lse, D
   const int blocks = (a.Sk + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks);
+  const Where w = where(a, blocks, a.kv_parts, id, grid);
+  const int parts = a.kv_parts;
   const int n = keys_of(a, w.b), j0 = w.block * OWN * NW;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int j = j0 + wave * OWN + (l & 31);
   const int nt = j0 < n ? (a.R + TILE - 1) / TILE : 0;      // keys behind the sequence: zeros
-  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const bool active = j0 + wave * OWN < n;
   Frag kf[DH / 16], vf[DH / 16];
   f32x16 dk[DH / 32], dv[DH / 32];
@@ -563,12 +578,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_kv_kernel(CrossArgs
     load_owned<DH>(kf, a.k + ((int64_t)w.b * a.Sk + jc) * a.ldk + w.h * DH);
     load_owned<DH>(vf, a.v + ((int64_t)w.b * a.Sk + jc) * a.ldv + w.h * DH);
   }
-  const RowLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * RowLoads<DH, NW>::N + 1;
+  const TileLoads<DH, NW> loads(wave);
+  constexpr int LPT = 2 * TileLoads<DH, NW>::N + 1;
   const float* stat = (wave & 1 ? a.stat_d : a.stat_lse) + (int64_t)w.unit * a.Rp;   // (even waves bring the lse, odd ones D)
   auto issue = [&](int t) {
     char* to = smem + (t - t0) % NS * SLOT;
-    loads.issue(a, w.b, w.h, a.q, a.ldq, a.dout, a.lddo, t * TILE, to, to + kTileBytes<DH>);
+    loads.rows(a, w.b, w.h, a.q, a.ldq, a.dout, a.lddo, t * TILE, to, to + kTileBytes<DH>);
     load_floats(stat + t * TILE, to + 2 * kTileBytes<DH> + (wave & 1) * TILE * 4);
   };
 #pragma unroll
@@ -586,22 +601,22 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_kv_kernel(CrossArgs
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
       f32x16 s[1], dp[1];
-      clear(s); clear(dp);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse + sub * 32 + 8 * q + 4 * grp);
+        const f32x4 D = *reinterpret_cast<const f32x4*>(lse + TILE + sub * 32 + 8 * q + 4 * grp);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) { s[0][4 * q + x] = ls[x]; dp[0][4 * q + x] = D[x]; }
+      }
 #pragma unroll
       for (int kk = 0; kk < DH / 16; ++kk) {
         s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Qs, sub * 32, kk), kf[kk], s[0], 0, 0, 0);
         dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Os, sub * 32, kk), vf[kk], dp[0], 0, 0, 0);
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f32x4 ls = *reinterpret_cast<const f32x4*>(lse + sub * 32 + 8 * q + 4 * grp);
-        const f32x4 D = *reinterpret_cast<const f32x4*>(lse + TILE + sub * 32 + 8 * q + 4 * grp);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float p = __builtin_amdgcn_exp2f(__fmaf_rn(s[0][4 * q + x], a.c2, -ls[x]));
-          s[0][4 * q + x] = p;
-          dp[0][4 * q + x] = p * (dp[0][4 * q + x] - D[x]);
-        }
+      for (int x = 0; x < 16; ++x) {
+        s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
+        dp[0][x] *= s[0][x];
       }
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
@@ -616,27 +631,37 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_bwd_kv_kernel(CrossArgs
   }
   if (j >= a.Sk) return;
   if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
-  if (a.parts == 1) {
+  if (parts == 1) {
     store_owned<DH>(dk, a.scale, a.dk + ((int64_t)w.b * a.Sk + j) * a.lddk + w.h * DH);
     store_owned<DH>(dv, 1.0f, a.dv + ((int64_t)w.b * a.Sk + j) * a.lddv + w.h * DH);
   } else {
-    float* to = a.part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.Sk + j) * 2 * DH;
+    float* to = a.kv_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.Sk + j) * 2 * DH;
     store_owned32<DH>(dk, to);
     store_owned32<DH>(dv, to + DH);
   }
+}
+template <int DH> constexpr int kBwdSlot = 2 * kTileBytes<DH> + 2 * TILE * 4;
+// Both in one launch, the longer workgroups (dK and dV: four products to dQ's three) first: where neither fills the chip by itself, and for
+// the last workgroups of the one to run beside the first of the other.
+template <int DH, int NW, int NS>
+__global__ __launch_bounds__(64 * NW, 2) void cross_bwd_kernel(CrossArgs a) {
+  if ((int)blockIdx.x < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, blockIdx.x, a.kv_grid);
+  else bwd_q_body<DH, NW, NS>(a, blockIdx.x - a.kv_grid, gridDim.x - a.kv_grid);
 }
 // parts -> dq (KV false), or dk and dv
 template <int DH, bool KV>
 __global__ __launch_bounds__(256) void cross_bwd_join_kernel(CrossArgs a) {
   constexpr int W = KV ? 2 * DH : DH;
-  const int per = KV ? a.Sk : a.R;
+  const int per = KV ? a.Sk : a.R, parts = KV ? a.kv_parts : a.q_parts;
+  const float* sums = KV ? a.kv_part : a.q_part;
   const int64_t rows = (int64_t)a.B * a.Hkv * per;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
   const int c = (int)(i % (W / 8)) * 8;
   if (row >= rows) return;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-  for (int s = 0; s < a.parts; ++s) {
-    const f32x4* p = reinterpret_cast<const f32x4*>(a.part + (s * rows + row) * W + c);
+#pragma unroll 4
+  for (int s = 0; s < parts; ++s) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(sums + (s * rows + row) * W + c);
     v[0] += p[0]; v[1] += p[1];
   }
   const int unit = (int)(row / per), r = (int)(row - (int64_t)unit * per), b = unit / a.Hkv, h = unit % a.Hkv;
@@ -662,7 +687,7 @@ struct CrossPlan {
   bool token;                              // up to 32 rows to a key/value head
   int R, Rp, fwd_parts, q_parts, kv_parts;
   size_t fwd_ml, fwd_bytes;                // forward: [sums][pairs]
-  size_t d, part, bwd_bytes;               // backward: [lse][D][sums]
+  size_t d, part, kv_part, bwd_bytes;      // backward: [lse][D][sums of dq][of dk and dv]
 };
 bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh) {
   if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128)) return false;
@@ -680,8 +705,8 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   p.fwd_bytes = parts ? p.fwd_ml + round((size_t)8 * p.fwd_parts * U * R) : 0;
   p.d = round((size_t)4 * U * p.Rp);
   p.part = 2 * p.d;
-  const size_t q = p.q_parts > 1 ? (size_t)4 * p.q_parts * U * R * dh : 0, kv = p.kv_parts > 1 ? (size_t)8 * p.kv_parts * U * Sk * dh : 0;
-  p.bwd_bytes = p.part + round(q > kv ? q : kv);
+  p.kv_part = p.part + (p.q_parts > 1 ? round((size_t)4 * p.q_parts * U * R * dh) : 0);
+  p.bwd_bytes = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : 0);
   return true;
 }
 
@@ -713,25 +738,28 @@ rv_status forward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   a.parts = p.fwd_parts;
   a.part = (float*)work; a.part_ml = (float2*)(work + p.fwd_ml);
   if (p.token) {
-    constexpr int ring = TOKEN_NW * kTokenRing<DH>, image = TOKEN_NW * (DH / 2 * 64 * 4 + 32 * 8);
-    RV_TRY((launch<cross_token_kernel<DH>>(a, U * a.parts, 64 * TOKEN_NW, ring > image ? ring : image, st)));
+    constexpr int waves = kTokenWaves<DH>, ring = waves * kTokenRing<DH>, image = waves * (DH / 2 * 64 * 4 + 32 * 8);
+    RV_TRY((launch<cross_token_kernel<DH>>(a, U * a.parts, 64 * waves, ring > image ? ring : image, st)));
   } else {
     RV_TRY((launch<cross_fwd_kernel<DH, 4, 2>>(a, U * a.parts * up(a.R, OWN * 4), 256, 2 * 2 * kTileBytes<DH>, st)));
   }
-  if (p.token || a.parts > 1) RV_TRY((launch<cross_join_kernel<DH>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
+  if (!p.token && a.parts == 1) return RV_OK;
+  if (a.parts > 4) RV_TRY((launch<cross_join_kernel<DH, 8>>(a, up(U * a.R * (DH / 8), 32), 256, 0, st)));
+  else RV_TRY((launch<cross_join_kernel<DH, 1>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
   return RV_OK;
 }
 template <int DH>
 rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
-  a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.part = (float*)(work + p.part);
+  a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
+  a.q_parts = p.q_parts; a.kv_parts = p.kv_parts;
   RV_TRY((launch<cross_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
-  a.parts = p.q_parts;
-  RV_TRY((launch<cross_bwd_q_kernel<DH, 4, 2>>(a, U * a.parts * up(a.R, OWN * 4), 256, 2 * 2 * kTileBytes<DH>, st)));
-  if (a.parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
-  a.parts = p.kv_parts;
-  RV_TRY((launch<cross_bwd_kv_kernel<DH, 4, 2>>(a, U * a.parts * up(a.Sk, OWN * 4), 256, 2 * (2 * kTileBytes<DH> + 2 * TILE * 4), st)));
-  if (a.parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
+  const int64_t kv = U * a.kv_parts * up(a.Sk, OWN * BWD_NW), q = U * a.q_parts * up(a.R, OWN * BWD_NW);
+  if (kv > 0x3FFFFFFF || q > 0x3FFFFFFF) return RV_E_INVAL;
+  a.kv_grid = (int)kv;
+  RV_TRY((launch<cross_bwd_kernel<DH, BWD_NW, 2>>(a, kv + q, 64 * BWD_NW, 2 * kBwdSlot<DH>, st)));
+  if (a.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
+  if (a.kv_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
   return RV_OK;
 }
 
