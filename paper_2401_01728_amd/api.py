@@ -4,6 +4,7 @@ torch is used for device memory and streams; every step of the path runs in libr
 """
 import ctypes
 from contextlib import nullcontext
+from functools import lru_cache
 
 import torch
 
@@ -252,16 +253,22 @@ def _on(stream, *tensors):
     return stream, torch.cuda.stream(stream)
 
 
+@lru_cache(maxsize=256)
+def _loss_work(T, d, V, ldw, rows, gradients):
+    n = ctypes.c_size_t(0)
+    _check(_lib.lib().rv_loss_work(T, d, V, ldw, rows, gradients, ctypes.byref(n)))
+    return n.value
+
+
 def _loss(x, w, label, rows, gradients, call, stream, **more):
     """Fills in what both calls share; scratch and outputs come from the call's own stream."""
     T, d = x.shape
     V = w.shape[0]
     a = _lib.LossDesc(x=_ptr(x), ldx=_rows(x, torch.bfloat16, (T, d)), w=_ptr(w), ldw=_rows(w, torch.bfloat16, (V, d)),
                       label=_ptr(_flat(label, torch.int64, (T,))), T=T, d=d, V=V, rows=rows, stream=_stream_handle(stream), **more)
-    n = ctypes.c_size_t(0)
-    _check(_lib.lib().rv_loss_work(T, d, V, a.ldw, rows, gradients, ctypes.byref(n)))
-    work = torch.empty(n.value, dtype=torch.uint8, device=x.device)
-    a.work, a.work_bytes = _ptr(work), n.value
+    a.work_bytes = _loss_work(T, d, V, a.ldw, rows, gradients)
+    work = torch.empty(a.work_bytes, dtype=torch.uint8, device=x.device)
+    a.work = _ptr(work)
     _check(call(ctypes.byref(a)))
 
 

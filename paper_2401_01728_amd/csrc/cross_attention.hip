@@ -24,6 +24,8 @@ namespace {
 constexpr int TILE = 64;                 // streamed rows
 constexpr int OWN = 32;                  // rows or keys a wave owns
 
+// blocks of rows or keys of a (sequence, key/value head), parts of the streamed side, and how the list of them is dealt out (where)
+struct Grid { int blocks, parts, groups; };
 struct CrossArgs {
   const uint16_t* q; const uint16_t* k; const uint16_t* v;
   int64_t ldq, ldk, ldv;
@@ -37,7 +39,8 @@ struct CrossArgs {
   float* stat_lse; float* stat_d;        // [B][Hkv][Rp]: see cross_stat_kernel
   float* part; float2* part_ml;          // forward: sums of the parts
   float* q_part; float* kv_part;         // backward
-  int B, Sq, Sk, share, Hkv, R, Rp, parts, q_parts, kv_parts, kv_grid;
+  int B, Sq, Sk, share, Hkv, R, Rp, kv_grid;
+  Grid fwd, bq, bkv;
   float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
 };
 
@@ -54,20 +57,23 @@ __device__ __forceinline__ int64_t row_at(const CrossArgs& a, int b, int h, int 
 }
 
 // Workgroup -> (sequence, key/value head, part, block): ids go to the 8 XCDs in turn; each takes a contiguous range of a list in which the
-// blocks of one (head, sequence), which read the same keys, are neighbours, and the sequences of one head follow one another - their
-// lengths differ, and a range of heads of every sequence is as long as any other.
+// blocks of one (head, sequence), which read the same keys, are neighbours.  Where sequences have lengths of their own a range has to hold as
+// much of each as any other: the list then goes through the heads, or through `groups` equal shares of a head's blocks where
+// there are fewer than eight heads or no multiple of it, and has a share's blocks of every sequence behind one another (16 heads over 4, lengths of
+// 2048 .. 0: 238 us with whole heads, 232 with halves).
+__host__ __device__ inline int share_of(const Grid& g) { return (g.blocks * g.parts + g.groups - 1) / g.groups; }
 struct Where { int b, h, part, block, unit; };
-__device__ __forceinline__ Where where(const CrossArgs& a, int blocks, int parts, int id, int total) {
-  const int base = total / 8, rem = total % 8;
-  const int g = id % 8, v = g * base + (g < rem ? g : rem) + id / 8;
-  Where w;
-  w.block = v % blocks;
-  const int x = v / blocks;
-  w.part = x % parts;
-  const int u = x / parts;
-  w.b = u % a.B; w.h = u / a.B;
+__device__ __forceinline__ bool where(const CrossArgs& a, const Grid& g, int id, int total, Where& w) {
+  const int base = total / 8, rem = total % 8, x = id % 8, share = share_of(g);
+  const int v = x * base + (x < rem ? x : rem) + id / 8;
+  int u = v / share;
+  w.b = u % a.B; u /= a.B;
+  w.h = u / g.groups;
+  const int i = u % g.groups * share + v % share;
+  w.part = i / g.blocks;
+  w.block = i - w.part * g.blocks;
   w.unit = w.b * a.Hkv + w.h;
-  return w;
+  return w.part < g.parts;
 }
 
 typedef __bf16 Frag __attribute__((ext_vector_type(8)));
@@ -98,6 +104,27 @@ __device__ __forceinline__ Frag frag_cols(const char* lds, int row0, int col0) {
   };
   const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(row + 8));
   return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// N products in a row whose A fragments come from LDS: fragment i is asked for DEPTH products before its own.  (Left to itself the compiler reads
+// each one right in front of its product and waits out the latency of LDS every time.)
+template <int N, int DEPTH, typename Load, typename Use>
+__device__ __forceinline__ void in_a_row(Load load, Use use) {
+  decltype(load(0)) f[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH && i < N; ++i) f[i] = load(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    use(i, f[i % DEPTH]);
+    if (i + DEPTH < N) f[i % DEPTH] = load(i + DEPTH);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// what was loaded from memory is there behind this point: a wait for it inside a loop would wait for the loads of tiles, too
+template <int N>
+__device__ __forceinline__ void settle(Frag (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
 // registers 8 ks .. 8 ks + 7 of an accumulator, rounded: a B fragment
 __device__ __forceinline__ Frag pack_frag(const f32x16& a, int ks) {
@@ -204,11 +231,13 @@ __device__ __forceinline__ void store_owned32(const f32x16 (&acc)[DH / 32], floa
 }
 
 // Softmax of a tile of scores s (SUBS x 32 keys from k0 on) with the running maximum m and sum l of a lane's row, in base 2: s becomes
-// exp2(s c2 - m); the factor for what was summed before is returned.
+// exp2(s c2 - m); the factor for what was summed before is returned.  The empty asm keeps the mask of the last tile behind its branch:
+// without it the compiler made selects of it that every tile paid for, a third of a tile's vector instructions.
 template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, int k0, int n, float& m, float& lsum) {
   const int grp = (threadIdx.x & 63) >> 5;
   if (k0 + SUBS * 32 > n) {            // (wave-uniform) only the last tile ends inside
+    asm volatile("");
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
@@ -242,10 +271,11 @@ template <int DH, int NW, int NS>
 __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH>;               // keys, values
-  const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks, a.parts, blockIdx.x, gridDim.x);
+  const int parts = a.fwd.parts;
+  Where w;
+  if (!where(a, a.fwd, blockIdx.x, gridDim.x, w)) return;
   const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
-  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int r = w.block * OWN * NW + wave * OWN + (l & 31);
   const bool active = w.block * OWN * NW + wave * OWN < a.R;
@@ -255,6 +285,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
 
   Frag qf[DH / 16];
   load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
+  settle(qf);
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
@@ -266,25 +297,13 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
     loads.keys(K, a.ldk, t * TILE, n, to);
     loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
-  for (int t = t0; t < t1; ++t) {
-    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
-    else wait_loads<0>();
-    __syncthreads();                                     // tile t is there, and everyone has left tile t - 1
-    if (t + NS - 1 < t1) issue(t + NS - 1);
-    if (!active) continue;
-    const char* Ks = smem + (t - t0) % NS * SLOT;
+  auto tile = [&](int k0, const char* Ks) {
     const char* Vs = Ks + kTileBytes<DH>;
     f32x16 s[2];
     clear(s);
-#pragma unroll
-    for (int kk = 0; kk < DH / 16; ++kk)
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub)
-        s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, sub * 32, kk), qf[kk], s[sub], 0, 0, 0);
-    const float alpha = softmax_tile(s, a.c2, t * TILE, n, m, lsum);
+    in_a_row<DH / 8, DH == 128 ? 6 : 3>([&](int i) { return frag_rows<DH>(Ks, i % 2 * 32, i / 2); },
+                        [&](int i, const Frag& f) { s[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / 2], s[i % 2], 0, 0, 0); });
+    const float alpha = softmax_tile(s, a.c2, k0, n, m, lsum);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {    // maxima that have settled leave the sums as they are
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
@@ -298,10 +317,21 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
         for (int dt = 0; dt < DH / 32; ++dt)
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Vs, sub * 32 + ks * 16, dt * 32), p, o[dt], 0, 0, 0);
       }
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  for (int t = t0; t < t1; ++t) {
+    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
+    __syncthreads();                                     // tile t is there, and everyone has left tile t - 1
+    if (t + NS - 1 < t1) issue(t + NS - 1);
+    if (!active) continue;
+    tile(t * TILE, smem + (t - t0) % NS * SLOT);
   }
   if (!active || r >= a.R) return;
   const float tot = lsum + __shfl_xor(lsum, 32, 64);
-  if (a.parts == 1) {
+  if (parts == 1) {
     store_owned<DH>(o, tot == 0.f ? 0.f : 1.0f / tot, a.out + row_at<DH>(a, w.b, w.h, r, a.ldo));
     if (grp == 0) a.lse2[(int64_t)w.unit * a.R + r] = m + __builtin_amdgcn_logf(tot);     // v_log_f32 is log2
   } else {
@@ -313,29 +343,25 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
 
 // Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the four waves walks over tiles of 32
 // keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.
-#ifndef TOK_NW
-#define TOK_NW(DH) (DH == 128 ? 2 : 4)
-#define TOK_NS(DH) 2
-#endif
-#ifndef BWD_NW
-#define BWD_NW 4
-#endif
-constexpr int TOKEN_KEYS = 32;
-template <int DH> constexpr int kTokenWaves = TOK_NW(DH);
-template <int DH> constexpr int kTokenSlots = TOK_NS(DH);
-template <int DH> constexpr int kTokenRing = kTokenSlots<DH> * 2 * TOKEN_KEYS * DH * 2;   // of a wave
+constexpr int TOKEN_KEYS = 32, kTokenGrid = 256;
+template <int DH> constexpr int kTokenWaves = DH == 128 ? 2 : 4;
+constexpr int kTokenSlots = 2;
+template <int DH> constexpr int kTokenRing = kTokenSlots * 2 * TOKEN_KEYS * DH * 2;   // of a wave
 template <int DH>
 __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(CrossArgs a) {
-  constexpr int TOKEN_NW = kTokenWaves<DH>, NS = kTokenSlots<DH>, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
-  const Where w = where(a, 1, a.parts, blockIdx.x, gridDim.x);
+  constexpr int TOKEN_NW = kTokenWaves<DH>, NS = kTokenSlots, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
+  const int parts = a.fwd.parts;
+  Where w;
+  if (!where(a, a.fwd, blockIdx.x, gridDim.x, w)) return;
   const int n = keys_of(a, w.b), nt = (n + TOKEN_KEYS - 1) / TOKEN_KEYS;
-  const int t0 = (int)((int64_t)nt * w.part / a.parts), t1 = (int)((int64_t)nt * (w.part + 1) / a.parts);
+  const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5, r = l & 31;
   char* ring = dtl_smem + wave * kTokenRing<DH>;
   const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
   const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
   Frag qf[DH / 16];
   load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, r < a.R ? r : a.R - 1, a.ldq));
+  settle(qf);
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
@@ -360,9 +386,10 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
     const char* Vs = Ks + HALF;
     f32x16 s[1];
     clear(s);
-#pragma unroll
-    for (int kk = 0; kk < DH / 16; ++kk) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, 0, kk), qf[kk], s[0], 0, 0, 0);
-    const float alpha = softmax_tile(s, a.c2, (t0 + wave + i * TOKEN_NW) * TOKEN_KEYS, n, m, lsum);
+    in_a_row<DH / 16, 4>([&](int i) { return frag_rows<DH>(Ks, 0, i); },
+                         [&](int i, const Frag& f) { s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i], s[0], 0, 0, 0); });
+    const int k0 = (t0 + wave + i * TOKEN_NW) * TOKEN_KEYS;
+    const float alpha = softmax_tile(s, a.c2, k0, n, m, lsum);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
@@ -397,7 +424,9 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
   }
   if (r >= a.R) return;
   const int64_t at = ((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r;
-  constexpr int PER = DH / 2 / TOKEN_NW;                 // registers: 8 or 16
+  const float inv = tot == 0.f ? 0.f : 1.0f / tot;
+  uint16_t* out = a.out + row_at<DH>(a, w.b, w.h, r, a.ldo);
+  constexpr int PER = DH / 2 / TOKEN_NW;                 // registers of a wave's share
 #pragma unroll
   for (int x = 0; x < PER; x += 4) {
     const int reg = wave * PER + x;
@@ -408,9 +437,13 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
 #pragma unroll
       for (int i = 0; i < TOKEN_NW; ++i) v[e] += image[(i * (DH / 2) + reg + e) * 64 + l] * f[i];
     }
-    *reinterpret_cast<f32x4*>(a.part + at * DH + (reg >> 4) * 32 + acc_row(reg & 15, grp)) = v;
+    const int col = (reg >> 4) * 32 + acc_row(reg & 15, grp);
+    if (parts > 1) *reinterpret_cast<f32x4*>(a.part + at * DH + col) = v;
+    else *reinterpret_cast<u32x2*>(out + col) = u32x2{rv_pack_bf16x2(v.x * inv, v.y * inv), rv_pack_bf16x2(v.z * inv, v.w * inv)};
   }
-  if (wave == 0 && grp == 0) a.part_ml[at] = float2{top, tot};
+  if (wave != 0 || grp != 0) return;
+  if (parts > 1) a.part_ml[at] = float2{top, tot};
+  else a.lse2[(int64_t)w.unit * a.R + r] = top + __builtin_amdgcn_logf(tot);
 }
 
 // parts -> out, lse2.  Eight columns to a lane; LANES lanes share the parts of one (a chain of up to 64 round trips else: single tokens of 8
@@ -437,7 +470,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
   };
   if (row < rows) {
 #pragma unroll 4
-    for (int s = lane; s < a.parts; s += LANES) {
+    for (int s = lane; s < a.fwd.parts; s += LANES) {
       const int64_t at = s * rows + row;
       const f32x4* p = reinterpret_cast<const f32x4*>(a.part + at * DH + c);
       add(a.part_ml[at], p[0], p[1]);
@@ -489,9 +522,9 @@ template <int DH, int NW, int NS>
 __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH>;
-  const int blocks = (a.R + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks, a.q_parts, id, grid);
-  const int parts = a.q_parts;
+  const int parts = a.bq.parts;
+  Where w;
+  if (!where(a, a.bq, id, grid, w)) return;
   const int n = keys_of(a, w.b), nt = (n + TILE - 1) / TILE;
   const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
@@ -503,7 +536,9 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
   Frag qf[DH / 16], of[DH / 16];
   load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
   load_owned<DH>(of, a.dout + row_at<DH>(a, w.b, w.h, rc, a.lddo));
-  const float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
+  float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
+  settle(qf); settle(of);
+  asm volatile("" : "+v"(lse), "+v"(D));
   f32x16 dq[DH / 32];
   clear(dq);
   const TileLoads<DH, NW> loads(wave);
@@ -513,31 +548,23 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
     loads.keys(K, a.ldk, t * TILE, n, to);
     loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
-  for (int t = t0; t < t1; ++t) {
-    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
-    else wait_loads<0>();
-    __syncthreads();
-    if (t + NS - 1 < t1) issue(t + NS - 1);
-    if (!active) continue;
-    const char* Ks = smem + (t - t0) % NS * SLOT;
+  auto tile = [&](int first, const char* Ks) {
     const char* Vs = Ks + kTileBytes<DH>;
-#pragma unroll
+#pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int x = 0; x < 16; ++x) { s[0][x] = lse; dp[0][x] = D; }
-#pragma unroll
-      for (int kk = 0; kk < DH / 16; ++kk) {
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Ks, sub * 32, kk), qf[kk], s[0], 0, 0, 0);
-        dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Vs, sub * 32, kk), of[kk], dp[0], 0, 0, 0);
-      }
-      const int k0 = t * TILE + sub * 32;
+      in_a_row<DH / 8, DH == 128 ? 4 : 2>([&](int i) { return frag_rows<DH>(i % 2 ? Vs : Ks, sub * 32, i / 2); },
+                          [&](int i, const Frag& f) {
+                            if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, of[i / 2], dp[0], 0, 0, 0);
+                            else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / 2], s[0], 0, 0, 0);
+                          });
+      const int k0 = first + sub * 32;
 #pragma unroll
       for (int x = 0; x < 16; ++x) dp[0][x] *= __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       if (k0 + 32 > n) {
+        asm volatile("");
 #pragma unroll
         for (int x = 0; x < 16; ++x)
           if (k0 + acc_row(x, grp) >= n) dp[0][x] = 0.f;
@@ -550,6 +577,17 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
           dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Ks, sub * 32 + ks * 16, dt * 32), ds, dq[dt], 0, 0, 0);
       }
     }
+  };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  for (int t = t0; t < t1; ++t) {
+    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
+    __syncthreads();
+    if (t + NS - 1 < t1) issue(t + NS - 1);
+    if (!active) continue;
+    tile(t * TILE, smem + (t - t0) % NS * SLOT);
   }
   if (!active || r >= a.R) return;
   if (parts == 1) store_owned<DH>(dq, a.scale, a.dq + row_at<DH>(a, w.b, w.h, r, a.lddq));
@@ -561,15 +599,19 @@ template <int DH, int NW, int NS>
 __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH> + 2 * TILE * 4;   // queries, do, lse, D
-  const int blocks = (a.Sk + OWN * NW - 1) / (OWN * NW);
-  const Where w = where(a, blocks, a.kv_parts, id, grid);
-  const int parts = a.kv_parts;
+  const int parts = a.bkv.parts;
+  Where w;
+  if (!where(a, a.bkv, id, grid, w)) return;
   const int n = keys_of(a, w.b), j0 = w.block * OWN * NW;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int j = j0 + wave * OWN + (l & 31);
   const int nt = j0 < n ? (a.R + TILE - 1) / TILE : 0;      // keys behind the sequence: zeros
   const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const bool active = j0 + wave * OWN < n;
+  // Heads of 128: keys, values, their two gradients and the scores are 256 registers by themselves; the values stay in LDS, which has
+  // bandwidth left (29 % of cycles)
+  constexpr bool kValuesInLds = DH == 128;
+  Frag* vl = reinterpret_cast<Frag*>(smem + NS * SLOT + wave * OWN * DH * 2) + l;
   Frag kf[DH / 16], vf[DH / 16];
   f32x16 dk[DH / 32], dv[DH / 32];
   clear(dk); clear(dv);
@@ -577,6 +619,11 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
     const int jc = j < n ? j : n - 1;
     load_owned<DH>(kf, a.k + ((int64_t)w.b * a.Sk + jc) * a.ldk + w.h * DH);
     load_owned<DH>(vf, a.v + ((int64_t)w.b * a.Sk + jc) * a.ldv + w.h * DH);
+    settle(kf); settle(vf);
+    if (kValuesInLds) {
+#pragma unroll
+      for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
+    }
   }
   const TileLoads<DH, NW> loads(wave);
   constexpr int LPT = 2 * TileLoads<DH, NW>::N + 1;
@@ -598,7 +645,7 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
     const char* Qs = smem + (t - t0) % NS * SLOT;
     const char* Os = Qs + kTileBytes<DH>;
     const float* lse = reinterpret_cast<const float*>(Os + kTileBytes<DH>);
-#pragma unroll
+#pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
       f32x16 s[1], dp[1];
 #pragma unroll
@@ -608,11 +655,17 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
 #pragma unroll
         for (int x = 0; x < 4; ++x) { s[0][4 * q + x] = ls[x]; dp[0][4 * q + x] = D[x]; }
       }
-#pragma unroll
-      for (int kk = 0; kk < DH / 16; ++kk) {
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Qs, sub * 32, kk), kf[kk], s[0], 0, 0, 0);
-        dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DH>(Os, sub * 32, kk), vf[kk], dp[0], 0, 0, 0);
-      }
+      struct Two { Frag rows, values; };
+      in_a_row<DH / 8, DH == 128 ? 4 : 2>([&](int i) {
+                            Two t;
+                            t.rows = frag_rows<DH>(i % 2 ? Os : Qs, sub * 32, i / 2);
+                            if (kValuesInLds && i % 2) t.values = vl[i / 2 * 64];
+                            return t;
+                          },
+                          [&](int i, const Two& t) {
+                            if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kValuesInLds ? t.values : vf[i / 2], dp[0], 0, 0, 0);
+                            else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kf[i / 2], s[0], 0, 0, 0);
+                          });
 #pragma unroll
       for (int x = 0; x < 16; ++x) {
         s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
@@ -640,11 +693,11 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
     store_owned32<DH>(dv, to + DH);
   }
 }
-template <int DH> constexpr int kBwdSlot = 2 * kTileBytes<DH> + 2 * TILE * 4;
+template <int DH, int NW, int NS> constexpr int kBwdLds = NS * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
 // Both in one launch, the longer workgroups (dK and dV: four products to dQ's three) first: where neither fills the chip by itself, and for
 // the last workgroups of the one to run beside the first of the other.
 template <int DH, int NW, int NS>
-__global__ __launch_bounds__(64 * NW, 2) void cross_bwd_kernel(CrossArgs a) {
+__global__ __launch_bounds__(64 * NW, DH == 128 ? 2 : 3) void cross_bwd_kernel(CrossArgs a) {
   if ((int)blockIdx.x < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, blockIdx.x, a.kv_grid);
   else bwd_q_body<DH, NW, NS>(a, blockIdx.x - a.kv_grid, gridDim.x - a.kv_grid);
 }
@@ -652,7 +705,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_bwd_kernel(CrossArgs a) {
 template <int DH, bool KV>
 __global__ __launch_bounds__(256) void cross_bwd_join_kernel(CrossArgs a) {
   constexpr int W = KV ? 2 * DH : DH;
-  const int per = KV ? a.Sk : a.R, parts = KV ? a.kv_parts : a.q_parts;
+  const int per = KV ? a.Sk : a.R, parts = KV ? a.bkv.parts : a.bq.parts;
   const float* sums = KV ? a.kv_part : a.q_part;
   const int64_t rows = (int64_t)a.B * a.Hkv * per;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
@@ -696,11 +749,11 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   if (R > (1ll << 30) || U * up(R, OWN) > (1ll << 30) || U * up(Sk, OWN) > (1ll << 30) || U * R * dh / 8 > (1ll << 38) || U * Sk * dh / 8 > (1ll << 38)) return false;
   p.R = (int)R; p.Rp = (int)(up(R, TILE) * TILE);
   p.token = R <= OWN;
-  p.fwd_parts = p.token ? parts_for(U, up(Sk, TOKEN_KEYS), 512, 8) : parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
+  p.fwd_parts = p.token ? parts_for(U, up(Sk, TOKEN_KEYS), kTokenGrid, 8) : parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
   p.q_parts = parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
   p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(R, TILE), 512, 4);
   auto round = [](size_t b) { return (b + 255) / 256 * 256; };
-  const bool parts = p.token || p.fwd_parts > 1;
+  const bool parts = p.fwd_parts > 1;
   p.fwd_ml = parts ? round((size_t)4 * p.fwd_parts * U * R * dh) : 0;
   p.fwd_bytes = parts ? p.fwd_ml + round((size_t)8 * p.fwd_parts * U * R) : 0;
   p.d = round((size_t)4 * U * p.Rp);
@@ -726,40 +779,50 @@ CrossArgs common_args(const CrossPlan& p, const void* q, int64_t ldq, const void
   CrossArgs a{};
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
   a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.klen = klen;
-  a.B = B; a.Sq = Sq; a.Sk = Sk; a.share = H / Hkv; a.Hkv = Hkv; a.R = p.R; a.Rp = p.Rp; a.parts = 1;
+  a.B = B; a.Sq = Sq; a.Sk = Sk; a.share = H / Hkv; a.Hkv = Hkv; a.R = p.R; a.Rp = p.Rp;
   a.scale = 1.0f / sqrtf((float)dh);
   a.c2 = 1.4426950408889634f * a.scale;
   return a;
 }
 
+// the launch of `blocks` x parts per (sequence, key/value head)
+int64_t deal(Grid& g, const CrossArgs& a, int64_t blocks, int parts) {
+  g.blocks = (int)blocks; g.parts = parts; g.groups = 1;
+  if (a.klen && a.B > 1) {
+    while (g.groups < 8 && a.Hkv * g.groups % 8) g.groups *= 2;
+    if (g.groups > blocks * parts) g.groups = (int)(blocks * parts);
+  }
+  return (int64_t)a.B * a.Hkv * g.groups * share_of(g);
+}
+
 template <int DH>
 rv_status forward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
-  a.parts = p.fwd_parts;
   a.part = (float*)work; a.part_ml = (float2*)(work + p.fwd_ml);
   if (p.token) {
     constexpr int waves = kTokenWaves<DH>, ring = waves * kTokenRing<DH>, image = waves * (DH / 2 * 64 * 4 + 32 * 8);
-    RV_TRY((launch<cross_token_kernel<DH>>(a, U * a.parts, 64 * waves, ring > image ? ring : image, st)));
+    const int64_t grid = deal(a.fwd, a, 1, p.fwd_parts);
+    RV_TRY((launch<cross_token_kernel<DH>>(a, grid, 64 * waves, ring > image ? ring : image, st)));
   } else {
-    RV_TRY((launch<cross_fwd_kernel<DH, 4, 2>>(a, U * a.parts * up(a.R, OWN * 4), 256, 2 * 2 * kTileBytes<DH>, st)));
+    const int64_t grid = deal(a.fwd, a, up(a.R, OWN * 4), p.fwd_parts);
+    RV_TRY((launch<cross_fwd_kernel<DH, 4, 2>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
   }
-  if (!p.token && a.parts == 1) return RV_OK;
-  if (a.parts > 4) RV_TRY((launch<cross_join_kernel<DH, 8>>(a, up(U * a.R * (DH / 8), 32), 256, 0, st)));
+  if (p.fwd_parts == 1) return RV_OK;
+  if (p.fwd_parts > 4) RV_TRY((launch<cross_join_kernel<DH, 8>>(a, up(U * a.R * (DH / 8), 32), 256, 0, st)));
   else RV_TRY((launch<cross_join_kernel<DH, 1>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
   return RV_OK;
 }
-template <int DH>
+template <int DH, int NW>
 rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
-  a.q_parts = p.q_parts; a.kv_parts = p.kv_parts;
   RV_TRY((launch<cross_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
-  const int64_t kv = U * a.kv_parts * up(a.Sk, OWN * BWD_NW), q = U * a.q_parts * up(a.R, OWN * BWD_NW);
+  const int64_t kv = deal(a.bkv, a, up(a.Sk, OWN * NW), p.kv_parts), q = deal(a.bq, a, up(a.R, OWN * NW), p.q_parts);
   if (kv > 0x3FFFFFFF || q > 0x3FFFFFFF) return RV_E_INVAL;
   a.kv_grid = (int)kv;
-  RV_TRY((launch<cross_bwd_kernel<DH, BWD_NW, 2>>(a, kv + q, 64 * BWD_NW, 2 * kBwdSlot<DH>, st)));
-  if (a.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
-  if (a.kv_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
+  RV_TRY((launch<cross_bwd_kernel<DH, NW, 2>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, 2>, st)));
+  if (p.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
+  if (p.kv_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
   return RV_OK;
 }
 
@@ -801,5 +864,9 @@ extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const 
   CrossArgs a = common_args(p, q, ldq, k, ldk, v, ldv, klen, B, Sq, Sk, n_heads, n_kv_heads, d_head);
   a.o = (const uint16_t*)out; a.ldo = ldo; a.dout = (const uint16_t*)dout; a.lddo = lddo; a.lse2 = (float*)lse2;
   a.dq = (uint16_t*)dq; a.lddq = lddq; a.dk = (uint16_t*)dk; a.lddk = lddk; a.dv = (uint16_t*)dv; a.lddv = lddv;
-  return d_head == 64 ? backward<64>(a, p, (char*)work, (hipStream_t)stream) : backward<128>(a, p, (char*)work, (hipStream_t)stream);
+  const hipStream_t st = (hipStream_t)stream;
+  // Heads of 128: two waves to a SIMD either way (registers); eight share a streamed tile, 736 -> 775 TFLOP/s over 4096 x 4096 tokens, but for
+  // rows or keys that four waves hold the others would idle.  Heads of 64 are faster with four: three waves to a SIMD, 770 / 701.
+  if (d_head == 64) return backward<64, 4>(a, p, (char*)work, st);
+  return p.R > 4 * OWN && Sk > 4 * OWN ? backward<128, 8>(a, p, (char*)work, st) : backward<128, 4>(a, p, (char*)work, st);
 }

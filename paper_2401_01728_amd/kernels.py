@@ -1,5 +1,6 @@
 """Thin binding of include/rv_kernels.h (per-kernel entry points; marshalling only)."""
 import ctypes
+from functools import lru_cache
 
 import torch
 
@@ -146,10 +147,11 @@ def _cross_sizes(q, k, n_heads, n_kv_heads):
     return B, Sq, k.shape[1], n_heads, n_kv_heads, cols // n_heads
 
 
-def _cross_work(sizes, backward, device):
+@lru_cache(maxsize=256)
+def _cross_work(sizes, backward):
     n = ctypes.c_size_t(0)
     _check(_lib.lib().rv_k_cross_attention_work(*sizes, backward, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None, n.value
+    return n.value
 
 
 def cross_attention_fwd(q, k, v, n_heads, n_kv_heads, klen=None, out=None, stream=None):
@@ -160,7 +162,8 @@ def cross_attention_fwd(q, k, v, n_heads, n_kv_heads, klen=None, out=None, strea
     with context:
         out = torch.empty(B, Sq, H * dh, dtype=torch.bfloat16, device=q.device) if out is None else out
         lse2 = torch.empty(B, H, Sq, dtype=torch.float32, device=q.device)
-        work, n = _cross_work(sizes, 0, q.device)
+        n = _cross_work(sizes, 0)
+        work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
         _check(_lib.lib().rv_k_cross_attention_fwd(
             _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
             _ptr(_flat(klen, torch.int32, (B,)) if klen is not None else None), _ptr(out), _tokens(out, B, Sq, H * dh), _ptr(lse2), *sizes,
@@ -174,7 +177,8 @@ def cross_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, klen=None
     stream, context = _on(stream, q, k, v, klen, out, dout, lse2, dq, dk, dv)
     with context:
         dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v)))
-        work, n = _cross_work(sizes, 1, q.device)
+        n = _cross_work(sizes, 1)
+        work = torch.empty(n, dtype=torch.uint8, device=q.device)
         _check(_lib.lib().rv_k_cross_attention_bwd(
             _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
             _ptr(_flat(klen, torch.int32, (B,)) if klen is not None else None), _ptr(out), _tokens(out, B, Sq, H * dh),

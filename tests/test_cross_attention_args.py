@@ -47,8 +47,8 @@ def test_refused_by_the_backward(change):
 
 
 def test_too_little_work_memory():
-    token = dict(GOOD, Sq=1)
-    need = _work(Sq=1)[1]
+    token = dict(GOOD, Sq=1, Sk=5000)       # long enough to be cut into parts
+    need = _work(Sq=1, Sk=5000)[1]
     assert need > 0
     assert _lib.lib().rv_k_cross_attention_fwd(*(dict(token, bytes=need - 1)[n] for n in NAMES)) == INVAL
     assert _lib.lib().rv_k_cross_attention_fwd(*(dict(token, work=None)[n] for n in NAMES)) == INVAL
