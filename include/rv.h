@@ -280,7 +280,7 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).
  *             Nothing in it has to be kept between calls; calls that may run at one time need one each, and so do graphs
  *             that may be replayed at one time.
- * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8.  Outputs must not share memory
+ * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8, ldx at most 2^22.  Outputs must not share memory
  * with inputs or one another but as said.  Allocates nothing; RV_E_INVAL, before anything is enqueued, on what is not covered.
  */
 typedef struct {

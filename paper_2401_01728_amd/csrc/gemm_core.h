@@ -787,9 +787,12 @@ __device__ __forceinline__ u32x4 f32_to_bf16x8(const f32x4 (&v)[2]) {
   return o;
 }
 
-template <int BM, int BN, int G, int NW, int NS, bool AKM, bool BKM, int EPI>
+// (TAIL as in gemm_dtl_body)
+template <int BM, int BN, int G, int NW, int NS, bool AKM, bool BKM, int EPI, bool TAIL = false>
 __device__ __forceinline__ void gemm_split_body(const uint16_t* __restrict__ A, int64_t lda, int64_t a_bs,
-                                                const uint16_t* __restrict__ B, int64_t ldb, int64_t b_bs, int M, int N, int K, int bm, int bn, const Epi& e) {
+                                                const uint16_t* __restrict__ B, int64_t ldb, int64_t b_bs, int M, int N, int K, int bm, int bn, const Epi& e,
+                                                const uint16_t* __restrict__ b_tail = nullptr, int t_tail = 0) {
+  static_assert(!TAIL || BKM, "the tail is rows of a k-major operand");
   constexpr int BK = 32, NT = 64 * NW * G;               // a group's NW waves: NW / 2 (m) x 2 (n)
   constexpr int WM = BM / (NW / 2), WN = BN / 2, TM = WM / 32, TN = WN / 32;
   constexpr int A_BYTES = dtl_tile_bytes(BM, BK), BUF = A_BYTES + dtl_tile_bytes(BN, BK);
@@ -816,7 +819,8 @@ __device__ __forceinline__ void gemm_split_body(const uint16_t* __restrict__ A, 
     const int t = i * G + group;
     const int lb = __builtin_amdgcn_readfirstlane((int)(size_t)(ring + (i % NS) * BUF) + wave * 1024);
     const uint16_t* pa = AKM ? A + (int64_t)t * BK * lda : A + (int64_t)t * a_bs;
-    const uint16_t* pb = BKM ? B + (int64_t)t * BK * ldb : B + (int64_t)t * b_bs;
+    const uint16_t* pb = TAIL && t >= t_tail ? b_tail + (int64_t)(t - t_tail) * BK * ldb
+                                             : BKM ? B + (int64_t)t * BK * ldb : B + (int64_t)t * b_bs;
 #pragma unroll
     for (int q = 0; q < NA; ++q) dtl_load_s(pa, (unsigned)da.off[q] * 2u, lb + q * NW * 1024);
 #pragma unroll

@@ -37,7 +37,7 @@ struct RowInfo { float lse2, g, at_label; int label; };
 struct CutForm { int tile, S; };
 struct Plan {
   int T, d, V, Vp, P, pieces;            // V rounded up to whole strips; rows of a piece and their number
-  bool grads;
+  bool grads, few;                       // few: rows are not gathered
   int64_t ldw;
   CutForm dx;                            // tile and stretches of dx; stretches of dW
   int S_w;
@@ -47,17 +47,40 @@ struct Plan {
 __host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
 __host__ __device__ inline int round_up(int a, int b) { return div_up(a, b) * b; }
 
-// rows of piece p (device count n)
-__device__ __forceinline__ int piece_rows(int n, int p, int P) {
-  const int left = n - p * P;
-  return left < P ? left : P;
+// The rows that the kernels work on.  Gathered (count != null): *count rows without gaps, lab and idx their labels and places; pieces of P of
+// them.  Up to kFewRows rows stay where they are: one piece, and those that take no part become zeros where dz is made.
+struct Rows {
+  const int* count; const int* lab; const int* idx; const int* pos;
+  const int64_t* label;
+  int T, V, p, P;
+};
+constexpr int kFewRows = 256;
+__device__ __forceinline__ int rows_of(const Rows& r) {
+  const int left = (r.count ? *r.count : r.T) - r.p * r.P;
+  return left < r.P ? left : r.P;
+}
+// the label of a row of the piece, -1: takes no part
+__device__ __forceinline__ int label_of(const Rows& r, int row) {
+  if (r.count) return r.lab[r.p * r.P + row];
+  const int64_t y = r.label[row];
+  return y >= 0 && y < r.V ? (int)y : -1;
+}
+
+// row r of the tail of W: the rows from V / 32 * 32 on, zeros behind the last (see input_grad_body)
+__device__ __forceinline__ void copy_tail(const uint16_t* __restrict__ w, int64_t ldw, int d, int V, uint16_t* __restrict__ tail, int r) {
+  const int v = V / 32 * 32 + r;
+  for (int c = threadIdx.x; c < d / 8; c += 256) {
+    u32x4 u = {0u, 0u, 0u, 0u};
+    if (v < V) u = *reinterpret_cast<const u32x4*>(w + (int64_t)v * ldw + c * 8);
+    *reinterpret_cast<u32x4*>(tail + (int64_t)r * ldw + c * 8) = u;
+  }
 }
 
 // ---- rows that take part ----------------------------------------------------------------------
 // A block takes `per` (up to 64) consecutive rows; where they go follows from the number of labels before them that take part, which
 // it counts itself: T labels are 8 T bytes out of L2, at most a thousand blocks do it, and a scan of its own would be a launch more.
 // pos[t] = place among the rows kept or -1; idx, lab: the other way round.  The block of the last rows leaves their number.
-// Behind the row blocks, with `tail`: 64 rows that stand for rows V / 32 * 32 .. of W, zeros behind its last (see input_grad_kernel).
+// Behind the row blocks: the tail of W.
 __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict__ x, int64_t ldx, const int64_t* __restrict__ label, int T,
                                                      int d, int V, int P, int per, int* __restrict__ count, int* __restrict__ pos,
                                                      int* __restrict__ idx, int* __restrict__ lab, uint16_t* __restrict__ xw,
@@ -65,12 +88,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict_
                                                      int64_t ldw, uint16_t* __restrict__ tail, int row_blocks) {
   const int tid = threadIdx.x, l = tid & 63;
   if ((int)blockIdx.x >= row_blocks) {
-    const int r = blockIdx.x - row_blocks, v = V / 32 * 32 + r;
-    for (int c = tid; c < d / 8; c += 256) {
-      u32x4 u = {0u, 0u, 0u, 0u};
-      if (v < V) u = *reinterpret_cast<const u32x4*>(w + (int64_t)v * ldw + c * 8);
-      *reinterpret_cast<u32x4*>(tail + (int64_t)r * ldw + c * 8) = u;
-    }
+    copy_tail(w, ldw, d, V, tail, blockIdx.x - row_blocks);
     return;
   }
   __shared__ int part[4], place[64];
@@ -121,7 +139,6 @@ struct LogitsOut {
   uint16_t* e;         // [Vp / 32][P][32]
   float2* stat;        // [Vp / 64][P]
   float* target;       // [P] the label's logit
-  const int* lab;      // [P]
   int P, V, Vp;
 };
 
@@ -145,7 +162,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {   // round to
 }
 
 template <bool STORE, int TM, int TN>
-__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, int mw, int nw0, int M) {
+__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, const Rows& rows, int mw, int nw0, int M) {
   constexpr int TS = STRIP / 16;
   static_assert(TN % TS == 0, "a wave's columns are whole strips");
   const int l = threadIdx.x & 63, grp = l >> 4;
@@ -168,7 +185,7 @@ __device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const
             if (nw + c * 16 + 4 * grp + k >= o.V) a[c][k] = -INFINITY;
         }
       }
-      const int y = ok ? o.lab[row] - nw : -1;
+      const int y = ok ? label_of(rows, row) - nw : -1;
       if (__builtin_amdgcn_ballot_w64(y >= 0 && y < STRIP)) {   // few strips hold a label of their rows
         float at = 0.f;
         bool mine = false;
@@ -217,26 +234,25 @@ __device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const
 }
 
 template <int BM, int BN, int NS, int NW, bool STORE>
-__global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __restrict__ xw, const uint16_t* __restrict__ w, int64_t ldw, int d,
-                                                            const int* __restrict__ count, int p, LogitsOut o) {
-  const int M = piece_rows(*count, p, o.P);
+__global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __restrict__ x, int64_t ldx, int64_t x_bs, const uint16_t* __restrict__ w,
+                                                            int64_t ldw, int d, Rows rows, LogitsOut o) {
+  const int M = rows_of(rows);
   if (M <= 0) return;
   const int vm = div_up(M, BM), vn = div_up(o.Vp, BN);
   const int id = blockIdx.x;
   if (id >= vm * vn) return;
   const int bm = id % vm, bn = id / vm;
-  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, m0 + wm0, n0 + wn0, M); };
-  gemm_dtl_body<BM, BN, 32, NS, NW, false, false, EPI_OWN>(xw, 32, 32ll * o.P, w, ldw, 32, M, o.V, d, bm, bn, Epi{}, nullptr, 0, own);
+  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, rows, m0 + wm0, n0 + wn0, M); };
+  gemm_dtl_body<BM, BN, 32, NS, NW, false, false, EPI_OWN>(x, ldx, x_bs, w, ldw, 32, M, o.V, d, bm, bn, Epi{}, nullptr, 0, own);
 }
 
 // ---- strips joined to rows ----------------------------------------------------------------------
 // 16 rows to a block, 64 lanes to a row: a strip's pairs of 16 rows are one line.
-__global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ stat, const float* __restrict__ target, const int* __restrict__ lab,
-                                                    const int* __restrict__ idx, const int* __restrict__ count, int p, int P, int strips,
-                                                    float scale, const float* __restrict__ row_scale, float* __restrict__ loss,
-                                                    float* __restrict__ lse, RowInfo* __restrict__ info) {
+__global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ stat, const float* __restrict__ target, Rows rows, int strips, float scale,
+                                                    const float* __restrict__ row_scale, float* __restrict__ loss, float* __restrict__ lse,
+                                                    RowInfo* __restrict__ info) {
   __shared__ float2 part[64][17];
-  const int M = piece_rows(*count, p, P), r = threadIdx.x & 15, sl = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
+  const int P = rows.P, M = rows_of(rows), r = threadIdx.x & 15, sl = threadIdx.x >> 4, row = blockIdx.x * 16 + r;
   if ((int)blockIdx.x * 16 >= M) return;
   auto join = [](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.f : m;
@@ -255,40 +271,60 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
   }
   if (sl != 0 || row >= M) return;
   v = part[0][r];
-  const int t = idx[row];
+  const int t = rows.count ? rows.idx[rows.p * P + row] : row, y = label_of(rows, row);
+  if (y < 0) {                                    // (not gathered) whatever its logits were
+    loss[t] = 0.f;
+    if (lse) lse[t] = 0.f;
+    if (info) info[row] = RowInfo{0.f, 0.f, 0.f, -1};
+    return;
+  }
   const float lse2 = v.x + __builtin_amdgcn_logf(v.y), ln = lse2 * kLn2, at = target[row];   // v_log_f32 is log2
   loss[t] = ln - at;
   if (lse) lse[t] = ln;
   if (info) {
     const float g = row_scale ? scale * row_scale[t] : scale;
-    info[row] = RowInfo{lse2, g, g * expm1f(at - ln), lab[row]};
+    info[row] = RowInfo{lse2, g, g * expm1f(at - ln), y};
   }
 }
 
 // ---- e -> dz, in place ----------------------------------------------------------------------
-// 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows from the last one up to
-// whole tiles of 32 become zeros, of dz here and of the copy of x below: the weight gradient's product walks over them.
-__global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info,
-                                                 const int* __restrict__ count, int p, int P, int strips, int per, uint16_t* __restrict__ xw, int d) {
-  const int n = *count;
-  int M = piece_rows(n, p, P);
+// 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those from the
+// last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
+// Where rows are not gathered the copy is made here, by the blocks behind the strips', and the tail of W by those behind them.
+__global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info, Rows rows,
+                                                 int strips, int per, int strip_blocks, uint16_t* __restrict__ xw, int d, const uint16_t* __restrict__ x,
+                                                 int64_t ldx, const uint16_t* __restrict__ w, int64_t ldw, uint16_t* __restrict__ tail) {
+  const int P = rows.P;
+  int M = rows_of(rows);
   if (M <= 0) {
-    if (p) return;
+    if (rows.p) return;
     M = 0;                                        // no row at all: one tile of zeros
   }
   const int row = blockIdx.x * 64 + threadIdx.x / 4, q = threadIdx.x & 3;
   const int end = round_up(M > 0 ? M : 1, 32);
+  const u32x4 zero = {0u, 0u, 0u, 0u};
+  if ((int)blockIdx.y >= strip_blocks) {          // (rows not gathered) 8 blocks of 32 columns of x each, then a row of the tail each
+    const int c0 = (blockIdx.y - strip_blocks) * 8, copies = div_up(d / 32, 8);
+    if ((int)blockIdx.y - strip_blocks >= copies) {
+      if (blockIdx.x == 0) copy_tail(w, ldw, d, rows.V, tail, blockIdx.y - strip_blocks - copies);
+      return;
+    }
+    if (row >= end) return;
+    const bool in = row < M && label_of(rows, row) >= 0;
+    for (int cb = c0; cb < c0 + 8 && cb < d / 32; ++cb)
+      *reinterpret_cast<u32x4*>(xw + ((int64_t)cb * P + row) * 32 + q * 8) = in ? *reinterpret_cast<const u32x4*>(x + (int64_t)row * ldx + cb * 32 + q * 8) : zero;
+    return;
+  }
   if (row >= end) return;
   const int s0 = blockIdx.y * per, s1 = s0 + per < strips ? s0 + per : strips;
   uint16_t* base = e + (int64_t)row * 32 + q * 8;
   const int64_t bs = 32ll * P;
-  if (row >= M) {
-    const u32x4 zero = {0u, 0u, 0u, 0u};
+  if (row >= M || info[row].label < 0) {
     for (int s = s0; s < s1; ++s) {
       *reinterpret_cast<u32x4*>(base + 2 * s * bs) = zero;
       *reinterpret_cast<u32x4*>(base + (2 * s + 1) * bs) = zero;
     }
-    if (blockIdx.y == 0) {
+    if (rows.count && blockIdx.y == 0) {
       for (int cb = 0; cb < d / 32; ++cb) *reinterpret_cast<u32x4*>(xw + ((int64_t)cb * P + row) * 32 + q * 8) = zero;
     }
     return;
@@ -327,37 +363,52 @@ __device__ __forceinline__ int stretches(int S, int tiles_m, int vm, int nk) {
   n = n * 8 <= nk ? n : nk / 8;
   return n > S ? n : S;
 }
-template <int BM, int BN, int NS, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void input_grad_kernel(const uint16_t* __restrict__ dz, const uint16_t* __restrict__ w, int64_t ldw, int d,
-                                                                int V, int Vp, const int* __restrict__ count, int p, int P, int S_all, int tiles_m,
-                                                                const uint16_t* __restrict__ tail, float* __restrict__ part) {
-  const int M = piece_rows(*count, p, P);
+struct GradArgs {
+  const uint16_t* dz; const uint16_t* xw; const uint16_t* w;
+  int64_t ldw;
+  Rows rows;
+  int d, Vp;
+  int S_dx, tiles_m, dx_grid;             // dx: stretches for all rows, their tile rows, workgroups
+  const uint16_t* tail; float* part;
+  int S_w;                                // dW
+  float* sums; uint16_t* dw; const float* master; float* master_out; uint16_t* version; float eta;
+};
+// BM 256: tiles of 256x256, eight waves, in order of k; 128: of 128x128, the walk split over two groups of four waves.  The last k-tiles, which
+// end behind the last row of W, come from its copy with zeros behind (there is nothing behind W that could be read).
+template <int BM>
+__device__ __forceinline__ void input_grad_body(const GradArgs& a, int id) {
+  const int d = a.d, V = a.rows.V, P = a.rows.P, M = rows_of(a.rows);
   if (M <= 0) return;
-  const int vm = div_up(M, BM), vn = div_up(d, BN), tiles = vm * vn, nk = Vp / 32;
-  const int S = stretches(S_all, tiles_m, vm, nk);
-  const int id = blockIdx.x;
+  const int vm = div_up(M, BM), vn = div_up(d, BM), tiles = vm * vn, nk = a.Vp / 32;
+  const int S = stretches(a.S_dx, a.tiles_m, vm, nk);
   if (id >= tiles * S) return;
   const int s = id / tiles, in = id - s * tiles, bm = in % vm, bn = in / vm;
   const int k0 = (int)((int64_t)nk * s / S), k1 = (int)((int64_t)nk * (s + 1) / S);
   Epi out{};
-  out.out = part + (int64_t)s * vm * BM * d; out.ldo = d;
-  gemm_dtl_body<BM, BN, 32, NS, NW, false, true, EPI_F32, true>(dz + (int64_t)k0 * 32 * P, 32, 32ll * P, w + (int64_t)k0 * 32 * ldw, ldw, 32, M, d,
-                                                                (k1 - k0) * 32, bm, bn, out, tail, V / 32 - k0);
+  out.out = a.part + (int64_t)s * vm * BM * d; out.ldo = d;
+  const uint16_t* A = a.dz + (int64_t)k0 * 32 * P;
+  const uint16_t* B = a.w + (int64_t)k0 * 32 * a.ldw;
+  if constexpr (BM == 256)
+    gemm_dtl_body<256, 256, 32, 4, 8, false, true, EPI_F32, true>(A, 32, 32ll * P, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
+  else
+    gemm_split_body<128, 128, 2, 4, 4, false, true, EPI_F32, true>(A, 32, 32ll * P, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
 }
+template <int BM>
+__global__ __launch_bounds__(512, 2) void input_grad_kernel(GradArgs a) { input_grad_body<BM>(a, blockIdx.x); }
 // the stretches' sums, added in a fixed order and rounded, to the rows they belong to; zeros to the rows that take no part.  LANES lanes share
 // eight columns of a row: with dozens of stretches one lane's walk over them is a chain of round trips (256 rows of 448
 // columns, 64 stretches: 25 us with one lane).
 template <int LANES>
-__global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __restrict__ part, const int* __restrict__ pos, const int* __restrict__ count,
-                                                              int p, int P, int T, int d, int nk, int bm, int S_all, int tiles_m, uint16_t* __restrict__ dx,
-                                                              int64_t lddx) {
-  const int M = piece_rows(*count, p, P);
+__global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __restrict__ part, Rows rows, int d, int nk, int bm, int S_all, int tiles_m,
+                                                              uint16_t* __restrict__ dx, int64_t lddx) {
+  const int M = rows_of(rows), p = rows.p, P = rows.P;
   if (M <= 0 && p) return;
   const int lane = LANES > 1 ? threadIdx.x / (256 / LANES) : 0;
   const int64_t chunk = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x % (256 / LANES);
   const int per = d / 8;
-  const bool in = chunk < (int64_t)T * per;
-  const int t = in ? (int)(chunk / per) : 0, c = in ? (int)(chunk - (int64_t)t * per) * 8 : 0, j = in ? pos[t] : -1;
+  const bool in = chunk < (int64_t)rows.T * per;
+  const int t = in ? (int)(chunk / per) : 0, c = in ? (int)(chunk - (int64_t)t * per) * 8 : 0;
+  const int j = !in ? -1 : rows.count ? rows.pos[t] : label_of(rows, t) >= 0 ? t : -1;
   const bool here = j >= 0 && j / P == p;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   if (here) {
@@ -390,17 +441,15 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
 constexpr int WB = 256, W_NS = 4, W_NW = 8;
 __device__ __forceinline__ int row_stretches(int S, int nk) { return S < nk ? S : nk; }
 template <int KIND>
-__global__ __launch_bounds__(64 * W_NW, 2) void weight_grad_kernel(const uint16_t* __restrict__ dz, const uint16_t* __restrict__ xw, int d, int V, int Vp,
-                                                                   const int* __restrict__ count, int p, int P, int S, float* __restrict__ sums,
-                                                                   uint16_t* __restrict__ dw, const float* __restrict__ master,
-                                                                   float* __restrict__ master_out, uint16_t* __restrict__ version, float eta) {
-  int M = piece_rows(*count, p, P);
+__device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
+  const int d = a.d, V = a.rows.V, Vp = a.Vp, P = a.rows.P;
+  int M = rows_of(a.rows);
   if (M <= 0) {
-    if (p) return;
+    if (a.rows.p) return;
     M = 1;                                        // (a tile of zeros: dz_kernel)
   }
-  const int nk = div_up(M, 32), vm = div_up(V, WB), vn = div_up(d, WB), tiles = vm * vn, parts = KIND == 2 ? row_stretches(S, nk) : 1;
-  const int id = blockIdx.x, s = id / tiles;
+  const int nk = div_up(M, 32), vm = div_up(V, WB), vn = div_up(d, WB), tiles = vm * vn, parts = KIND == 2 ? row_stretches(a.S_w, nk) : 1;
+  const int s = id / tiles;
   if (s >= parts) return;
   const int in = id - s * tiles, bn = in % vn, bm = in / vn;
   const int k0 = nk * s / parts, k1 = nk * (s + 1) / parts;
@@ -409,32 +458,41 @@ __global__ __launch_bounds__(64 * W_NW, 2) void weight_grad_kernel(const uint16_
     Epi o{};
     o.ldo = d;
     if constexpr (KIND == 0) {
-      o.out = dw;
+      o.out = a.dw;
       write_tile_staged<WB, WB, 64 * W_NW, f32x4, TM, TN, EPI_BF16>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
     } else if constexpr (KIND == 1) {
-      o.out = master_out; o.resid = master; o.ldr = d; o.out2 = version; o.eta = eta;
+      o.out = a.master_out; o.resid = a.master; o.ldr = d; o.out2 = a.version; o.eta = a.eta;
       f32_tile_through_lds<WB, WB, W_NW, f32x4, TM, TN, 2, true>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
     } else if constexpr (KIND == 2) {
-      o.out = sums + (int64_t)s * V * d;
+      o.out = a.sums + (int64_t)s * V * d;
       write_tile<f32x4, TM, TN, EPI_F32>(acc, o, m0 + wm0, n0 + wn0, V, d);
     } else {
-      o.out = sums; o.resid = sums; o.ldr = d;
+      o.out = a.sums; o.resid = a.sums; o.ldr = d;
       f32_tile_through_lds<WB, WB, W_NW, f32x4, TM, TN, 3, false>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
     }
   };
   // (the loads of dz run over whole strips, the results end at V)
-  gemm_dtl_body<WB, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(dz + (int64_t)k0 * 32 * 32, 32, 32ll * P, xw + (int64_t)k0 * 32 * 32, 32, 32ll * P, Vp, d,
+  gemm_dtl_body<WB, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, 32ll * P, a.xw + (int64_t)k0 * 32 * 32, 32, 32ll * P, Vp, d,
                                                              (k1 - k0) * 32, bm, bn, Epi{}, nullptr, 0, own);
 }
+template <int KIND>
+__global__ __launch_bounds__(512, 2) void weight_grad_kernel(GradArgs a) { weight_grad_body<KIND>(a, blockIdx.x); }
+// dx in tiles of 128 and dW in one launch, where neither keeps the chip busy for long.  (With dx in tiles of 256, which do, it costs: 8192 tokens,
+// V 128000, d 2048 10.64 ms apart, 10.81 together; 4096, V 32000 1.47 / 1.49; half of 4096, V 50257, d 1024 720 / 710 us.)
+template <int KIND>
+__global__ __launch_bounds__(512, 2) void both_grads_kernel(GradArgs a) {
+  if ((int)blockIdx.x < a.dx_grid) input_grad_body<128>(a, blockIdx.x);
+  else weight_grad_body<KIND>(a, blockIdx.x - a.dx_grid);
+}
 // fp32 sums of stretches or pieces -> dw, or the update
-__global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __restrict__ sums, int S, const int* __restrict__ count, int pieces, int P, int64_t n,
+__global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __restrict__ sums, int S, Rows rows, int pieces, int64_t n,
                                                                uint16_t* __restrict__ dw, const float* __restrict__ master, float* __restrict__ master_out,
                                                                uint16_t* __restrict__ version, float eta) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
   int parts = 1;
   if (pieces == 1) {
-    const int M = piece_rows(*count, 0, P);
+    const int M = rows_of(rows);
     parts = row_stretches(S, div_up(M > 0 ? M : 1, 32));
   }
   f32x4 v[2] = {reinterpret_cast<const f32x4*>(sums + i)[0], reinterpret_cast<const f32x4*>(sums + i)[1]};
@@ -464,19 +522,20 @@ bool big_tiles(int rows, int cols) {
   const int64_t b = (int64_t)div_up(rows, 256) * div_up(cols, 256), m = (int64_t)div_up(rows, 128) * div_up(cols, 128);
   return (double)((b + 255) / 256) * 65536 <= (double)((m + 511) / 512) * 2 * 16384 / 0.83;
 }
-// Tile (256: one workgroup to a CU, 128: two) and stretches of a product [M, N] over nk k-tiles whose fp32 sums a kernel adds: the least
-// modelled time, us.  A round is a start and a walk, whose step takes longer where the launch fills the chip (the forms of gemm_bf16.hip,
-// by 32 in k); the sums are written and read at 5 TB/s.
-CutForm cut_form(int M, int N, int nk, bool mid) {
+// Tile and stretches of a product [M, N] over nk k-tiles whose fp32 sums a kernel adds: the least modelled time, us, of tiles of 256 and, with
+// `small`, of 128 whose walk is split over the two halves of a workgroup; one workgroup to a CU.  A round is a start and a walk, whose
+// step takes longer where the launch fills the chip (the forms 5256 and 1128 of gemm_bf16.hip, by 32 in k); the sums are written and read
+// at 5 TB/s.
+CutForm cut_form(int M, int N, int nk, bool small) {
   CutForm best{256, 1};
   float least = 3e38f;
-  for (int form = 0; form < (mid ? 2 : 1); ++form) {
+  for (int form = 0; form < (small ? 2 : 1); ++form) {
     const int B = form ? 128 : 256;
-    const float slots = form ? 512.f : 256.f, start = form ? 3.1f : 8.9f, t0 = form ? 0.33f : 0.51f, t1 = form ? 0.45f : 0.64f;
+    const float start = form ? 4.3f : 8.9f, t0 = form ? 0.235f : 0.51f, t1 = form ? 0.24f : 0.64f;
     const float tiles = (float)div_up(M, B) * div_up(N, B);
     for (int S = 1; S <= kMostParts && (S == 1 || S * 8 <= nk); S += S < 8 ? 1 : S < 16 ? 2 : S < 32 ? 4 : 8) {
-      const float fill = tiles * S < slots ? tiles * S / slots : 1.f;
-      const float time = ceilf(tiles * S / slots) * (start + ceilf((float)nk / S) * (t0 + (t1 - t0) * fill * fill)) + (float)M * N * S * 8 / 5e6f;
+      const float fill = tiles * S < 256.f ? tiles * S / 256.f : 1.f;
+      const float time = ceilf(tiles * S / 256.f) * (start + ceilf((float)nk / S) * (t0 + (t1 - t0) * fill * fill)) + (float)M * N * S * 8 / 5e6f;
       if (time < least) { least = time; best = {B, S}; }
     }
   }
@@ -501,14 +560,15 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
     q.pieces = (int)((T + P - 1) / P);
   }
   q.P = (int)P;
+  q.few = q.pieces == 1 && T <= kFewRows;
   size_t at = 0;
+  q.count = q.pos = q.idx = q.lab = q.xw = q.info = q.tail = q.e = q.part = q.acc = 0;
   auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
   const size_t all = (size_t)q.pieces * P;
-  q.count = take(4);
-  q.pos = take(4 * all); q.idx = take(4 * all); q.lab = take(4 * all);
+  if (!q.few) { q.count = take(4); q.pos = take(4 * all); q.idx = take(4 * all); q.lab = take(4 * all); }
   q.target = take(4 * P);
   q.stat = take((size_t)8 * (q.Vp / STRIP) * P);
-  q.xw = take((size_t)2 * all * d);
+  if (!q.few || grads) q.xw = take((size_t)2 * all * d);
   if (grads) {
     q.info = take(sizeof(RowInfo) * P);
     q.tail = take((size_t)2 * 64 * ldw);
@@ -528,58 +588,78 @@ hipError_t allow_lds(int bytes) {
   static const hipError_t done = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   return done;
 }
-constexpr int kBigLds = 4 * 2 * dtl_tile_bytes(256, 32), kMidLds = 4 * 2 * dtl_tile_bytes(128, 32);
+constexpr int kBigLds = 4 * 2 * dtl_tile_bytes(256, 32), kMidLds = 4 * 2 * dtl_tile_bytes(128, 32), kSplitLds = split_lds<128, 128, 2, 4>();
 constexpr int kWeightLds = WB * stage_pitch(WB) > upd_image_bytes(WB, WB) ? WB * stage_pitch(WB) : upd_image_bytes(WB, WB);
-static_assert(kWeightLds >= kBigLds && kWeightLds <= 160 * 1024, "LDS of one CU");
+constexpr int kBothLds = kSplitLds > kWeightLds ? kSplitLds : kWeightLds;
+static_assert(kWeightLds >= kBigLds && kBothLds <= 160 * 1024, "LDS of one CU");
+
+Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
+  Rows r{};
+  if (!q.few) {
+    r.count = (const int*)(work + q.count); r.lab = (const int*)(work + q.lab); r.idx = (const int*)(work + q.idx); r.pos = (const int*)(work + q.pos);
+  }
+  r.label = a.label;
+  r.T = q.T; r.V = q.V; r.p = p; r.P = q.P;
+  return r;
+}
 
 template <bool STORE>
-rv_status launch_logits(const Plan& q, char* work, const uint16_t* w, int p, hipStream_t st) {
-  const uint16_t* xw = (const uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d;
-  const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), (const int*)(work + q.lab) + (int64_t)p * q.P,
-                    q.P, q.V, q.Vp};
-  const int* count = (const int*)(work + q.count);
-  const int rows = q.T < q.P ? q.T : q.P;
-  if (big_tiles(rows, q.Vp)) {
+rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const Rows& rows, hipStream_t st) {
+  const uint16_t* w = (const uint16_t*)a.w;
+  const uint16_t* x = q.few ? (const uint16_t*)a.x : (const uint16_t*)(work + q.xw) + (int64_t)rows.p * q.P * q.d;
+  const int64_t ldx = q.few ? a.ldx : 32, x_bs = q.few ? 32 : 32ll * q.P;
+  const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), q.P, q.V, q.Vp};
+  const int most = q.T < q.P ? q.T : q.P;
+  if (big_tiles(most, q.Vp)) {
     constexpr auto kern = logits_kernel<256, 256, 4, 8, STORE>;
     if (allow_lds<kern>(kBigLds) != hipSuccess) return RV_E_DEVICE;
-    hipLaunchKernelGGL(kern, dim3(div_up(rows, 256) * div_up(q.Vp, 256)), dim3(512), kBigLds, st, xw, w, q.ldw, q.d, count, p, o);
+    hipLaunchKernelGGL(kern, dim3(div_up(most, 256) * div_up(q.Vp, 256)), dim3(512), kBigLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
   } else {
     constexpr auto kern = logits_kernel<128, 128, 4, 4, STORE>;
     if (allow_lds<kern>(kMidLds) != hipSuccess) return RV_E_DEVICE;
-    hipLaunchKernelGGL(kern, dim3(div_up(rows, 128) * div_up(q.Vp, 128)), dim3(256), kMidLds, st, xw, w, q.ldw, q.d, count, p, o);
+    hipLaunchKernelGGL(kern, dim3(div_up(most, 128) * div_up(q.Vp, 128)), dim3(256), kMidLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
   }
   return rv_launch_status();
 }
 
-template <int B, int NW, int LDS>
-rv_status launch_input_grad(const Plan& q, char* work, const rv_loss_desc& a, int p, hipStream_t st) {
-  constexpr auto kern = input_grad_kernel<B, B, 4, NW>;
-  if (allow_lds<kern>(LDS) != hipSuccess) return RV_E_DEVICE;
-  const int* count = (const int*)(work + q.count);
-  float* part = (float*)(work + q.part);
-  const int rows = q.T < q.P ? q.T : q.P, vm = div_up(rows, B), vn = div_up(q.d, B), S = q.dx.S;
-  // (fewer tile rows, more stretches: never more workgroups than this, nor more memory)
-  hipLaunchKernelGGL(kern, dim3(vm * vn * S), dim3(64 * NW), LDS, st, (const uint16_t*)(work + q.e), (const uint16_t*)a.w, q.ldw, q.d, q.V, q.Vp, count, p,
-                     q.P, S, vm, (const uint16_t*)(work + q.tail), part);
-  RV_TRY(rv_launch_status());
-  const int64_t chunks = (int64_t)q.T * (q.d / 8);
-  auto join = [&](auto k, int lanes) {
-    hipLaunchKernelGGL(k, dim3((unsigned)((chunks * lanes + 255) / 256)), dim3(256), 0, st, part, (const int*)(work + q.pos), count, p, q.P, q.T, q.d,
-                       q.Vp / 32, B, S, vm, (uint16_t*)a.dx, a.lddx);
-  };
-  if (S > 8) join(input_grad_join_kernel<8>, 8);
-  else join(input_grad_join_kernel<1>, 1);
+template <auto Kern>
+rv_status launch_512(const GradArgs& g, int grid, int lds, hipStream_t st) {
+  if (allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
+  hipLaunchKernelGGL(Kern, dim3(grid), dim3(512), lds, st, g);
   return rv_launch_status();
 }
-
+// KIND of dW, -1: none
 template <int KIND>
-rv_status launch_weight_grad(const Plan& q, char* work, const rv_loss_desc& a, int p, int S, hipStream_t st) {
-  constexpr auto kern = weight_grad_kernel<KIND>;
-  if (allow_lds<kern>(kWeightLds) != hipSuccess) return RV_E_DEVICE;
-  const int tiles = div_up(q.V, WB) * div_up(q.d, WB);
-  hipLaunchKernelGGL(kern, dim3(tiles * S), dim3(64 * W_NW), kWeightLds, st, (const uint16_t*)(work + q.e),
-                     (const uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d, q.d, q.V, q.Vp, (const int*)(work + q.count), p, q.P, S, (float*)(work + q.acc),
-                     (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.eta);
+rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const Rows& rows, hipStream_t st) {
+  GradArgs g{};
+  g.dz = (const uint16_t*)(work + q.e); g.xw = (const uint16_t*)(work + q.xw) + (int64_t)rows.p * q.P * q.d; g.w = (const uint16_t*)a.w;
+  g.ldw = q.ldw; g.rows = rows; g.d = q.d; g.Vp = q.Vp;
+  // (fewer tile rows than all rows have, more stretches: never more workgroups than this, nor more memory)
+  g.S_dx = q.dx.S; g.tiles_m = div_up(q.T < q.P ? q.T : q.P, q.dx.tile);
+  g.dx_grid = a.dx ? g.tiles_m * div_up(q.d, q.dx.tile) * q.dx.S : 0;
+  g.tail = (const uint16_t*)(work + q.tail); g.part = (float*)(work + q.part);
+  g.S_w = q.S_w; g.sums = (float*)(work + q.acc);
+  g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version; g.eta = a.eta;
+  const int w_grid = div_up(q.V, WB) * div_up(q.d, WB) * (KIND == 2 ? q.S_w : 1);
+  // together, but for an update in place: dx reads the weights that it overwrites
+  const bool both = KIND >= 0 && a.dx && q.dx.tile == 128 &&
+                    !(KIND == 1 && rv_overlap(a.w, 2 * (size_t)q.V * q.ldw, a.version, 2 * (size_t)q.V * q.d));
+  if (a.dx && !both) {
+    if (q.dx.tile == 256) RV_TRY((launch_512<input_grad_kernel<256>>(g, g.dx_grid, kBigLds, st)));
+    else RV_TRY((launch_512<input_grad_kernel<128>>(g, g.dx_grid, kSplitLds, st)));
+  }
+  if constexpr (KIND >= 0) {
+    if (both) RV_TRY((launch_512<both_grads_kernel<KIND>>(g, g.dx_grid + w_grid, kBothLds, st)));
+    else RV_TRY((launch_512<weight_grad_kernel<KIND>>(g, w_grid, kWeightLds, st)));
+  }
+  if (!a.dx) return RV_OK;
+  const int64_t chunks = (int64_t)q.T * (q.d / 8);
+  auto join = [&](auto k, int lanes) {
+    hipLaunchKernelGGL(k, dim3((unsigned)((chunks * lanes + 255) / 256)), dim3(256), 0, st, g.part, rows, q.d, q.Vp / 32, q.dx.tile, g.S_dx, g.tiles_m,
+                       (uint16_t*)a.dx, a.lddx);
+  };
+  if (g.S_dx > 8) join(input_grad_join_kernel<8>, 8);
+  else join(input_grad_join_kernel<1>, 1);
   return rv_launch_status();
 }
 
@@ -589,7 +669,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   Plan q;
   if (!make_plan(q, a.T, a.d, a.V, a.ldw, a.rows, grads)) return RV_E_INVAL;
   if (!a.x || !a.w || !a.label || !a.loss || !a.work || a.work_bytes < q.bytes) return RV_E_INVAL;
-  if (a.ldx < a.d || a.ldx % 8 || misaligned(a.x, 16) || misaligned(a.w, 16) || misaligned(a.work, 256) || misaligned(a.label, 8) ||
+  if (a.ldx < a.d || a.ldx % 8 || a.ldx > (1 << 22) || misaligned(a.x, 16) || misaligned(a.w, 16) || misaligned(a.work, 256) || misaligned(a.label, 8) ||
       misaligned(a.loss, 4) || misaligned(a.lse, 4) || misaligned(a.row_scale, 4)) return RV_E_INVAL;
   const bool update = grads && a.master;
   if (grads) {
@@ -602,49 +682,44 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   const hipStream_t st = (hipStream_t)a.stream;
   char* work = (char*)a.work;
   const uint16_t* w = (const uint16_t*)a.w;
-  int* count = (int*)(work + q.count);
-  int* lab = (int*)(work + q.lab);
-  int per = 4;
-  while (per < 64 && per * 1024 < q.T) per *= 2;
-  const int row_blocks = div_up(q.T, per), tail_blocks = grads ? q.Vp - q.V / 32 * 32 : 0;
-  hipLaunchKernelGGL(gather_kernel, dim3(row_blocks + tail_blocks), dim3(256), 0, st, (const uint16_t*)a.x, a.ldx, a.label, q.T, q.d, q.V, q.P, per, count,
-                     (int*)(work + q.pos), (int*)(work + q.idx), lab, (uint16_t*)(work + q.xw), a.loss, a.lse, w, q.ldw,
-                     grads ? (uint16_t*)(work + q.tail) : nullptr, row_blocks);
-  RV_TRY(rv_launch_status());
-  const int strips = q.Vp / STRIP, S = grads ? q.S_w : 1;
-  const int rows = q.T < q.P ? q.T : q.P;
+  const int tail_rows = grads ? q.Vp - q.V / 32 * 32 : 0;
+  if (!q.few) {
+    int per = 4;
+    while (per < 64 && per * 1024 < q.T) per *= 2;
+    const int row_blocks = div_up(q.T, per);
+    hipLaunchKernelGGL(gather_kernel, dim3(row_blocks + tail_rows), dim3(256), 0, st, (const uint16_t*)a.x, a.ldx, a.label, q.T, q.d, q.V, q.P, per,
+                       (int*)(work + q.count), (int*)(work + q.pos), (int*)(work + q.idx), (int*)(work + q.lab), (uint16_t*)(work + q.xw), a.loss, a.lse, w,
+                       q.ldw, (uint16_t*)(work + q.tail), row_blocks);
+    RV_TRY(rv_launch_status());
+  }
+  const int strips = q.Vp / STRIP, most = q.T < q.P ? q.T : q.P;
+  const bool cut = q.pieces > 1 || (grads && q.S_w > 1);      // dW through fp32 sums
   for (int p = 0; p < q.pieces; ++p) {
-    if (grads) RV_TRY(launch_logits<true>(q, work, w, p, st));
-    else RV_TRY(launch_logits<false>(q, work, w, p, st));
+    const Rows rows = rows_at(q, work, a, p);
+    if (grads) RV_TRY(launch_logits<true>(q, work, a, rows, st));
+    else RV_TRY(launch_logits<false>(q, work, a, rows, st));
     RowInfo* info = grads ? (RowInfo*)(work + q.info) : nullptr;
-    hipLaunchKernelGGL(join_kernel, dim3(div_up(rows, 16)), dim3(1024), 0, st, (const float2*)(work + q.stat), (const float*)(work + q.target),
-                       lab + (int64_t)p * q.P, (const int*)(work + q.idx) + (int64_t)p * q.P, count, p, q.P, strips, a.scale, a.row_scale, a.loss, a.lse, info);
+    hipLaunchKernelGGL(join_kernel, dim3(div_up(most, 16)), dim3(1024), 0, st, (const float2*)(work + q.stat), (const float*)(work + q.target), rows, strips,
+                       a.scale, a.row_scale, a.loss, a.lse, info);
     RV_TRY(rv_launch_status());
     if (!grads) continue;
     // strips a block takes one after the other: up to 8, fewer where that leaves fewer than 2048 blocks
-    const int64_t dz_blocks = (int64_t)div_up(rows, 64) * strips / 2048;
-    const int per_dz = dz_blocks < 1 ? 1 : dz_blocks < 8 ? (int)dz_blocks : 8;
-    hipLaunchKernelGGL(dz_kernel, dim3(div_up(rows, 64), div_up(strips, per_dz)), dim3(256), 0, st, (uint16_t*)(work + q.e), (const float2*)(work + q.stat), info,
-                       count, p, q.P, strips, per_dz, (uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d, q.d);
+    const int64_t dz_blocks = (int64_t)div_up(most, 64) * strips / 2048;
+    const int per_dz = dz_blocks < 1 ? 1 : dz_blocks < 8 ? (int)dz_blocks : 8, strip_blocks = div_up(strips, per_dz);
+    hipLaunchKernelGGL(dz_kernel, dim3(div_up(most, 64), strip_blocks + (q.few ? div_up(q.d / 32, 8) + tail_rows : 0)), dim3(256), 0, st,
+                       (uint16_t*)(work + q.e), (const float2*)(work + q.stat), info, rows, strips, per_dz, strip_blocks,
+                       (uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d, q.d, (const uint16_t*)a.x, a.ldx, w, q.ldw, (uint16_t*)(work + q.tail));
     RV_TRY(rv_launch_status());
-    if (a.dx) {
-      if (q.dx.tile == 256) RV_TRY((launch_input_grad<256, 8, kBigLds>(q, work, a, p, st)));
-      else RV_TRY((launch_input_grad<128, 4, kMidLds>(q, work, a, p, st)));
-    }
-    if (!a.dw && !update) continue;
-    if (q.pieces == 1 && S == 1) {
-      if (update) RV_TRY(launch_weight_grad<1>(q, work, a, p, 1, st));
-      else RV_TRY(launch_weight_grad<0>(q, work, a, p, 1, st));
-    } else if (p == 0) {
-      RV_TRY(launch_weight_grad<2>(q, work, a, p, S, st));
-    } else {
-      RV_TRY(launch_weight_grad<3>(q, work, a, p, 1, st));
-    }
+    if (!a.dw && !update) RV_TRY(launch_grads<-1>(q, work, a, rows, st));
+    else if (p > 0) RV_TRY(launch_grads<3>(q, work, a, rows, st));
+    else if (cut) RV_TRY(launch_grads<2>(q, work, a, rows, st));
+    else if (update) RV_TRY(launch_grads<1>(q, work, a, rows, st));
+    else RV_TRY(launch_grads<0>(q, work, a, rows, st));
   }
-  if (grads && (a.dw || update) && (q.pieces > 1 || S > 1)) {
+  if (grads && (a.dw || update) && cut) {
     const int64_t n = (int64_t)q.V * q.d;
-    hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, (const float*)(work + q.acc), S, count, q.pieces, q.P, n,
-                       (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.eta);
+    hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, (const float*)(work + q.acc), q.S_w,
+                       rows_at(q, work, a, 0), q.pieces, n, (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.eta);
     RV_TRY(rv_launch_status());
   }
   return RV_OK;

@@ -31,7 +31,7 @@ def _inputs(seed, T, d, V, out=0.0, sure=6.0):
 
 
 def _reference(x, w, label, g):
-    """loss, lse, dz [T, V], and the bound of the logits' error, in 64 bits; rows out of the batch are zero"""
+    """loss, lse, dz [T, V], and the bound of the logits' error, in 64 bits (where the operands are); rows out of the batch are zero"""
     T, d = x.shape
     V = w.shape[0]
     takes = (label >= 0) & (label < V)
@@ -42,7 +42,7 @@ def _reference(x, w, label, g):
     at = z.gather(1, y[:, None])[:, 0]
     p = torch.exp(z - lse[:, None])
     hot = torch.zeros_like(z)
-    hot[torch.arange(T), y] = 1.0
+    hot.scatter_(1, y[:, None], 1.0)
     gt = torch.where(takes, g.double(), 0.0)[:, None]
     dz = (p - hot) * gt
     zerr = (d + 8) * 2.0 ** -24 * float((x64.abs() @ w64.abs().T).max())
@@ -52,29 +52,29 @@ def _reference(x, w, label, g):
 
 def _check(x, w, label, g, got_loss, got_lse, dx=None, dw=None, master=None, eta=0.0, new=None, version=None):
     loss, lse, dz, zerr, x64, w64, y, takes = _reference(x, w, label, g)
-    V = w.shape[0]
+    V, here = w.shape[0], x.device
     slack = 2 * zerr + (80 + V / 64) * 2.0 ** -24 + 2.0 ** -22 * float(lse.abs().max())
     for got, ref in ((got_loss, loss), (got_lse, lse)):
         if got is not None:
-            assert float((got.cpu().double() - ref).abs().max()) <= slack
+            assert float((got.to(here).double() - ref).abs().max()) <= slack
     # what dz may be off by: relative, but absolute (times the row's weight) at the label
     weight = torch.where(takes, g.double().abs(), 0.0)[:, None]
     off = dz.abs() * (2.0 ** -8 + 2.0 ** -10 + 2 * slack) + weight * 2.0 ** -40
-    rows = torch.arange(len(y))
+    rows = torch.arange(len(y), device=here)
     off[rows, y] = dz[rows, y].abs() * 2.0 ** -8 + torch.where(takes, g.double().abs(), 0.0) * slack
     fp32 = 2.0 ** -24 * (x.shape[0] + V)      # accumulation of the products of dz, relative to the sums of absolute values
     if dx is not None:
         ref = dz @ w64
         bound = (off + dz.abs() * fp32) @ w64.abs()
-        assert bool(((dx.cpu().double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
-        assert not dx.cpu()[~takes].any()
+        assert bool(((dx.to(here).double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
+        assert not dx.to(here)[~takes].any()
     ref = dz.T @ x64
     bound = (off + dz.abs() * fp32).T @ x64.abs()
     if dw is not None:
-        assert bool(((dw.cpu().double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
+        assert bool(((dw.to(here).double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
     if new is not None:
-        want = master.cpu().double() - eta * ref
-        assert bool(((new.cpu().double() - want).abs() <= eta * bound + 2.0 ** -23 * (want.abs() + eta * ref.abs())).all())
+        want = master.to(here).double() - eta * ref
+        assert bool(((new.to(here).double() - want).abs() <= eta * bound + 2.0 ** -23 * (want.abs() + eta * ref.abs())).all())
         assert torch.equal(version, new.to(torch.bfloat16))
 
 
@@ -93,6 +93,22 @@ def test_loss_and_gradients(T, d, V, out):
     _check(x, w, label, g, loss, lse)
     loss2, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=1.0 / T)
     _check(x, w, label, g, loss2, None, dx, dw)
+
+
+# tiles of 256 for dx (many rows of a wide state), half of the rows out; rows that a workgroup's label count walks over in more than one turn
+@pytest.mark.parametrize("T,d,V,out", [(4096, 4096, 1000, 0.5), (2048, 8192, 600, 0.0), (20000, 64, 100, 0.3)])
+def test_many_rows(T, d, V, out):
+    x, w, label, master = (t.cuda() for t in _inputs(2, T, d, V, out))
+    g = torch.full((T,), 1.0, device="cuda")
+    loss, dx, dw = rv.loss_step(x, w, label)
+    _check(x, w, label, g, loss, None, dx, dw)
+    got = rv.loss_step(x, w, label, master=master, eta=0.1)
+    assert torch.equal(got[0], loss) and torch.equal(got[1], dx)
+    _check(x, w, label, g, loss, None, dx, None, master, 0.1, got[2], got[3])
+    # in place
+    again = rv.loss_step(x, w, label, master=master, eta=0.1, master_out=master, version=w)
+    for a, b in zip(again, got):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("T,d,V,rows", [(300, 128, 777, 64), (300, 320, 1031, 128), (1100, 192, 513, 512), (65, 64, 100, 1)])

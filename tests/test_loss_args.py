@@ -46,7 +46,7 @@ def _desc(**change):
 
 @pytest.mark.parametrize("change", [
     dict(x=None), dict(w=None), dict(label=None), dict(loss=None), dict(work=None), dict(work_bytes=0), dict(x=1026), dict(w=2056), dict(label=4100),
-    dict(loss=8194), dict(lse=16386), dict(work=(1 << 20) + 16), dict(ldx=120), dict(ldx=130), dict(ldw=130), dict(ldw=64), dict(row_scale=2),
+    dict(loss=8194), dict(lse=16386), dict(work=(1 << 20) + 16), dict(ldx=120), dict(ldx=130), dict(ldx=(1 << 22) + 8), dict(ldw=130), dict(ldw=64), dict(row_scale=2),
     dict(T=0), dict(d=96), dict(V=0), dict(rows=-5)])
 def test_refused_by_both(change):
     a = _desc(**change)
