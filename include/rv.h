@@ -274,7 +274,7 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *             same call, master_out = master - eta * dz^T x (fp32), version = its bf16 rounding.  The product's fp32 sums are used,
  *             not their rounding.  master_out may be master, version may be w.
  * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16.
- *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 64): bounds the work
+ *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 128 or a multiple of 256): bounds the work
  *             memory at about 2 V * rows bytes; with several such pieces dw is added up in fp32, 4 V d bytes more.
  *             0: as many as 2 GiB hold.  Outputs do not depend on it but for the order of those sums.
  *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).

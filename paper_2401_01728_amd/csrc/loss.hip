@@ -176,73 +176,78 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {   // round to
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, f16x2));
 }
 
+// label: of the lane's rows, -1 where there is none.  Rows behind the last one are written like the others (P is whole tiles) and never read.
 template <bool STORE, int TM, int TN>
-__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, const Rows& rows, int mw, int nw0, int M) {
-  constexpr int TS = STRIP / 16;
-  static_assert(TN % TS == 0, "a wave's columns are whole strips");
-  const int l = threadIdx.x & 63, grp = l >> 4;
+__device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const LogitsOut& o, const int (&label)[TM], int mw, int nw, int M) {
+  static_assert(TN * 16 == STRIP, "a wave's columns are one strip");
+  if (nw >= o.Vp || mw >= M) return;
+  const int l = threadIdx.x & 63, grp = l >> 4, strip = nw / STRIP, row0 = mw + (l & 15);
+  f32x4 a[TM][TN];
+  bool hit = false;
 #pragma unroll
-  for (int u = 0; u < TN / TS; ++u) {
-    const int nw = nw0 + u * STRIP, strip = nw / STRIP;
-    if (nw >= o.Vp || mw >= M) return;
-    const bool ragged = nw + STRIP > o.V;     // (wave-uniform)
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int c = 0; c < TN; ++c) a[i][c] = acc[i][c];
+    hit |= (unsigned)(label[i] - nw) < (unsigned)STRIP;
+  }
+  // One branch for all rows each: a branch for every one of them would keep the rows' chains of instructions apart.
+  if (nw + STRIP > o.V) {                                  // (wave-uniform) the last strip ends inside
+    asm volatile("");
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int c = 0; c < TN; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (nw + c * 16 + 4 * grp + k >= o.V) a[i][c][k] = -INFINITY;
+  }
+  if (__builtin_amdgcn_ballot_w64(hit)) {                  // few strips hold a label of their rows
+    asm volatile("");
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int row = mw + i * 16 + (l & 15);
-      const bool ok = row < M;
-      f32x4 a[TS];
+      const int y = label[i] - nw;
 #pragma unroll
-      for (int c = 0; c < TS; ++c) {
-        a[c] = acc[i][u * TS + c];
-        if (ragged) {
+      for (int c = 0; c < TN; ++c)
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (nw + c * 16 + 4 * grp + k >= o.V) a[c][k] = -INFINITY;
-        }
+        for (int k = 0; k < 4; ++k)
+          if (y == c * 16 + 4 * grp + k) o.target[row0 + i * 16] = a[i][c][k];
+    }
+  }
+  float2* stat = o.stat + (int64_t)strip * o.P + row0;
+  uint16_t* e = o.e + ((int64_t)2 * strip * o.P + row0) * 32 + (grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp);
+  const int64_t block = 32ll * o.P;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    float m = a[i][0][0];
+#pragma unroll
+    for (int c = 0; c < TN; ++c)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m = fmaxf(m, a[i][c][k]);
+    m = __fmaf_rn(quad_max(m), kLog2e, -(float)kTop);
+    const float base = m == -INFINITY ? 0.f : m;           // (a strip of -inf alone: its sum is zero)
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < TN; ++c)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        a[i][c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[i][c][k], kLog2e, -base));
+        sum += a[i][c][k];
       }
-      const int y = ok ? label_of(rows, row) - nw : -1;
-      if (__builtin_amdgcn_ballot_w64(y >= 0 && y < STRIP)) {   // few strips hold a label of their rows
-        float at = 0.f;
-        bool mine = false;
+    sum = quad_sum(sum);
+    if (grp == 0) stat[i * 16] = float2{m, sum};
+    if (STORE) {
+      // Two quads of a lane are 16 columns apart; the swap of lane rows of 16 gives even rows eight consecutive columns of the first
+      // quad and odd ones of the second, and a wave's 16 bytes a lane are one run of 1 KiB of the block of 32 columns.
 #pragma unroll
-        for (int c = 0; c < TS; ++c)
+      for (int b = 0; b < TN / 2; ++b) {
+        u32x4 v;
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (y == c * 16 + 4 * grp + k) { at = a[c][k]; mine = true; }
-        if (mine) o.target[row] = at;
-      }
-      float m = a[0][0];
-#pragma unroll
-      for (int c = 0; c < TS; ++c)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) m = fmaxf(m, a[c][k]);
-      m = __fmaf_rn(quad_max(m), kLog2e, -(float)kTop);
-      const float base = m == -INFINITY ? 0.f : m;   // (a strip of -inf alone: its sum is zero)
-      float sum = 0.f;
-#pragma unroll
-      for (int c = 0; c < TS; ++c)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          a[c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[c][k], kLog2e, -base));
-          sum += a[c][k];
+        for (int h = 0; h < 2; ++h) {
+          const auto s = __builtin_amdgcn_permlane16_swap(pack_f16(a[i][2 * b][2 * h], a[i][2 * b][2 * h + 1]),
+                                                          pack_f16(a[i][2 * b + 1][2 * h], a[i][2 * b + 1][2 * h + 1]), false, false);
+          v[h] = s[0]; v[2 + h] = s[1];
         }
-      sum = quad_sum(sum);
-      if (grp == 0 && ok) o.stat[(int64_t)strip * o.P + row] = float2{m, sum};
-      if (STORE) {
-        // Two quads of a lane are 16 columns apart; the swap of lane rows of 16 gives even rows eight consecutive columns of the first
-        // quad and odd ones of the second, and a wave's 16 bytes a lane are one run of 1 KiB of the block of 32 columns.
-#pragma unroll
-        for (int b = 0; b < TS / 2; ++b) {
-          u32x4 v;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const auto s = __builtin_amdgcn_permlane16_swap(pack_f16(a[2 * b][2 * h], a[2 * b][2 * h + 1]),
-                                                            pack_f16(a[2 * b + 1][2 * h], a[2 * b + 1][2 * h + 1]), false, false);
-            v[h] = s[0]; v[2 + h] = s[1];
-          }
-          const int col = grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp;
-          if (ok) *reinterpret_cast<u32x4*>(o.e + ((int64_t)(2 * strip + b) * o.P + row) * 32 + col) = v;
-        }
+        *reinterpret_cast<u32x4*>(e + b * block + i * 512) = v;
       }
     }
   }
@@ -257,7 +262,13 @@ __global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __re
   if ((int)blockIdx.x >= vm * vn) return;
   int bm, bn;
   band_tile(xcd_range(blockIdx.x, vm * vn), vm, vn, bm, bn);
-  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, rows, m0 + wm0, n0 + wn0, M); };
+  // the labels of this lane's rows, asked for here: behind the walk along d each would be a round trip of its own
+  constexpr int TM = BM / 2 / 16;
+  const int first = bm * BM + (threadIdx.x >> 6 & 1) * (BM / 2) + (threadIdx.x & 15);
+  int label[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) label[i] = first + i * 16 < M ? label_of(rows, first + i * 16) : -1;
+  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, label, m0 + wm0, n0 + wn0, M); };
   gemm_dtl_body<BM, BN, 32, NS, NW, false, false, EPI_OWN>(x, ldx, x_bs, w, ldw, 32, M, o.V, d, bm, bn, Epi{}, nullptr, 0, own);
 }
 
@@ -565,19 +576,14 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   if (T < 1 || T > (1 << 24) || d < 64 || d % 64 || d > 16384 || V < 1 || V > (1 << 24) || ldw < d || ldw % 8 || rows < 0) return false;
   if (V * ldw >= (1ll << 31)) return false;       // offsets in the logits' product
   q.T = (int)T; q.d = (int)d; q.V = (int)V; q.Vp = round_up((int)V, STRIP); q.grads = grads; q.ldw = ldw;
-  int64_t most = kMostE / (q.Vp > q.d ? q.Vp : q.d) / 64 * 64;
-  if (rows && rows < most) most = (rows + 63) / 64 * 64;
-  const int64_t whole = (T + 63) / 64 * 64;
-  q.pieces = (int)((whole + most - 1) / most);
-  // pieces of nearly the same size, of whole tiles where there are several
-  int64_t P = whole;
-  if (q.pieces > 1) {
-    const int64_t step = most >= 512 ? 256 : 64;
-    P = (T + q.pieces - 1) / q.pieces;
-    P = (P + step - 1) / step * step;
-    if (P > most) P = most;
-    q.pieces = (int)((T + P - 1) / P);
-  }
+  // pieces of nearly the same size, of whole tiles of the logits' product: of 128 rows where that is all, else of 256
+  auto tiles = [](int64_t n) { return n <= 128 ? 128 : (n + 255) / 256 * 256; };
+  int64_t most = kMostE / (q.Vp > q.d ? q.Vp : q.d);
+  most = most < 256 ? 128 : most / 256 * 256;
+  if (rows && rows < most) most = tiles(rows);
+  q.pieces = (int)((T + most - 1) / most);
+  const int64_t P = tiles((T + q.pieces - 1) / q.pieces);
+  q.pieces = (int)((T + P - 1) / P);
   q.P = (int)P;
   q.few = q.pieces == 1 && T <= kFewRows;
   size_t at = 0;
