@@ -2,16 +2,18 @@
 //
 //   z = x W^T           x bf16 [T, d], W bf16 [V, d], z in fp32 registers only
 //   loss_t = lse_t - z[t, y_t],   lse_t = ln sum_v exp z[t, v]
-//   dz[t, v] = g_t (exp(z[t, v] - lse_t) - [v = y_t])
-//   dx = dz W,  dW = dz^T x       three products of 2 T V d flop each; the forward alone is one
+//   dz[t, v] = r_t (exp(z[t, v] - lse_t) - [v = y_t])      r: the caller's weight of a row
+//   dx = s dz W,  dW = s dz^T x                              s: the caller's scale, on the fp32 sums (in dz, where labels' entries are
+//                                                            near -1, its rounding would be that of all of them: a bias)
+// Three products of 2 T V d flop each; the forward alone is one.
 //
 // The logits are never written.  A wave of the first product holds 64 columns of the vocabulary - a strip - of its rows; it takes
 // each row's maximum over the strip (fp32), m = max z log2 e - 15, and writes the pair (m, sum of exp2(z log2 e - m)) and, for the
 // gradients, the exponentials e themselves in fp16: they are at most 2^15 whatever the logits are, keep 11 bits down to 2^-29 of the
 // strip's largest and are off by less than 2^-40 of it below.  (Logits in 16 bits would move a probability by |z| 2^-9 of itself, e in
 // bf16 by 2^-8: with the rounding of dz the gradients were then 1.6 times as far from 64 bits as their own rounding, now 1.2.)  The pairs of
-// a row's strips are joined to its lse, and  dz = e exp2(m - lse2) g  overwrites e in place, rounded to bf16, which is what the matrix
-// instructions take.  The label's own column gets  g expm1(z_y - lse)  from the fp32 logit: where the model is nearly certain,
+// a row's strips are joined to its lse, and  dz = e exp2(m - lse2) r  overwrites e in place, rounded to bf16, which is what the matrix
+// instructions take.  The label's own column gets  r expm1(z_y - lse)  from the fp32 logit: where the model is nearly certain,
 // p - 1 from a rounded p would have no digits left.
 // Computing z again for the gradients instead of keeping e would be a fourth product: 2 bytes of e written and 4 moved by the pass
 // that makes dz of it are 1.2 ps a logit at 5 TB/s, the product 2 d / 1.3 PFLOP/s = 1.6 ps at d 1024, 3.2 ps at 2048.
@@ -36,7 +38,7 @@ struct RowInfo { float lse2, g, at_label; int label; };
 
 struct CutForm { int tile, S; };
 struct Plan {
-  int T, d, V, Vp, P, pieces;            // V rounded up to whole strips; rows of a piece and their number
+  int T, d, V, Vp, P, R, pieces;         // V rounded up to whole strips; rows of a piece, of a block of e; number of pieces
   bool grads, few;                       // few: rows are not gathered
   int64_t ldw;
   CutForm dx;                            // tile and stretches of dx; stretches of dW
@@ -53,12 +55,16 @@ struct Rows {
   const int* count; const int* lab; const int* idx; const int* pos;
   const int64_t* label;
   int T, V, p, P;
+  int R;                                   // rows of a block of columns of e and of the copy of x: P, or 2 P for dz in two parts
+  int twice;                               // dW of dz in two parts (dz_kernel)
 };
 constexpr int kFewRows = 256;
 __device__ __forceinline__ int rows_of(const Rows& r) {
   const int left = (r.count ? *r.count : r.T) - r.p * r.P;
   return left < r.P ? left : r.P;
 }
+// k-tiles of dW's product over them, one of zeros where there is none
+__device__ __forceinline__ int row_tiles(const Rows& r, int M) { return div_up(M > 0 ? M : 1, 32) << r.twice; }
 // the label of a row of the piece, -1: takes no part
 __device__ __forceinline__ int label_of(const Rows& r, int row) {
   if (r.count) return r.lab[r.p * r.P + row];
@@ -151,10 +157,10 @@ __device__ __forceinline__ void band_tile(int i, int vm, int vn, int& bm, int& b
 // (The tiles are dealt out over the tile rows that are there: a map over the rows of all tokens would leave whole XCDs without work where half
 // of the rows are out.)
 struct LogitsOut {
-  uint16_t* e;         // [Vp / 32][P][32]
+  uint16_t* e;         // [Vp / 32][R][32]
   float2* stat;        // [Vp / 64][P]
   float* target;       // [P] the label's logit
-  int P, V, Vp;
+  int P, R, V, Vp;
 };
 
 // max and sum over the four lanes (l / 16) that share a row, left in all of them: lane rows swapped with their neighbours, then halves
@@ -214,8 +220,8 @@ __device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const
     }
   }
   float2* stat = o.stat + (int64_t)strip * o.P + row0;
-  uint16_t* e = o.e + ((int64_t)2 * strip * o.P + row0) * 32 + (grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp);
-  const int64_t block = 32ll * o.P;
+  uint16_t* e = o.e + ((int64_t)2 * strip * o.R + row0) * 32 + (grp & 1 ? 16 + 4 * (grp - 1) : 4 * grp);
+  const int64_t block = 32ll * o.R;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     float m = a[i][0][0];
@@ -274,7 +280,7 @@ __global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __re
 
 // ---- strips joined to rows ----------------------------------------------------------------------
 // 16 rows to a block, 64 lanes to a row: a strip's pairs of 16 rows are one line.
-__global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ stat, const float* __restrict__ target, Rows rows, int strips, float scale,
+__global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ stat, const float* __restrict__ target, Rows rows, int strips,
                                                     const float* __restrict__ row_scale, float* __restrict__ loss, float* __restrict__ lse,
                                                     RowInfo* __restrict__ info) {
   __shared__ float2 part[64][17];
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
   loss[t] = ln - at;
   if (lse) lse[t] = ln;
   if (info) {
-    const float g = row_scale ? scale * row_scale[t] : scale;
+    const float g = row_scale ? row_scale[t] : 1.0f;
     info[row] = RowInfo{lse2, g, g * expm1f(at - ln), y};
   }
 }
@@ -316,6 +322,10 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
 // ---- e -> dz, in place ----------------------------------------------------------------------
 // 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those from the
 // last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
+// Two parts (`twice`, few rows and an update): what dz loses to bf16 is rounded itself and stands, with the same rows of x, behind the rows, so that
+// dW has 16 bits of the labels' entries, which are most of it, and the 11 of e of the others - the fp32 master would otherwise be off by up to
+// 2^-9 of a single token's whole step.  The product is bound by the weights there; with many rows it would take twice as long, and what
+// one of them is off by is small against the step of all.
 // Where rows are not gathered the copy is made here, by the blocks behind the strips', and the tail of W by those behind them.
 __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info, Rows rows,
                                                  int strips, int per, int strip_blocks, uint16_t* __restrict__ xw, int d, const uint16_t* __restrict__ x,
@@ -337,21 +347,29 @@ __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const
     }
     if (row >= end) return;
     const bool in = row < M && label_of(rows, row) >= 0;
-    for (int cb = c0; cb < c0 + 8 && cb < d / 32; ++cb)
-      *reinterpret_cast<u32x4*>(xw + ((int64_t)cb * P + row) * 32 + q * 8) = in ? *reinterpret_cast<const u32x4*>(x + (int64_t)row * ldx + cb * 32 + q * 8) : zero;
+    for (int cb = c0; cb < c0 + 8 && cb < d / 32; ++cb) {
+      const u32x4 v = in ? *reinterpret_cast<const u32x4*>(x + (int64_t)row * ldx + cb * 32 + q * 8) : zero;
+      uint16_t* to = xw + ((int64_t)cb * rows.R + row) * 32 + q * 8;
+      *reinterpret_cast<u32x4*>(to) = v;
+      if (rows.twice) *reinterpret_cast<u32x4*>(to + end * 32) = v;
+    }
     return;
   }
   if (row >= end) return;
   const int s0 = blockIdx.y * per, s1 = s0 + per < strips ? s0 + per : strips;
   uint16_t* base = e + (int64_t)row * 32 + q * 8;
-  const int64_t bs = 32ll * P;
+  const int64_t bs = 32ll * rows.R;
   if (row >= M || info[row].label < 0) {
     for (int s = s0; s < s1; ++s) {
       *reinterpret_cast<u32x4*>(base + 2 * s * bs) = zero;
       *reinterpret_cast<u32x4*>(base + (2 * s + 1) * bs) = zero;
+      if (rows.twice) {
+        *reinterpret_cast<u32x4*>(base + 2 * s * bs + end * 32) = zero;
+        *reinterpret_cast<u32x4*>(base + (2 * s + 1) * bs + end * 32) = zero;
+      }
     }
     if (rows.count && blockIdx.y == 0) {
-      for (int cb = 0; cb < d / 32; ++cb) *reinterpret_cast<u32x4*>(xw + ((int64_t)cb * P + row) * 32 + q * 8) = zero;
+      for (int cb = 0; cb < d / 32; ++cb) *reinterpret_cast<u32x4*>(xw + ((int64_t)cb * rows.R + row) * 32 + q * 8) = zero;
     }
     return;
   }
@@ -373,7 +391,14 @@ __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const
       const int y = r.label - ((2 * s + h) * 32 + q * 8);
 #pragma unroll
       for (int k = 0; k < 8; ++k) v[k >> 2][k & 3] = y == k ? r.at_label : v[k >> 2][k & 3] * f;
-      *at = f32_to_bf16x8(v);
+      const u32x4 rounded = f32_to_bf16x8(v);
+      *at = rounded;
+      if (rows.twice) {
+        f32x4 back[2];
+        bf16x8_to_f32(back, rounded);
+        v[0] -= back[0]; v[1] -= back[1];
+        at[end * 4] = f32_to_bf16x8(v);
+      }
     }
   }
 }
@@ -397,13 +422,14 @@ struct GradArgs {
   int S_dx, tiles_m, dx_grid;             // dx: stretches for all rows, their tile rows, workgroups
   const uint16_t* tail; float* part;
   int S_w;                                // dW
-  float* sums; uint16_t* dw; const float* master; float* master_out; uint16_t* version; float eta;
+  float* sums; uint16_t* dw; const float* master; float* master_out; uint16_t* version;
+  float scale, eta;                       // eta: times scale
 };
 // BM 256: tiles of 256x256, eight waves, in order of k; 128: of 128x128, the walk split over two groups of four waves.  The last k-tiles, which
 // end behind the last row of W, come from its copy with zeros behind (there is nothing behind W that could be read).
 template <int BM>
 __device__ __forceinline__ void input_grad_body(const GradArgs& a, int id) {
-  const int d = a.d, V = a.rows.V, P = a.rows.P, M = rows_of(a.rows);
+  const int d = a.d, V = a.rows.V, M = rows_of(a.rows);
   if (M <= 0) return;
   const int vm = div_up(M, BM), vn = div_up(d, BM), tiles = vm * vn, nk = a.Vp / 32;
   const int S = stretches(a.S_dx, a.tiles_m, vm, nk);
@@ -415,12 +441,13 @@ __device__ __forceinline__ void input_grad_body(const GradArgs& a, int id) {
   const int k0 = (int)((int64_t)nk * s / S), k1 = (int)((int64_t)nk * (s + 1) / S);
   Epi out{};
   out.out = a.part + (int64_t)s * vm * BM * d; out.ldo = d;
-  const uint16_t* A = a.dz + (int64_t)k0 * 32 * P;
+  const uint16_t* A = a.dz + (int64_t)k0 * 32 * a.rows.R;
+  const int64_t bs = 32ll * a.rows.R;
   const uint16_t* B = a.w + (int64_t)k0 * 32 * a.ldw;
   if constexpr (BM == 256)
-    gemm_dtl_body<256, 256, 32, 4, 8, false, true, EPI_F32, true>(A, 32, 32ll * P, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
+    gemm_dtl_body<256, 256, 32, 4, 8, false, true, EPI_F32, true>(A, 32, bs, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
   else
-    gemm_split_body<128, 128, 2, 4, 4, false, true, EPI_F32, true>(A, 32, 32ll * P, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
+    gemm_split_body<128, 128, 2, 4, 4, false, true, EPI_F32, true>(A, 32, bs, B, a.ldw, 32, M, d, (k1 - k0) * 32, bm, bn, out, a.tail, V / 32 - k0);
 }
 template <int BM>
 __global__ __launch_bounds__(512, 2) void input_grad_kernel(GradArgs a) { input_grad_body<BM>(a, blockIdx.x); }
@@ -429,7 +456,7 @@ __global__ __launch_bounds__(512, 2) void input_grad_kernel(GradArgs a) { input_
 // columns, 64 stretches: 25 us with one lane).
 template <int LANES>
 __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __restrict__ part, Rows rows, int d, int nk, int bm, int S_all, int tiles_m,
-                                                              uint16_t* __restrict__ dx, int64_t lddx) {
+                                                              float scale, uint16_t* __restrict__ dx, int64_t lddx) {
   const int M = rows_of(rows), p = rows.p, P = rows.P;
   if (M <= 0 && p) return;
   const int lane = LANES > 1 ? threadIdx.x / (256 / LANES) : 0;
@@ -461,6 +488,7 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
       v[1] += sum[1][threadIdx.x + x * (256 / LANES)];
     }
   }
+  v[0] *= scale; v[1] *= scale;
   if (in && (here || (j < 0 && p == 0))) *reinterpret_cast<u32x4*>(dx + (int64_t)t * lddx + c) = f32_to_bf16x8(v);
 }
 
@@ -471,13 +499,10 @@ constexpr int WB = 256, W_NS = 4, W_NW = 8;
 __device__ __forceinline__ int row_stretches(int S, int nk) { return S < nk ? S : nk; }
 template <int KIND>
 __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
-  const int d = a.d, V = a.rows.V, Vp = a.Vp, P = a.rows.P;
-  int M = rows_of(a.rows);
-  if (M <= 0) {
-    if (a.rows.p) return;
-    M = 1;                                        // (a tile of zeros: dz_kernel)
-  }
-  const int nk = div_up(M, 32), vm = div_up(V, WB), vn = div_up(d, WB), tiles = vm * vn, parts = KIND == 2 ? row_stretches(a.S_w, nk) : 1;
+  const int d = a.d, V = a.rows.V, Vp = a.Vp, M = rows_of(a.rows);
+  if (M <= 0 && a.rows.p) return;
+  const int64_t bs = 32ll * a.rows.R;
+  const int nk = row_tiles(a.rows, M), vm = div_up(V, WB), vn = div_up(d, WB), tiles = vm * vn, parts = KIND == 2 ? row_stretches(a.S_w, nk) : 1;
   if (id >= tiles * parts) return;
   id = xcd_range(id, tiles * parts);
   const int s = id / tiles;
@@ -489,7 +514,12 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
     o.ldo = d;
     if constexpr (KIND == 0) {
       o.out = a.dw;
-      write_tile_staged<WB, WB, 64 * W_NW, f32x4, TM, TN, EPI_BF16>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
+      f32x4 scaled[TM][TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) scaled[i][j] = acc[i][j] * a.scale;
+      write_tile_staged<WB, WB, 64 * W_NW, f32x4, TM, TN, EPI_BF16>(scaled, o, m0, n0, wm0, wn0, V, d, dtl_smem);
     } else if constexpr (KIND == 1) {
       o.out = a.master_out; o.resid = a.master; o.ldr = d; o.out2 = a.version; o.eta = a.eta;
       f32_tile_through_lds<WB, WB, W_NW, f32x4, TM, TN, 2, true>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
@@ -502,7 +532,7 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
     }
   };
   // (the loads of dz run over whole strips, the results end at V)
-  gemm_dtl_body<WB, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, 32ll * P, a.xw + (int64_t)k0 * 32 * 32, 32, 32ll * P, Vp, d,
+  gemm_dtl_body<WB, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, bs, a.xw + (int64_t)k0 * 32 * 32, 32, bs, Vp, d,
                                                              (k1 - k0) * 32, bm, bn, Epi{}, nullptr, 0, own);
 }
 template <int KIND>
@@ -517,13 +547,12 @@ __global__ __launch_bounds__(512, 2) void both_grads_kernel(GradArgs a) {
 // fp32 sums of stretches or pieces -> dw, or the update
 __global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __restrict__ sums, int S, Rows rows, int pieces, int64_t n,
                                                                uint16_t* __restrict__ dw, const float* __restrict__ master, float* __restrict__ master_out,
-                                                               uint16_t* __restrict__ version, float eta) {
+                                                               uint16_t* __restrict__ version, float scale, float eta) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
   int parts = 1;
   if (pieces == 1) {
-    const int M = rows_of(rows);
-    parts = row_stretches(S, div_up(M > 0 ? M : 1, 32));
+    parts = row_stretches(S, row_tiles(rows, rows_of(rows)));
   }
   f32x4 v[2] = {reinterpret_cast<const f32x4*>(sums + i)[0], reinterpret_cast<const f32x4*>(sums + i)[1]};
   for (int s = 1; s < parts; ++s) {
@@ -531,6 +560,7 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __re
     v[0] += q[0]; v[1] += q[1];
   }
   if (dw) {
+    v[0] *= scale; v[1] *= scale;
     *reinterpret_cast<u32x4*>(dw + i) = f32_to_bf16x8(v);
     return;
   }
@@ -585,7 +615,8 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   const int64_t P = tiles((T + q.pieces - 1) / q.pieces);
   q.pieces = (int)((T + P - 1) / P);
   q.P = (int)P;
-  q.few = q.pieces == 1 && T <= kFewRows;
+  q.few = q.pieces == 1 && T <= kFewRows && 2 * P * q.Vp < (1ll << 31);   // (offsets, with dz in two parts)
+  q.R = q.few && grads ? 2 * q.P : q.P;
   size_t at = 0;
   q.count = q.pos = q.idx = q.lab = q.xw = q.info = q.tail = q.e = q.part = q.acc = 0;
   auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
@@ -593,15 +624,15 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   if (!q.few) { q.count = take(4); q.pos = take(4 * all); q.idx = take(4 * all); q.lab = take(4 * all); }
   q.target = take(4 * P);
   q.stat = take((size_t)8 * (q.Vp / STRIP) * P);
-  if (!q.few || grads) q.xw = take((size_t)2 * all * d);
+  if (!q.few || grads) q.xw = take((size_t)2 * q.pieces * q.R * d);
   if (grads) {
     q.info = take(sizeof(RowInfo) * P);
     q.tail = take((size_t)2 * 64 * ldw);
-    q.e = take((size_t)2 * P * q.Vp);
+    q.e = take((size_t)2 * q.R * q.Vp);
     const int most_rows = q.T < q.P ? q.T : q.P;
     q.dx = cut_form(most_rows, q.d, q.Vp / 32, true);
     q.part = take((size_t)div_up(most_rows, q.dx.tile) * q.dx.S * q.dx.tile * q.d * 4);
-    q.S_w = q.pieces > 1 ? 1 : cut_form(q.V, q.d, q.P / 32, false).S;
+    q.S_w = q.pieces > 1 ? 1 : cut_form(q.V, q.d, q.R / 32, false).S;
     q.acc = q.pieces > 1 || q.S_w > 1 ? take((size_t)4 * q.S_w * V * d) : 0;
   }
   q.bytes = at;
@@ -624,7 +655,8 @@ Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
     r.count = (const int*)(work + q.count); r.lab = (const int*)(work + q.lab); r.idx = (const int*)(work + q.idx); r.pos = (const int*)(work + q.pos);
   }
   r.label = a.label;
-  r.T = q.T; r.V = q.V; r.p = p; r.P = q.P;
+  r.T = q.T; r.V = q.V; r.p = p; r.P = q.P; r.R = q.R;
+  r.twice = q.few && a.master ? 1 : 0;
   return r;
 }
 
@@ -633,7 +665,7 @@ rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const 
   const uint16_t* w = (const uint16_t*)a.w;
   const uint16_t* x = q.few ? (const uint16_t*)a.x : (const uint16_t*)(work + q.xw) + (int64_t)rows.p * q.P * q.d;
   const int64_t ldx = q.few ? a.ldx : 32, x_bs = q.few ? 32 : 32ll * q.P;
-  const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), q.P, q.V, q.Vp};
+  const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), q.P, q.R, q.V, q.Vp};
   const int most = q.T < q.P ? q.T : q.P;
   if (big_tiles(most, q.Vp)) {
     constexpr auto kern = logits_kernel<256, 256, 4, 8, STORE>;
@@ -664,7 +696,8 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
   g.dx_grid = a.dx ? g.tiles_m * div_up(q.d, q.dx.tile) * q.dx.S : 0;
   g.tail = (const uint16_t*)(work + q.tail); g.part = (float*)(work + q.part);
   g.S_w = q.S_w; g.sums = (float*)(work + q.acc);
-  g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version; g.eta = a.eta;
+  g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version;
+  g.scale = a.scale; g.eta = a.eta * a.scale;
   const int w_grid = div_up(q.V, WB) * div_up(q.d, WB) * (KIND == 2 ? q.S_w : 1);
   // together, but for an update in place: dx reads the weights that it overwrites
   const bool both = KIND >= 0 && a.dx && q.dx.tile == 128 &&
@@ -681,7 +714,7 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
   const int64_t chunks = (int64_t)q.T * (q.d / 8);
   auto join = [&](auto k, int lanes) {
     hipLaunchKernelGGL(k, dim3((unsigned)((chunks * lanes + 255) / 256)), dim3(256), 0, st, g.part, rows, q.d, q.Vp / 32, q.dx.tile, g.S_dx, g.tiles_m,
-                       (uint16_t*)a.dx, a.lddx);
+                       a.scale, (uint16_t*)a.dx, a.lddx);
   };
   if (g.S_dx > 8) join(input_grad_join_kernel<8>, 8);
   else join(input_grad_join_kernel<1>, 1);
@@ -725,7 +758,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
     else RV_TRY(launch_logits<false>(q, work, a, rows, st));
     RowInfo* info = grads ? (RowInfo*)(work + q.info) : nullptr;
     hipLaunchKernelGGL(join_kernel, dim3(div_up(most, 16)), dim3(1024), 0, st, (const float2*)(work + q.stat), (const float*)(work + q.target), rows, strips,
-                       a.scale, a.row_scale, a.loss, a.lse, info);
+                       a.row_scale, a.loss, a.lse, info);
     RV_TRY(rv_launch_status());
     if (!grads) continue;
     // strips a block takes one after the other: up to 8, fewer where that leaves fewer than 2048 blocks
@@ -744,7 +777,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   if (grads && (a.dw || update) && cut) {
     const int64_t n = (int64_t)q.V * q.d;
     hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, (const float*)(work + q.acc), q.S_w,
-                       rows_at(q, work, a, 0), q.pieces, n, (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.eta);
+                       rows_at(q, work, a, 0), q.pieces, n, (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.scale, a.eta * a.scale);
     RV_TRY(rv_launch_status());
   }
   return RV_OK;

@@ -140,6 +140,32 @@ def test_update_and_row_weights(T, d, V):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("T,d,V", [(1, 64, 1000), (5, 192, 333), (200, 128, 700)])
+def test_update_of_few_rows_is_as_exact_as_its_master(T, d, V):
+    """A step as large as the weights.  Of dz the label's entry has 16 bits (two roundings to bf16, 2^-16), the others those of their
+    exponential, 2^-11; `slack` (see _check) moves both."""
+    x, w, label, master = _inputs(19, T, d, V, 0.2 if T > 1 else 0.0)
+    _, _, new, _ = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.37, master=master.cuda(), eta=2.0)
+    loss, lse, dz, zerr, x64, w64, y, takes = _reference(x, w, label, torch.full((T,), 0.37))
+    slack = 2 * zerr + (80 + V / 64) * 2.0 ** -24 + 2.0 ** -22 * float(lse.abs().max())
+    off = dz.abs() * (2.0 ** -11 + 2.0 ** -16 + 2 * slack) + 2.0 ** -40
+    rows = torch.arange(T)
+    off[rows, y] = dz[rows, y].abs() * 2.0 ** -16 + torch.where(takes, 0.37, 0.0) * slack
+    step = dz.T @ x64
+    bound = 2.0 * ((off + dz.abs() * (T + 8) * 2.0 ** -23).T @ x64.abs()) + 2.0 ** -22 * (master.double().abs() + 2.0 * step.abs())
+    assert bool(((new.cpu().double() - (master.double() - 2.0 * step)).abs() <= bound).all())
+
+
+def test_a_scale_is_no_bias():
+    """1 / 7783 rounded to bf16 is off by 2^-9: a gradient that carried the rounding of its scale would be off by that everywhere."""
+    x, w, label, _ = _inputs(21, 300, 128, 2000)
+    _, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=1.0)
+    _, dx2, dw2 = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=1.0 / 7783)
+    for a, b in ((dx, dx2), (dw, dw2)):
+        a, b = a.double().cpu(), b.double().cpu() * 7783
+        assert abs(float((a * b).sum() / (a * a).sum()) - 1.0) < 2.0 ** -12      # (the roundings of 10^5 results, averaged)
+
+
 def test_no_row_takes_part():
     T, d, V = 70, 128, 300
     x, w, label, master = _inputs(3, T, d, V, 1.0)
