@@ -283,9 +283,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
   const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
   const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
 
-  Frag qf[DH / 16];
-  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
-  settle(qf);
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
@@ -297,6 +294,12 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
     loads.keys(K, a.ldk, t * TILE, n, to);
     loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  Frag qf[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
+  settle(qf);
   auto tile = [&](int k0, const char* Ks) {
     const char* Vs = Ks + kTileBytes<DH>;
     f32x16 s[2];
@@ -318,9 +321,6 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
           o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DH>(Vs, sub * 32 + ks * 16, dt * 32), p, o[dt], 0, 0, 0);
       }
   };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
   for (int t = t0; t < t1; ++t) {
     if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
     else wait_loads<0>();
@@ -359,9 +359,6 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
   char* ring = dtl_smem + wave * kTokenRing<DH>;
   const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
   const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
-  Frag qf[DH / 16];
-  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, r < a.R ? r : a.R - 1, a.ldq));
-  settle(qf);
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
@@ -377,6 +374,9 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
     if (i < mine) issue(i);
+  Frag qf[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, r < a.R ? r : a.R - 1, a.ldq));
+  settle(qf);
   for (int i = 0; i < mine; ++i) {
     // the slot that is filled next was read a tile ago; its reads have come back before the load goes out
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
@@ -533,12 +533,6 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
   const int rc = r < a.R ? r : a.R - 1;
   const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
   const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
-  Frag qf[DH / 16], of[DH / 16];
-  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
-  load_owned<DH>(of, a.dout + row_at<DH>(a, w.b, w.h, rc, a.lddo));
-  float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
-  settle(qf); settle(of);
-  asm volatile("" : "+v"(lse), "+v"(D));
   f32x16 dq[DH / 32];
   clear(dq);
   const TileLoads<DH, NW> loads(wave);
@@ -548,6 +542,15 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
     loads.keys(K, a.ldk, t * TILE, n, to);
     loads.keys(V, a.ldv, t * TILE, n, to + kTileBytes<DH>);
   };
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
+  Frag qf[DH / 16], of[DH / 16];
+  load_owned<DH>(qf, a.q + row_at<DH>(a, w.b, w.h, rc, a.ldq));
+  load_owned<DH>(of, a.dout + row_at<DH>(a, w.b, w.h, rc, a.lddo));
+  float lse = a.stat_lse[(int64_t)w.unit * a.Rp + rc], D = a.stat_d[(int64_t)w.unit * a.Rp + rc];
+  settle(qf); settle(of);
+  asm volatile("" : "+v"(lse), "+v"(D));
   auto tile = [&](int first, const char* Ks) {
     const char* Vs = Ks + kTileBytes<DH>;
 #pragma unroll(DH == 128 ? 1 : 2)
@@ -578,9 +581,6 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
       }
     }
   };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
   for (int t = t0; t < t1; ++t) {
     if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
     else wait_loads<0>();
@@ -615,6 +615,17 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
   Frag kf[DH / 16], vf[DH / 16];
   f32x16 dk[DH / 32], dv[DH / 32];
   clear(dk); clear(dv);
+  const TileLoads<DH, NW> loads(wave);
+  const float* stat = (wave & 1 ? a.stat_d : a.stat_lse) + (int64_t)w.unit * a.Rp;   // (even waves bring the lse, odd ones D)
+  auto issue = [&](int t) {
+    char* to = smem + (t - t0) % NS * SLOT;
+    loads.rows(a, w.b, w.h, a.q, a.ldq, a.dout, a.lddo, t * TILE, to, to + kTileBytes<DH>);
+    load_floats(stat + t * TILE, to + 2 * kTileBytes<DH> + (wave & 1) * TILE * 4);
+  };
+  // One slot: the next tile is asked for when everyone has left this one.  The first tile goes out ahead of the wave's own keys: with few
+  // rows a workgroup is one chain of round trips.
+  static_assert(NS == 1 || NS == 2, "slots");
+  if (t0 < t1) issue(t0);
   if (active) {
     const int jc = j < n ? j : n - 1;
     load_owned<DH>(kf, a.k + ((int64_t)w.b * a.Sk + jc) * a.ldk + w.h * DH);
@@ -625,24 +636,7 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
       for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
     }
   }
-  const TileLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * TileLoads<DH, NW>::N + 1;
-  const float* stat = (wave & 1 ? a.stat_d : a.stat_lse) + (int64_t)w.unit * a.Rp;   // (even waves bring the lse, odd ones D)
-  auto issue = [&](int t) {
-    char* to = smem + (t - t0) % NS * SLOT;
-    loads.rows(a, w.b, w.h, a.q, a.ldq, a.dout, a.lddo, t * TILE, to, to + kTileBytes<DH>);
-    load_floats(stat + t * TILE, to + 2 * kTileBytes<DH> + (wave & 1) * TILE * 4);
-  };
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i)
-    if (t0 + i < t1) issue(t0 + i);
-  for (int t = t0; t < t1; ++t) {
-    if (t + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
-    else wait_loads<0>();
-    __syncthreads();
-    if (t + NS - 1 < t1) issue(t + NS - 1);
-    if (!active) continue;
-    const char* Qs = smem + (t - t0) % NS * SLOT;
+  auto tile = [&](const char* Qs) {
     const char* Os = Qs + kTileBytes<DH>;
     const float* lse = reinterpret_cast<const float*>(Os + kTileBytes<DH>);
 #pragma unroll(DH == 128 ? 1 : 2)
@@ -681,6 +675,16 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
         }
       }
     }
+  };
+  for (int t = t0; t < t1; ++t) {
+    wait_loads<0>();                                       // (at most one tile is on the way)
+    __syncthreads();
+    if (NS == 2 && t + 1 < t1) issue(t + 1);
+    if (active) tile(smem + (t - t0) % NS * SLOT);
+    if (NS == 1 && t + 1 < t1) {
+      __syncthreads();
+      issue(t + 1);
+    }
   }
   if (j >= a.Sk) return;
   if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
@@ -693,13 +697,14 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
     store_owned32<DH>(dv, to + DH);
   }
 }
-template <int DH, int NW, int NS> constexpr int kBwdLds = NS * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
+template <int DH, int NW, int NS_KV> constexpr int kKvLds = NS_KV * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
+template <int DH, int NW, int NS_KV> constexpr int kBwdLds = kKvLds<DH, NW, NS_KV> > 4 * kTileBytes<DH> ? kKvLds<DH, NW, NS_KV> : 4 * kTileBytes<DH>;
 // Both in one launch, the longer workgroups (dK and dV: four products to dQ's three) first: where neither fills the chip by itself, and for
 // the last workgroups of the one to run beside the first of the other.
-template <int DH, int NW, int NS>
+template <int DH, int NW, int NS_KV>
 __global__ __launch_bounds__(64 * NW, DH == 128 ? 2 : 3) void cross_bwd_kernel(CrossArgs a) {
-  if ((int)blockIdx.x < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, blockIdx.x, a.kv_grid);
-  else bwd_q_body<DH, NW, NS>(a, blockIdx.x - a.kv_grid, gridDim.x - a.kv_grid);
+  if ((int)blockIdx.x < a.kv_grid) bwd_kv_body<DH, NW, NS_KV>(a, blockIdx.x, a.kv_grid);
+  else bwd_q_body<DH, NW, 2>(a, blockIdx.x - a.kv_grid, gridDim.x - a.kv_grid);
 }
 // parts -> dq (KV false), or dk and dv
 template <int DH, bool KV>
@@ -812,7 +817,7 @@ rv_status forward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   else RV_TRY((launch<cross_join_kernel<DH, 1>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
   return RV_OK;
 }
-template <int DH, int NW>
+template <int DH, int NW, int NS_KV>
 rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
@@ -820,7 +825,7 @@ rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) 
   const int64_t kv = deal(a.bkv, a, up(a.Sk, OWN * NW), p.kv_parts), q = deal(a.bq, a, up(a.R, OWN * NW), p.q_parts);
   if (kv > 0x3FFFFFFF || q > 0x3FFFFFFF) return RV_E_INVAL;
   a.kv_grid = (int)kv;
-  RV_TRY((launch<cross_bwd_kernel<DH, NW, 2>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, 2>, st)));
+  RV_TRY((launch<cross_bwd_kernel<DH, NW, NS_KV>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, NS_KV>, st)));
   if (p.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
   if (p.kv_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
   return RV_OK;
@@ -865,8 +870,11 @@ extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const 
   a.o = (const uint16_t*)out; a.ldo = ldo; a.dout = (const uint16_t*)dout; a.lddo = lddo; a.lse2 = (float*)lse2;
   a.dq = (uint16_t*)dq; a.lddq = lddq; a.dk = (uint16_t*)dk; a.lddk = lddk; a.dv = (uint16_t*)dv; a.lddv = lddv;
   const hipStream_t st = (hipStream_t)stream;
-  // Heads of 128: two waves to a SIMD either way (registers); eight share a streamed tile, 736 -> 775 TFLOP/s over 4096 x 4096 tokens, but for
-  // rows or keys that four waves hold the others would idle.  Heads of 64 are faster with four: three waves to a SIMD, 770 / 701.
-  if (d_head == 64) return backward<64, 4>(a, p, (char*)work, st);
-  return p.R > 4 * OWN && Sk > 4 * OWN ? backward<128, 8>(a, p, (char*)work, st) : backward<128, 4>(a, p, (char*)work, st);
+  // Heads of 128: two waves to a SIMD either way (registers).  Eight that share two slots are the faster where there are rounds of them,
+  // two workgroups of four with a slot each where one is short of work or ends early.  us, eight / four: 4 x 4096 x 4096 tokens, 16 heads (2048
+  // workgroups of eight) 1709 / 1838; 162 tokens of 32 heads over 16 and up to 6893 keys (1120) 224 / 203; 1024 of 16 over 4 and up to 2048
+  // (512) 215 / 198; 48 rows over up to 9981 keys 168 / 153.  Heads of 64 are faster with four: three waves to a SIMD, 4 x 4096 x 4096 892 / 979.
+  if (d_head == 64) return backward<64, 4, 2>(a, p, (char*)work, st);
+  const int64_t eights = (int64_t)B * n_kv_heads * (up(Sk, 8 * OWN) * p.kv_parts + up(p.R, 8 * OWN) * p.q_parts);
+  return p.R > 4 * OWN && Sk > 4 * OWN && eights >= 1536 ? backward<128, 8, 2>(a, p, (char*)work, st) : backward<128, 4, 1>(a, p, (char*)work, st);
 }

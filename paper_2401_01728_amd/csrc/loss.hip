@@ -656,7 +656,7 @@ Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
   }
   r.label = a.label;
   r.T = q.T; r.V = q.V; r.p = p; r.P = q.P; r.R = q.R;
-  r.twice = q.few && a.master ? 1 : 0;
+  r.twice = q.few && (a.master || (a.dw && q.T <= 64)) ? 1 : 0;
   return r;
 }
 

@@ -33,7 +33,7 @@ def _reference(q, k, v, do, n, H, Hkv, o_given=None):
     B, Sq, _ = q.shape
     Sk = k.shape[1]
     dh = q.shape[2] // H
-    f64 = dict(dtype=torch.float64)
+    f64 = dict(dtype=torch.float64, device=q.device)
     out, lse2 = torch.zeros(q.shape, **f64), torch.full((B, H, Sq), -math.inf, **f64)
     dq, dk, dv = torch.zeros(q.shape, **f64), torch.zeros(k.shape, **f64), torch.zeros(k.shape, **f64)
     e_out, e_dq, e_dk, e_dv = (torch.zeros_like(t) for t in (out, dq, dk, dv))
@@ -67,7 +67,7 @@ def _reference(q, k, v, do, n, H, Hkv, o_given=None):
 
 
 def _near(got, ref, bound):
-    got = got.cpu().double()
+    got = got.to(ref.device).double()
     assert bool(torch.isfinite(got).all())
     over = (got - ref).abs() / bound
     assert bool((over <= 1.0).all()), "off by %.3g of the bound at %s" % (float(over.max()), int(over.argmax()))
@@ -108,6 +108,34 @@ def test_forward_and_backward(B, Sq, Sk, H, Hkv, dh):
 def test_lengths(B, Sq, Sk, H, Hkv, dh, klen):
     """Sequences of their own lengths, none among them; what lies behind is not a number."""
     _check(B, Sq, Sk, H, Hkv, dh, klen, seed=1)
+
+
+# grids of many workgroups: eight waves to one in the backward of heads of 128; parts on both sides; rows and keys that end inside all blocks
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh,klen", [
+    (8, 700, 700, 32, 32, 128, None), (9, 333, 1001, 40, 20, 128, [1001, 0, 1, 63, 500, 1000, 777, 64, 65]), (4, 513, 1030, 24, 12, 64, [1030, 1, 700, 0])])
+def test_many_workgroups(B, Sq, Sk, H, Hkv, dh, klen):
+    q, k, v, do, n = _inputs(6, B, Sq, Sk, H, Hkv, dh, klen)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    length = torch.tensor(klen, dtype=torch.int32).cuda() if klen is not None else None
+    got_out, got_lse = kernels.cross_attention_fwd(q, k, v, H, Hkv, length)
+    _near(got_out, out, e_out)
+    for a, ref, bound in zip(kernels.cross_attention_bwd(q, k, v, got_out, do, got_lse, H, Hkv, length), (dq, dk, dv), (e_dq, e_dk, e_dv)):
+        _near(a, ref, bound)
+
+
+def test_same_bits_every_time():
+    q, k, v, do, _ = _inputs(7, 3, 300, 500, 8, 4, 128, None)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    length = torch.tensor([500, 123, 311], dtype=torch.int32).cuda()
+    ref = None
+    for _ in range(4):
+        o = kernels.cross_attention_fwd(q, k, v, 8, 4, length)
+        got = (*o, *kernels.cross_attention_bwd(q, k, v, o[0], do, o[1], 8, 4, length))
+        if ref is not None:
+            for a, b in zip(got, ref):
+                assert torch.equal(a, b)
+        ref = got
 
 
 def test_strides_and_what_lies_beside():
