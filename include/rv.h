@@ -260,7 +260,7 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
 /*
  * The loss at the end of a chain of peers, and the gradient that its backward begins with: softmax cross entropy of
  * every token against a vocabulary, over the head's product z = x w^T.
- *   x         device bf16 [T, d], rows ldx elements apart: the last block's output.  d a multiple of 64, up to 16384.
+ *   x         device bf16 [T, d], rows ldx elements apart: the last block's output.  1 <= T <= 2^20, d a multiple of 64, up to 16384.
  *   w         device bf16 [V, d], rows ldw elements apart, one per token of the vocabulary (as an embedding that is
  *             shared with the input has them).  1 <= V <= 2^24, any number; V * ldw below 2^31.
  *   label     device int64 [T].  A label outside [0, V) takes its row out of the batch (prompts, padding): its loss, lse
@@ -280,7 +280,7 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).
  *             Nothing in it has to be kept between calls; calls that may run at one time need one each, and so do graphs
  *             that may be replayed at one time.
- * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8, ldx at most 2^22.  Outputs must not share memory
+ * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8, ldx and ldw at most 2^20.  Outputs must not share memory
  * with inputs or one another but as said.  Allocates nothing; RV_E_INVAL, before anything is enqueued, on what is not covered.
  */
 typedef struct {

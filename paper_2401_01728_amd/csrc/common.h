@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <stddef.h>
+#include <atomic>
 #include "../../include/rv.h"
 
 #define RV_HIP_TRY(expr)                         \
@@ -19,6 +20,20 @@
 
 static inline rv_status rv_launch_status() {
   return hipGetLastError() == hipSuccess ? RV_OK : RV_E_DEVICE;
+}
+
+// Lets Kern be launched with `bytes` of dynamic LDS on the current device: asked for once per device (the same bytes in every call).
+template <auto Kern>
+static inline hipError_t rv_allow_lds(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+  const hipError_t set = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (set == hipSuccess) done.fetch_or(bit, std::memory_order_release);
+  return set;
 }
 
 // fp32 -> bf16 bits, round to nearest even (finite inputs).

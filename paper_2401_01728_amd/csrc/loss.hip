@@ -83,10 +83,10 @@ __device__ __forceinline__ void copy_tail(const uint16_t* __restrict__ w, int64_
 }
 
 // ---- rows that take part ----------------------------------------------------------------------
-// A block takes `per` (up to 64) consecutive rows; where they go follows from the number of labels before them that take part, which
-// it counts itself: T labels are 8 T bytes out of L2, at most a thousand blocks do it, and a scan of its own would be a launch more.
+// A block takes `per` consecutive rows, 64 at a time; where they go follows from the number of labels before them that take part, which
+// it counts itself: at most a thousand blocks do it, 8 T bytes each out of L2, and a scan of its own would be a launch more.
 // pos[t] = place among the rows kept or -1; idx, lab: the other way round.  The block of the last rows leaves their number.
-// Behind the row blocks: the tail of W.
+// Behind the row blocks: the tail of W.  Bound by memory: 8192 rows of d 2048 18 us, 3.6 TB/s.
 __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict__ x, int64_t ldx, const int64_t* __restrict__ label, int T,
                                                      int d, int V, int P, int per, int* __restrict__ count, int* __restrict__ pos,
                                                      int* __restrict__ idx, int* __restrict__ lab, uint16_t* __restrict__ xw,
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict_
     return;
   }
   __shared__ int part[4], place[64];
-  const int t0 = blockIdx.x * per, rows = T - t0 < per ? T - t0 : per;
+  const int t0 = blockIdx.x * per, t1 = T - t0 < per ? T : t0 + per;
   auto takes = [&](int64_t y) { return y >= 0 && y < V; };
   int before = 0;
   for (int t = tid; t < t0; t += 8 * 256) {   // (eight on the way at a time)
@@ -112,29 +112,34 @@ __global__ __launch_bounds__(256) void gather_kernel(const uint16_t* __restrict_
   for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o, 64);
   if (l == 0) part[tid >> 6] = before;
   __syncthreads();
-  if (tid < 64) {
-    before = part[0] + part[1] + part[2] + part[3];
-    const int64_t y = l < rows ? label[t0 + l] : -1;
-    const bool in = takes(y);
-    const uint64_t all = __builtin_amdgcn_ballot_w64(in);
-    const int j = before + __popcll(all & ((1ull << l) - 1));
-    place[l] = in ? j : -1;
-    if (l < rows) {
-      pos[t0 + l] = in ? j : -1;
-      if (in) { idx[j] = t0 + l; lab[j] = (int)y; }
-      else { loss[t0 + l] = 0.f; if (lse) lse[t0 + l] = 0.f; }
+  before = part[0] + part[1] + part[2] + part[3];
+  for (int first = t0; first < t1; first += 64) {
+    const int rows = t1 - first < 64 ? t1 - first : 64;
+    if (tid < 64) {
+      const int64_t y = l < rows ? label[first + l] : -1;
+      const bool in = takes(y);
+      const uint64_t all = __builtin_amdgcn_ballot_w64(in);
+      const int j = before + __popcll(all & ((1ull << l) - 1));
+      place[l] = in ? j : -1;
+      if (l < rows) {
+        pos[first + l] = in ? j : -1;
+        if (in) { idx[j] = first + l; lab[j] = (int)y; }
+        else { loss[first + l] = 0.f; if (lse) lse[first + l] = 0.f; }
+      }
+      before += __popcll(all);
+      if (l == 0 && first + rows == T) *count = before;
     }
-    if (l == 0 && t0 + rows == T) *count = before + __popcll(all);
-  }
-  __syncthreads();
-  const int chunks = rows * (d / 8);
-  for (int i = tid; i < chunks; i += 256) {
-    // four chunks of a block of 32 columns in neighbouring lanes, then the next row: what is written is runs of 64 bytes a row
-    const int q = i & 3, r = (i >> 2) % rows, cb = (i >> 2) / rows, j = place[r];
-    if (j < 0) continue;
-    const int p = j / P, jr = j - p * P;
-    const u32x4 u = *reinterpret_cast<const u32x4*>(x + (int64_t)(t0 + r) * ldx + cb * 32 + q * 8);
-    *reinterpret_cast<u32x4*>(xw + (int64_t)p * P * d + (int64_t)cb * 32 * P + 32 * jr + q * 8) = u;
+    __syncthreads();
+    const int chunks = rows * (d / 8);
+    for (int i = tid; i < chunks; i += 256) {
+      // four chunks of a block of 32 columns in neighbouring lanes, then the next row: what is written is runs of 64 bytes a row
+      const int q = i & 3, r = (i >> 2) % rows, cb = (i >> 2) / rows, j = place[r];
+      if (j < 0) continue;
+      const int p = j / P, jr = j - p * P;
+      const u32x4 u = *reinterpret_cast<const u32x4*>(x + (int64_t)(first + r) * ldx + cb * 32 + q * 8);
+      *reinterpret_cast<u32x4*>(xw + (int64_t)p * P * d + (int64_t)cb * 32 * P + 32 * jr + q * 8) = u;
+    }
+    __syncthreads();
   }
 }
 
@@ -154,6 +159,8 @@ __device__ __forceinline__ void band_tile(int i, int vm, int vn, int& bm, int& b
 }
 
 // ---- the logits' product ----------------------------------------------------------------------
+// Bound by the matrix cores at the board's power cap: 7783 rows, V 128000, d 2048 3.35 ms, 1.22 PFLOP/s (a library product of 8192^3 1.37); of that
+// 0.35 ms are the epilogue, exponentials and stores about half each.  A tile of 128x256, two to a CU, whose epilogues run beside walks: 3.8 ms.
 // (The tiles are dealt out over the tile rows that are there: a map over the rows of all tokens would leave whole XCDs without work where half
 // of the rows are out.)
 struct LogitsOut {
@@ -279,7 +286,8 @@ __global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __re
 }
 
 // ---- strips joined to rows ----------------------------------------------------------------------
-// 16 rows to a block, 64 lanes to a row: a strip's pairs of 16 rows are one line.
+// 16 rows to a block, 64 lanes to a row: a strip's pairs of 16 rows are one line.  Bound by memory and, with few rows, by its chain of round
+// trips: 7783 rows of V 128000 40 us, 3.1 TB/s; one row of V 32000 4 us.
 __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ stat, const float* __restrict__ target, Rows rows, int strips,
                                                     const float* __restrict__ row_scale, float* __restrict__ loss, float* __restrict__ lse,
                                                     RowInfo* __restrict__ info) {
@@ -320,6 +328,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
 }
 
 // ---- e -> dz, in place ----------------------------------------------------------------------
+// Bound by memory: 7783 rows of V 128000 780 us, 5.1 TB/s, a large copy's rate.
 // 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those from the
 // last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
 // Two parts (`twice`, few rows and an update): what dz loses to bf16 is rounded itself and stands, with the same rows of x, behind the rows, so that
@@ -426,7 +435,8 @@ struct GradArgs {
   float scale, eta;                       // eta: times scale
 };
 // BM 256: tiles of 256x256, eight waves, in order of k; 128: of 128x128, the walk split over two groups of four waves.  The last k-tiles, which
-// end behind the last row of W, come from its copy with zeros behind (there is nothing behind W that could be read).
+// end behind the last row of W, come from its copy with zeros behind (there is nothing behind W that could be read).  7783 rows, V 128000,
+// d 2048 3.0 ms, 1.36 PFLOP/s; 2048 rows, V 50257, d 1024, in eight stretches, 0.18 ms, 1.15.
 template <int BM>
 __device__ __forceinline__ void input_grad_body(const GradArgs& a, int id) {
   const int d = a.d, V = a.rows.V, M = rows_of(a.rows);
@@ -493,6 +503,8 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
 }
 
 // ---- dW ----------------------------------------------------------------------
+// 256x256 tiles, the contraction over the rows: 7783 rows, V 128000, d 2048 3.0 ms, 1.36 PFLOP/s; 2048, V 50257, d 1024 0.22 ms, 0.96 (788 tiles are
+// three rounds of the CUs and a twelfth); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update 74 us with dx, 4.7 TB/s.
 // KIND 0: bf16 dw.  1: the update of Eq. 2 on an fp32 master (w' = w - eta dW, one fused multiply-add) and its bf16 version.
 // 2: fp32 sums of one of S stretches of the rows (few tiles), or of the first piece.  3: added to those of the pieces before.
 constexpr int WB = 256, W_NS = 4, W_NW = 8;
@@ -603,7 +615,7 @@ CutForm cut_form(int M, int N, int nk, bool small) {
 }
 
 bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t rows, bool grads) {
-  if (T < 1 || T > (1 << 24) || d < 64 || d % 64 || d > 16384 || V < 1 || V > (1 << 24) || ldw < d || ldw % 8 || rows < 0) return false;
+  if (T < 1 || T > (1 << 20) || d < 64 || d % 64 || d > 16384 || V < 1 || V > (1 << 24) || ldw < d || ldw % 8 || ldw > (1 << 20) || rows < 0) return false;
   if (V * ldw >= (1ll << 31)) return false;       // offsets in the logits' product
   q.T = (int)T; q.d = (int)d; q.V = (int)V; q.Vp = round_up((int)V, STRIP); q.grads = grads; q.ldw = ldw;
   // pieces of nearly the same size, of whole tiles of the logits' product: of 128 rows where that is all, else of 256
@@ -639,11 +651,6 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   return true;
 }
 
-template <auto Kern>
-hipError_t allow_lds(int bytes) {
-  static const hipError_t done = hipFuncSetAttribute((const void*)Kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  return done;
-}
 constexpr int kBigLds = 4 * 2 * dtl_tile_bytes(256, 32), kMidLds = 4 * 2 * dtl_tile_bytes(128, 32), kSplitLds = split_lds<128, 128, 2, 4>();
 constexpr int kWeightLds = WB * stage_pitch(WB) > upd_image_bytes(WB, WB) ? WB * stage_pitch(WB) : upd_image_bytes(WB, WB);
 constexpr int kBothLds = kSplitLds > kWeightLds ? kSplitLds : kWeightLds;
@@ -669,11 +676,11 @@ rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const 
   const int most = q.T < q.P ? q.T : q.P;
   if (big_tiles(most, q.Vp)) {
     constexpr auto kern = logits_kernel<256, 256, 4, 8, STORE>;
-    if (allow_lds<kern>(kBigLds) != hipSuccess) return RV_E_DEVICE;
+    if (rv_allow_lds<kern>(kBigLds) != hipSuccess) return RV_E_DEVICE;
     hipLaunchKernelGGL(kern, dim3(div_up(most, 256) * div_up(q.Vp, 256)), dim3(512), kBigLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
   } else {
     constexpr auto kern = logits_kernel<128, 128, 4, 4, STORE>;
-    if (allow_lds<kern>(kMidLds) != hipSuccess) return RV_E_DEVICE;
+    if (rv_allow_lds<kern>(kMidLds) != hipSuccess) return RV_E_DEVICE;
     hipLaunchKernelGGL(kern, dim3(div_up(most, 128) * div_up(q.Vp, 128)), dim3(256), kMidLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
   }
   return rv_launch_status();
@@ -681,7 +688,7 @@ rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const 
 
 template <auto Kern>
 rv_status launch_512(const GradArgs& g, int grid, int lds, hipStream_t st) {
-  if (allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
+  if (rv_allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
   hipLaunchKernelGGL(Kern, dim3(grid), dim3(512), lds, st, g);
   return rv_launch_status();
 }
@@ -727,7 +734,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   Plan q;
   if (!make_plan(q, a.T, a.d, a.V, a.ldw, a.rows, grads)) return RV_E_INVAL;
   if (!a.x || !a.w || !a.label || !a.loss || !a.work || a.work_bytes < q.bytes) return RV_E_INVAL;
-  if (a.ldx < a.d || a.ldx % 8 || a.ldx > (1 << 22) || misaligned(a.x, 16) || misaligned(a.w, 16) || misaligned(a.work, 256) || misaligned(a.label, 8) ||
+  if (a.ldx < a.d || a.ldx % 8 || a.ldx > (1 << 20) || misaligned(a.x, 16) || misaligned(a.w, 16) || misaligned(a.work, 256) || misaligned(a.label, 8) ||
       misaligned(a.loss, 4) || misaligned(a.lse, 4) || misaligned(a.row_scale, 4)) return RV_E_INVAL;
   const bool update = grads && a.master;
   if (grads) {
@@ -743,7 +750,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   const int tail_rows = grads ? q.Vp - q.V / 32 * 32 : 0;
   if (!q.few) {
     int per = 4;
-    while (per < 64 && per * 1024 < q.T) per *= 2;
+    while (per * 1024 < q.T) per *= 2;
     const int row_blocks = div_up(q.T, per);
     hipLaunchKernelGGL(gather_kernel, dim3(row_blocks + tail_rows), dim3(256), 0, st, (const uint16_t*)a.x, a.ldx, a.label, q.T, q.d, q.V, q.P, per,
                        (int*)(work + q.count), (int*)(work + q.pos), (int*)(work + q.idx), (int*)(work + q.lab), (uint16_t*)(work + q.xw), a.loss, a.lse, w,

@@ -96,7 +96,8 @@ def test_loss_and_gradients(T, d, V, out):
 
 
 # tiles of 256 for dx (many rows of a wide state), half of the rows out; rows that a workgroup's label count walks over in more than one turn
-@pytest.mark.parametrize("T,d,V,out", [(4096, 4096, 1000, 0.5), (2048, 8192, 600, 0.0), (20000, 64, 100, 0.3)])
+@pytest.mark.parametrize("T,d,V,out", [(4096, 4096, 1000, 0.5), (2048, 8192, 600, 0.0), (20000, 64, 100, 0.3),
+                                         (140001, 64, 40, 0.3)])
 def test_many_rows(T, d, V, out):
     x, w, label, master = (t.cuda() for t in _inputs(2, T, d, V, out))
     g = torch.full((T,), 1.0, device="cuda")

@@ -15,10 +15,10 @@ def _work(T=100, d=128, V=1000, ldw=128, rows=0, gradients=1):
 
 def test_sizes():
     assert _lib.lib().rv_loss_work(100, 128, 1000, 128, 0, 1, None) == INVAL
-    for bad in (dict(T=0), dict(T=-1), dict(T=(1 << 24) + 1), dict(d=0), dict(d=32), dict(d=100), dict(d=16448), dict(V=0), dict(V=(1 << 24) + 1),
+    for bad in (dict(T=0), dict(T=-1), dict(T=(1 << 20) + 1), dict(ldw=(1 << 20) + 8, V=10), dict(d=0), dict(d=32), dict(d=100), dict(d=16448), dict(V=0), dict(V=(1 << 24) + 1),
                 dict(ldw=64), dict(ldw=132), dict(rows=-1), dict(V=1 << 24, ldw=128), dict(d=16384, ldw=16384, V=131072)):
         assert _work(**bad)[0] == INVAL, bad
-    for good in (dict(T=1), dict(T=1 << 24, V=1), dict(d=64, ldw=64), dict(d=16384, ldw=16384, V=131071), dict(V=1), dict(V=(1 << 24) - 1, ldw=128, T=64),
+    for good in (dict(T=1), dict(T=1 << 20, V=1), dict(d=64, ldw=64), dict(d=16384, ldw=16384, V=131071), dict(V=1), dict(V=(1 << 24) - 1, ldw=128, T=64),
                  dict(ldw=136), dict(rows=1)):
         st, n = _work(**good)
         assert st == OK and n > 0, good
@@ -46,7 +46,7 @@ def _desc(**change):
 
 @pytest.mark.parametrize("change", [
     dict(x=None), dict(w=None), dict(label=None), dict(loss=None), dict(work=None), dict(work_bytes=0), dict(x=1026), dict(w=2056), dict(label=4100),
-    dict(loss=8194), dict(lse=16386), dict(work=(1 << 20) + 16), dict(ldx=120), dict(ldx=130), dict(ldx=(1 << 22) + 8), dict(ldw=130), dict(ldw=64), dict(row_scale=2),
+    dict(loss=8194), dict(lse=16386), dict(work=(1 << 20) + 16), dict(ldx=120), dict(ldx=130), dict(ldx=(1 << 20) + 8), dict(ldw=130), dict(ldw=64), dict(row_scale=2),
     dict(T=0), dict(d=96), dict(V=0), dict(rows=-5)])
 def test_refused_by_both(change):
     a = _desc(**change)
