@@ -21,8 +21,9 @@
 // memory has a bound that does not grow with T; from the second piece on the weight gradient is added up in fp32.
 //
 // Rows whose label lies outside [0, V) - prompts, padding - take no part: a first kernel gathers the others, in order, into a copy of
-// x without gaps, in blocks of 32 columns (rv_mat), and all kernels behind it go by the number of rows it counted.  So nothing
-// such a row holds (NaN of an unwritten buffer) reaches a product, and a batch that is half prompt costs half.
+// x without gaps, in blocks of 32 columns (rv_mat), and all kernels behind it go by the number of rows it counted.  So a batch that is half
+// prompt costs half.  Up to 256 rows, whose products are bound by the weights, are not gathered: a launch less, and the rows that take no
+// part become zeros where dz and its copy of x are made.  Either way nothing such a row holds (NaN of an unwritten buffer) reaches an output.
 #include <math.h>
 #include "gemm_core.h"
 
@@ -160,7 +161,8 @@ __device__ __forceinline__ void band_tile(int i, int vm, int vn, int& bm, int& b
 
 // ---- the logits' product ----------------------------------------------------------------------
 // Bound by the matrix cores at the board's power cap: 7783 rows, V 128000, d 2048 3.35 ms, 1.22 PFLOP/s (a library product of 8192^3 1.37); of that
-// 0.35 ms are the epilogue, exponentials and stores about half each.  A tile of 128x256, two to a CU, whose epilogues run beside walks: 3.8 ms.
+// 0.35 ms are the epilogue, exponentials and stores about half each.  (Tiles of 128x256, two to a CU, whose epilogues run beside walks: the whole
+// step 11.03 ms to 10.77.)
 // (The tiles are dealt out over the tile rows that are there: a map over the rows of all tokens would leave whole XCDs without work where half
 // of the rows are out.)
 struct LogitsOut {
@@ -329,12 +331,12 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
 
 // ---- e -> dz, in place ----------------------------------------------------------------------
 // Bound by memory: 7783 rows of V 128000 780 us, 5.1 TB/s, a large copy's rate.
-// 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those from the
-// last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
-// Two parts (`twice`, few rows and an update): what dz loses to bf16 is rounded itself and stands, with the same rows of x, behind the rows, so that
-// dW has 16 bits of the labels' entries, which are most of it, and the 11 of e of the others - the fp32 master would otherwise be off by up to
-// 2^-9 of a single token's whole step.  The product is bound by the weights there; with many rows it would take twice as long, and what
-// one of them is off by is small against the step of all.
+// 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those
+// from the last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
+// Two parts (`twice`: an update by up to 256 rows, dW of up to 64): what dz loses to bf16 is rounded itself and stands, with the same rows of x,
+// behind the rows, so that dW has 16 bits of the labels' entries, which are most of it, and the 11 of e of the others - the fp32 master would
+// otherwise be off by up to 2^-9 of a single token's whole step.  The product is bound by the weights there; with many rows it would take
+// twice as long, and what one of them is off by is small against the step of all.
 // Where rows are not gathered the copy is made here, by the blocks behind the strips', and the tail of W by those behind them.
 __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info, Rows rows,
                                                  int strips, int per, int strip_blocks, uint16_t* __restrict__ xw, int d, const uint16_t* __restrict__ x,

@@ -228,3 +228,33 @@ def test_other_stream_and_captured_graph():
         torch.cuda.synchronize()
         for a, b in zip((*got, *token), (*both(), *kernels.cross_attention_fwd(q[:, :1].contiguous(), k, v, H, Hkv, length))):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Sq,dh", [(1, 64), (80, 128)])
+def test_offsets_behind_32_bits(Sq, dh):
+    """Keys and values as columns of a cache of 6 G elements, tokens 2^24 elements apart: bit for bit what matrices without gaps give, and near 64 bits."""
+    B, Sk, H, Hkv = 2, 200000, 4, 2
+    q, k, v, do, n = _inputs(9, B, Sq, Sk, H, Hkv, dh, [Sk, Sk - 70])
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    length = torch.tensor(n, dtype=torch.int32).cuda()
+
+    def apart(t, ld, at=0):
+        w = torch.empty(*t.shape[:2], ld, dtype=torch.bfloat16, device="cuda")[..., at:at + t.shape[2]]
+        w.copy_(t)
+        return w
+
+    ref = kernels.cross_attention_fwd(q, k, v, H, Hkv, length)
+    grads = kernels.cross_attention_bwd(q, k, v, ref[0], do, ref[1], H, Hkv, length)
+    kw, vw, qw, dow, out = apart(k, 16384), apart(v, 16384, 16000), apart(q, 1 << 24), apart(do, 1 << 24), apart(torch.zeros_like(q), 1 << 24)
+    got = kernels.cross_attention_fwd(qw, kw, vw, H, Hkv, length, out=out)
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    both = torch.empty(B, Sk, 16384, dtype=torch.bfloat16, device="cuda")
+    got = kernels.cross_attention_bwd(qw, kw, vw, out, dow, ref[1], H, Hkv, length, apart(torch.zeros_like(q), 1 << 24), both[..., 8:8 + Hkv * dh],
+                                      both[..., 16384 - Hkv * dh:])
+    for a, b in zip(got, grads):
+        assert torch.equal(a, b)
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    _near(ref[0], out, e_out)
+    assert float((ref[1].double() - lse2).abs().max()) <= 2.0 ** -10
+    for a, r, bound in zip(grads, (dq, dk, dv), (e_dq, e_dk, e_dv)):
+        _near(a, r, bound)

@@ -5,7 +5,8 @@ Tolerances, element by element, from the roundings that the kernels make (a bf16
   loss, lse that of the logits, and a softmax sum of exp2 (2 ulp) in up to 64 + V / 64 additions of a chain, and their log
   dx, dw    the exponential is rounded to fp16 (2^-11, and 2^-40 of a row's weight where it is subnormal), dz to bf16 (2^-8), together below
             2^-8 + 2^-10, and an error of the logits, of the lse and of an exponential, `slack`, moves dz by a factor of
-            exp(slack) < 1 + 2 slack; through a product of absolute values; then the result's own rounding.  The label's column has p - 1 from fp32: its error is that of z, absolute.
+            exp(slack) < 1 + 2 slack; through a product of absolute values; then the result's own rounding.  The label's column has p - 1
+            from fp32: its error is that of z, absolute.
 """
 import math
 
@@ -280,3 +281,47 @@ def test_same_bits_every_time():
     for _ in range(3):
         for a, b in zip(rv.loss_step(x, w, label), ref):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,d,V", [(3, 16384, 131071), (130, 64, (1 << 24) - 1)])
+def test_offsets_behind_31_bits(T, d, V):
+    """The widest weights, 4 GiB of them, and the longest vocabulary, whose exponentials of a piece of rows are 4 GiB, against 64 bits a range of
+    the vocabulary at a time.  Of the additions of a softmax sum a chain has 16 + 2 in a strip, V / 4096 strips and 6 lanes, three roundings
+    each: 80 + V / 1024.  Most of the weights are zero, whose products dx adds without a rounding: only the others count."""
+    g = torch.Generator(device="cuda").manual_seed(21)
+    w = torch.randn(V, d, generator=g, device="cuda", dtype=torch.bfloat16)
+    w *= d ** -0.5
+    w[4096:V // 2] = 0.0
+    w[V // 2 + 4096:V - 4096] = 0.0
+    x = torch.randn(T, d, generator=g, device="cuda").to(torch.bfloat16)
+    label = torch.tensor([V - 1, 0, V - 40], device="cuda").repeat(T // 3 + 1)[:T].contiguous()
+    loss, dx, dw = rv.loss_step(x, w, label)
+    only, lse = rv.loss_forward(x, w, label)
+    step = (1 << 26) // d
+    parts = [(v, min(v + step, V)) for v in range(0, V, step)]
+    x64 = x.double()
+    ref_lse, at, zmax = torch.full((T,), -math.inf, dtype=torch.float64, device="cuda"), torch.zeros(T, dtype=torch.float64, device="cuda"), 0.0
+    for a, b in parts:
+        w64 = w[a:b].double()
+        z = x64 @ w64.T
+        ref_lse = torch.logaddexp(ref_lse, torch.logsumexp(z, 1))
+        zmax = max(zmax, float((x64.abs() @ w64.abs().T).max()))
+        here = (label >= a) & (label < b)
+        at[here] = z[here, label[here] - a]
+    slack = 2 * (d + 8) * 2.0 ** -24 * zmax + (80 + V / 1024) * 2.0 ** -24 + 2.0 ** -22 * float(ref_lse.abs().max())
+    for got, ref in ((loss, ref_lse - at), (only, ref_lse - at), (lse, ref_lse)):
+        assert float((got.double() - ref).abs().max()) <= slack
+    ref_dx, off_dx = torch.zeros_like(x64), torch.zeros_like(x64)
+    for a, b in parts:
+        w64 = w[a:b].double()
+        dz = torch.exp(x64 @ w64.T - ref_lse[:, None])
+        off = dz * (2.0 ** -8 + 2.0 ** -10 + 2 * slack) + 2.0 ** -40
+        rows = torch.nonzero((label >= a) & (label < b))[:, 0]
+        dz[rows, label[rows] - a] -= 1.0
+        off[rows, label[rows] - a] = dz[rows, label[rows] - a].abs() * 2.0 ** -8 + slack
+        ref_dx += dz @ w64
+        off_dx += (off + dz.abs() * 2.0 ** -24 * 3 * 4096) @ w64.abs()
+        ref = dz.T @ x64
+        bound = (off + dz.abs() * 2.0 ** -24 * T).T @ x64.abs()
+        assert bool(((dw[a:b].double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all()), (a, b)
+    assert bool(((dx.double() - ref_dx).abs() <= off_dx * (1 + 2.0 ** -8) + 2.0 ** -8 * ref_dx.abs() + 1e-38).all())
