@@ -258,3 +258,23 @@ def test_offsets_behind_32_bits(Sq, dh):
     assert float((ref[1].double() - lse2).abs().max()) <= 2.0 ** -10
     for a, r, bound in zip(grads, (dq, dk, dv), (e_dq, e_dk, e_dv)):
         _near(a, r, bound)
+
+
+def test_two_calls_at_once():
+    """A long backward beside single tokens on another stream."""
+    q, k, v, do, _ = _inputs(11, 4, 600, 1500, 8, 4, 128, None)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    one = q[:, :1].contiguous()
+    length = torch.tensor([1500, 0, 77, 1024], dtype=torch.int32).cuda()
+    ref = kernels.cross_attention_fwd(q, k, v, 8, 4, length)
+    grads, token = kernels.cross_attention_bwd(q, k, v, ref[0], do, ref[1], 8, 4, length), kernels.cross_attention_fwd(one, k, v, 8, 4, length)
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        got.append((kernels.cross_attention_bwd(q, k, v, ref[0], do, ref[1], 8, 4, length, stream=first),
+                    kernels.cross_attention_fwd(one, k, v, 8, 4, length, stream=second)))
+    torch.cuda.synchronize()
+    for a, b in got:
+        for x, y in zip((*a, *b), (*grads, *token)):
+            assert torch.equal(x, y)

@@ -325,3 +325,33 @@ def test_offsets_behind_31_bits(T, d, V):
         bound = (off + dz.abs() * 2.0 ** -24 * T).T @ x64.abs()
         assert bool(((dw[a:b].double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all()), (a, b)
     assert bool(((dx.double() - ref_dx).abs() <= off_dx * (1 + 2.0 ** -8) + 2.0 ** -8 * ref_dx.abs() + 1e-38).all())
+
+
+@pytest.mark.parametrize("T,rows", [(5, 0), (200, 0), (700, 0), (700, 256)])
+def test_input_gradient_over_its_input(T, rows):
+    x, w, label, _ = _inputs(31, T, 256, 1500, 0.2)
+    x, w, label = x.cuda(), w.cuda(), label.cuda()
+    ref = rv.loss_step(x, w, label, rows=rows)
+    got = rv.loss_step(x, w, label, rows=rows, dx=x)
+    assert got[1] is x
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    cases = []
+    for T, seed in ((1500, 32), (60, 33)):
+        x, w, label, master = (t.cuda() for t in _inputs(seed, T, 512, 20000, 0.1))
+        cases.append(dict(x=x, w=w, label=label, master=master, eta=0.1))
+    ref = [rv.loss_step(**c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, c in enumerate(cases):
+            got[i].append(rv.loss_step(**c, stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for one in got[i]:
+            for a, b in zip(one, ref[i]):
+                assert torch.equal(a, b)
