@@ -158,6 +158,21 @@ __device__ __forceinline__ void band_tile(int i, int vm, int vn, int& bm, int& b
   bm = first + in % rows;
   bn = in / rows;
 }
+// Of a list of tiles of 256x256, those that are handed out whole: where the last round has work for up to half of the CUs its tiles go
+// to two workgroups each, upper and lower half, which take three quarters of a whole one's time.  us, without / with: half of 4096 tokens,
+// V 50257, d 1024 (logits 6.2 rounds, dW 3.1) 717 / 690; update, 1024, V 20000, d 1024 (1.2, 1.2) 220 / 209; 3001, V 50257, d 1600, logits
+// alone (8.5) 394 / 391.  (Quarters would gain a few percent of such a round more, and only where it has 64 tiles or fewer.)
+__host__ __device__ inline int whole_tiles(int tiles) { return tiles > 256 && tiles % 256 <= 128 ? tiles - tiles % 256 : tiles; }
+__host__ __device__ inline int halved_grid(int tiles) { return 2 * tiles - whole_tiles(tiles); }
+// workgroup of halved_grid -> number in the list; half: -1, or which
+__device__ __forceinline__ int dealt_tile(int id, int tiles, int& half) {
+  const int whole = whole_tiles(tiles);
+  half = -1;
+  if (id < whole) return xcd_range(id, whole);
+  id = xcd_range(id - whole, 2 * (tiles - whole));
+  half = id & 1;
+  return whole + id / 2;
+}
 
 // ---- the logits' product ----------------------------------------------------------------------
 // Bound by the matrix cores at the board's power cap: 7783 rows, V 128000, d 2048 3.35 ms, 1.22 PFLOP/s (a library product of 8192^3 1.37); of that
@@ -273,18 +288,22 @@ __global__ __launch_bounds__(64 * NW, 2) void logits_kernel(const uint16_t* __re
                                                             int64_t ldw, int d, Rows rows, LogitsOut o) {
   const int M = rows_of(rows);
   if (M <= 0) return;
-  const int vm = div_up(M, BM), vn = div_up(o.Vp, BN);
-  if ((int)blockIdx.x >= vm * vn) return;
-  int bm, bn;
-  band_tile(xcd_range(blockIdx.x, vm * vn), vm, vn, bm, bn);
-  // the labels of this lane's rows, asked for here: behind the walk along d each would be a round trip of its own
-  constexpr int TM = BM / 2 / 16;
-  const int first = bm * BM + (threadIdx.x >> 6 & 1) * (BM / 2) + (threadIdx.x & 15);
-  int label[TM];
+  const int vm = div_up(M, BM), vn = div_up(o.Vp, BN), tiles = vm * vn;
+  int bm, bn, half = -1;
+  if ((int)blockIdx.x >= (BM == 256 ? halved_grid(tiles) : tiles)) return;
+  band_tile(BM == 256 ? dealt_tile(blockIdx.x, tiles, half) : xcd_range(blockIdx.x, tiles), vm, vn, bm, bn);
+  auto tile = [&](auto rows_of_tile, int bm) {
+    constexpr int BT = rows_of_tile, TM = BT / 2 / 16;
+    // the labels of this lane's rows, asked for here: behind the walk along d each would be a round trip of its own
+    const int first = bm * BT + (threadIdx.x >> 6 & 1) * (BT / 2) + (threadIdx.x & 15);
+    int label[TM];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) label[i] = first + i * 16 < M ? label_of(rows, first + i * 16) : -1;
-  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, label, m0 + wm0, n0 + wn0, M); };
-  gemm_dtl_body<BM, BN, 32, NS, NW, false, false, EPI_OWN>(x, ldx, x_bs, w, ldw, 32, M, o.V, d, bm, bn, Epi{}, nullptr, 0, own);
+    for (int i = 0; i < TM; ++i) label[i] = first + i * 16 < M ? label_of(rows, first + i * 16) : -1;
+    auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) { strip_epilogue<STORE>(acc, o, label, m0 + wm0, n0 + wn0, M); };
+    gemm_dtl_body<BT, BN, 32, NS, NW, false, false, EPI_OWN>(x, ldx, x_bs, w, ldw, 32, M, o.V, d, bm, bn, Epi{}, nullptr, 0, own);
+  };
+  if (BM == 128 || half < 0) tile(std::integral_constant<int, BM>{}, bm);
+  else if ((2 * bm + half) * 128 < M) tile(std::integral_constant<int, 128>{}, 2 * bm + half);
 }
 
 // ---- strips joined to rows ----------------------------------------------------------------------
@@ -505,8 +524,8 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
 }
 
 // ---- dW ----------------------------------------------------------------------
-// 256x256 tiles, the contraction over the rows: 7783 rows, V 128000, d 2048 3.0 ms, 1.36 PFLOP/s; 2048, V 50257, d 1024 0.22 ms, 0.96 (788 tiles are
-// three rounds of the CUs and a twelfth); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update 74 us with dx, 4.7 TB/s.
+// 256x256 tiles, the contraction over the rows: 7783 rows, V 128000, d 2048 3.0 ms, 1.36 PFLOP/s; 2048, V 50257, d 1024 0.21 ms, 1.0 (788 tiles are
+// three rounds of the CUs and a twelfth, which is dealt out in halves); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update 74 us with dx, 4.7 TB/s.
 // KIND 0: bf16 dw.  1: the update of Eq. 2 on an fp32 master (w' = w - eta dW, one fused multiply-add) and its bf16 version.
 // 2: fp32 sums of one of S stretches of the rows (few tiles), or of the first piece.  3: added to those of the pieces before.
 constexpr int WB = 256, W_NS = 4, W_NW = 8;
@@ -517,37 +536,44 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
   if (M <= 0 && a.rows.p) return;
   const int64_t bs = 32ll * a.rows.R;
   const int nk = row_tiles(a.rows, M), vm = div_up(V, WB), vn = div_up(d, WB), tiles = vm * vn, parts = KIND == 2 ? row_stretches(a.S_w, nk) : 1;
-  if (id >= tiles * parts) return;
-  id = xcd_range(id, tiles * parts);
+  constexpr bool kHalves = KIND != 2;
+  if (id >= (kHalves ? halved_grid(tiles) : tiles * parts)) return;
+  int half = -1;
+  id = kHalves ? dealt_tile(id, tiles, half) : xcd_range(id, tiles * parts);
   const int s = id / tiles;
   const int in = id - s * tiles, bn = in % vn, bm = in / vn;
   const int k0 = nk * s / parts, k1 = nk * (s + 1) / parts;
-  auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) {
-    constexpr int TM = WB / 2 / 16, TN = WB / (W_NW / 2) / 16;
-    Epi o{};
-    o.ldo = d;
-    if constexpr (KIND == 0) {
-      o.out = a.dw;
-      f32x4 scaled[TM][TN];
+  auto tile = [&](auto rows_of_tile, int bm) {
+    constexpr int BT = rows_of_tile;
+    auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) {
+      constexpr int TM = BT / 2 / 16, TN = WB / (W_NW / 2) / 16;
+      Epi o{};
+      o.ldo = d;
+      if constexpr (KIND == 0) {
+        o.out = a.dw;
+        f32x4 scaled[TM][TN];
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) scaled[i][j] = acc[i][j] * a.scale;
-      write_tile_staged<WB, WB, 64 * W_NW, f32x4, TM, TN, EPI_BF16>(scaled, o, m0, n0, wm0, wn0, V, d, dtl_smem);
-    } else if constexpr (KIND == 1) {
-      o.out = a.master_out; o.resid = a.master; o.ldr = d; o.out2 = a.version; o.eta = a.eta;
-      f32_tile_through_lds<WB, WB, W_NW, f32x4, TM, TN, 2, true>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
-    } else if constexpr (KIND == 2) {
-      o.out = a.sums + (int64_t)s * V * d;
-      write_tile<f32x4, TM, TN, EPI_F32>(acc, o, m0 + wm0, n0 + wn0, V, d);
-    } else {
-      o.out = a.sums; o.resid = a.sums; o.ldr = d;
-      f32_tile_through_lds<WB, WB, W_NW, f32x4, TM, TN, 3, false>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
-    }
+          for (int j = 0; j < TN; ++j) scaled[i][j] = acc[i][j] * a.scale;
+        write_tile_staged<BT, WB, 64 * W_NW, f32x4, TM, TN, EPI_BF16>(scaled, o, m0, n0, wm0, wn0, V, d, dtl_smem);
+      } else if constexpr (KIND == 1) {
+        o.out = a.master_out; o.resid = a.master; o.ldr = d; o.out2 = a.version; o.eta = a.eta;
+        f32_tile_through_lds<BT, WB, W_NW, f32x4, TM, TN, 2, true>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
+      } else if constexpr (KIND == 2) {
+        o.out = a.sums + (int64_t)s * V * d;
+        write_tile<f32x4, TM, TN, EPI_F32>(acc, o, m0 + wm0, n0 + wn0, V, d);
+      } else {
+        o.out = a.sums; o.resid = a.sums; o.ldr = d;
+        f32_tile_through_lds<BT, WB, W_NW, f32x4, TM, TN, 3, false>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
+      }
+    };
+    // (the loads of dz run over whole strips, the results end at V)
+    gemm_dtl_body<BT, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, bs, a.xw + (int64_t)k0 * 32 * 32, 32, bs, Vp, d,
+                                                               (k1 - k0) * 32, bm, bn, Epi{}, nullptr, 0, own);
   };
-  // (the loads of dz run over whole strips, the results end at V)
-  gemm_dtl_body<WB, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, bs, a.xw + (int64_t)k0 * 32 * 32, 32, bs, Vp, d,
-                                                             (k1 - k0) * 32, bm, bn, Epi{}, nullptr, 0, own);
+  if (!kHalves || half < 0) tile(std::integral_constant<int, WB>{}, bm);
+  else if (kHalves && (2 * bm + half) * (WB / 2) < V) tile(std::integral_constant<int, WB / 2>{}, 2 * bm + half);
 }
 template <int KIND>
 __global__ __launch_bounds__(512, 2) void weight_grad_kernel(GradArgs a) { weight_grad_body<KIND>(a, blockIdx.x); }
@@ -591,10 +617,12 @@ __global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __re
 // ---- host ----------------------------------------------------------------------
 
 // The 256x256 tile, or 128x128 ones, two workgroups to a CU, where they take less of the chip's time (rounds * area / efficiency, the
-// ratio of the two as in gemm_bf16.hip)
-bool big_tiles(int rows, int cols) {
+// ratio of the two as in gemm_bf16.hip).  A last round of halves counts three quarters where the walk is long enough: 2048 rows, V 9000, d 2048
+// (288 tiles) 96 us with tiles of 256, 101 of 128; 4096, V 4400, d 1024 (288) 61 / 62.5; but 8192, V 2500, d 512 (320) 45 / 43.
+bool big_tiles(int rows, int cols, int d) {
   const int64_t b = (int64_t)div_up(rows, 256) * div_up(cols, 256), m = (int64_t)div_up(rows, 128) * div_up(cols, 128);
-  return (double)((b + 255) / 256) * 65536 <= (double)((m + 511) / 512) * 2 * 16384 / 0.83;
+  const double rounds = (double)((b + 255) / 256) - (d >= 1024 && b % 256 && whole_tiles((int)b) < b ? 0.25 : 0);
+  return rounds * 65536 <= (double)((m + 511) / 512) * 2 * 16384 / 0.83;
 }
 // Tile and stretches of a product [M, N] over nk k-tiles whose fp32 sums a kernel adds: the least modelled time, us, of tiles of 256 and, with
 // `small`, of 128 whose walk is split over the two halves of a workgroup; one workgroup to a CU.  A round is a start and a walk, whose
@@ -676,10 +704,11 @@ rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const 
   const int64_t ldx = q.few ? a.ldx : 32, x_bs = q.few ? 32 : 32ll * q.P;
   const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), q.P, q.R, q.V, q.Vp};
   const int most = q.T < q.P ? q.T : q.P;
-  if (big_tiles(most, q.Vp)) {
+  if (big_tiles(most, q.Vp, q.d)) {
     constexpr auto kern = logits_kernel<256, 256, 4, 8, STORE>;
     if (rv_allow_lds<kern>(kBigLds) != hipSuccess) return RV_E_DEVICE;
-    hipLaunchKernelGGL(kern, dim3(div_up(most, 256) * div_up(q.Vp, 256)), dim3(512), kBigLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
+    // (fewer tile rows than all rows have may be dealt out in halves where those are not)
+    hipLaunchKernelGGL(kern, dim3(div_up(most, 256) * div_up(q.Vp, 256) + 128), dim3(512), kBigLds, st, x, ldx, x_bs, w, q.ldw, q.d, rows, o);
   } else {
     constexpr auto kern = logits_kernel<128, 128, 4, 4, STORE>;
     if (rv_allow_lds<kern>(kMidLds) != hipSuccess) return RV_E_DEVICE;
@@ -707,7 +736,7 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
   g.S_w = q.S_w; g.sums = (float*)(work + q.acc);
   g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version;
   g.scale = a.scale; g.eta = a.eta * a.scale;
-  const int w_grid = div_up(q.V, WB) * div_up(q.d, WB) * (KIND == 2 ? q.S_w : 1);
+  const int w_tiles = div_up(q.V, WB) * div_up(q.d, WB), w_grid = KIND == 2 ? w_tiles * q.S_w : halved_grid(w_tiles);
   // together, but for an update in place: dx reads the weights that it overwrites
   const bool both = KIND >= 0 && a.dx && q.dx.tile == 128 &&
                     !(KIND == 1 && rv_overlap(a.w, 2 * (size_t)q.V * q.ldw, a.version, 2 * (size_t)q.V * q.d));

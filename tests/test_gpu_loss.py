@@ -355,3 +355,18 @@ def test_two_calls_at_once():
         for one in got[i]:
             for a, b in zip(one, ref[i]):
                 assert torch.equal(a, b)
+
+
+# more tiles of 256x256 than CUs, a few left for a last round: of the logits, and of dW; the last tile row and column end in their upper half
+@pytest.mark.parametrize("T,d,V", [(5200, 64, 6400), (300, 4096, 4400)])
+def test_last_round_in_halves(T, d, V):
+    x, w, label, master = (t.cuda() for t in _inputs(41, T, d, V))
+    g = torch.full((T,), 0.5, device="cuda")
+    loss, lse = rv.loss_forward(x, w, label)
+    _check(x, w, label, g, loss, lse)
+    loss, dx, dw = rv.loss_step(x, w, label, scale=0.5)
+    _check(x, w, label, g, loss, None, dx, dw)
+    loss, dx, new, version = rv.loss_step(x, w, label, scale=0.5, master=master, eta=0.1)
+    _check(x, w, label, g, loss, None, dx, None, master, 0.1, new, version)
+    loss, dx, dw = rv.loss_step(x, w, label, scale=0.5, rows=128)
+    _check(x, w, label, g, loss, None, dx, dw)
