@@ -765,7 +765,10 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   p.token = R <= OWN;
   p.fwd_parts = p.token ? parts_for(U, up(Sk, TOKEN_KEYS), kTokenGrid, 8) : parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
   p.q_parts = parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);
-  p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(R, TILE), 512, 4);
+  // half as many for dK and dV: dQ's workgroups run beside them, and a part costs 8 bytes a key's element.  us, 512 / 256: 1024 of 16 heads over 4 of
+  // 128, 2048 keys 250 / 231; 1500 of 12 heads over 400 60 / 53; 512 of 16 over 4, 577 keys, 8 sequences 91 / 97.  (256 for dQ, too: 162 rows
+  // over up to 6893 keys 194 / 233.)
+  p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(R, TILE), 256, 4);
   auto round = [](size_t b) { return (b + 255) / 256 * 256; };
   const bool parts = p.fwd_parts > 1;
   p.fwd_ml = parts ? round((size_t)4 * p.fwd_parts * U * R * dh) : 0;
