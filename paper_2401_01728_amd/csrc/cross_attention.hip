@@ -883,8 +883,8 @@ extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const 
   const hipStream_t st = (hipStream_t)stream;
   // Heads of 128: two waves to a SIMD either way (registers).  Eight that share two slots are the faster where there are rounds of them,
   // two workgroups of four with a slot each where one is short of work or ends early.  us, eight / four: 4 x 4096 x 4096 tokens, 16 heads (2048
-  // workgroups of eight) 1709 / 1838; 162 tokens of 32 heads over 16 and up to 6893 keys (1120) 224 / 203; 1024 of 16 over 4 and up to 2048
-  // (512) 215 / 198; 48 rows over up to 9981 keys 168 / 153.  Heads of 64 are faster with four: three waves to a SIMD, 4 x 4096 x 4096 892 / 979.
+  // workgroups of eight) 1711 / 1830; 162 tokens of 32 heads over 16 and up to 6893 keys (1184) 223 / 195; 1024 of 16 over 4 and up to 2048
+  // (384) 219 / 193.  Heads of 64 are faster with four: three waves to a SIMD, 4 x 4096 x 4096 892 / 979.
   if (d_head == 64) return backward<64, 4, 2>(a, p, (char*)work, st);
   const int64_t eights = (int64_t)B * n_kv_heads * (up(Sk, 8 * OWN) * p.kv_parts + up(p.R, 8 * OWN) * p.q_parts);
   return p.R > 4 * OWN && Sk > 4 * OWN && eights >= 1536 ? backward<128, 8, 2>(a, p, (char*)work, st) : backward<128, 4, 1>(a, p, (char*)work, st);
