@@ -144,6 +144,14 @@ __device__ __forceinline__ void clear(f32x16 (&v)[N]) {
     for (int r = 0; r < 16; ++r) v[i][r] = 0.f;
 }
 
+// A sequence of one key: its probability is 1 whatever the score, so the score's gradient is zero; what stands here is the difference of one sum
+// formed in two orders.  (Times zero: what is not a number stays none.)
+template <int N>
+__device__ __forceinline__ void of_one_key(f32x16 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] *= 0.f;
+}
+
 // waits that later LDS reads are not moved in front of
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
@@ -597,6 +605,7 @@ __device__ __forceinline__ void bwd_q_body(const CrossArgs& a, int id, int grid)
     tile(t * TILE, smem + (t - t0) % NS * SLOT);
   }
   if (!active || r >= a.R) return;
+  if (n == 1) of_one_key(dq);
   if (parts == 1) store_owned<DH>(dq, a.scale, a.dq + row_at<DH>(a, w.b, w.h, r, a.lddq));
   else store_owned32<DH>(dq, a.q_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r) * DH);
 }
@@ -694,6 +703,7 @@ __device__ __forceinline__ void bwd_kv_body(const CrossArgs& a, int id, int grid
     }
   }
   if (j >= a.Sk) return;
+  if (n == 1) of_one_key(dk);
   if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
   if (parts == 1) {
     store_owned<DH>(dk, a.scale, a.dk + ((int64_t)w.b * a.Sk + j) * a.lddk + w.h * DH);

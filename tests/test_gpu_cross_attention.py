@@ -278,3 +278,24 @@ def test_two_calls_at_once():
     for a, b in got:
         for x, y in zip((*a, *b), (*grads, *token)):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("B,Sq,Sk,dh,klen", [(2, 20, 1, 128, None), (1, 300, 1, 64, None), (3, 40, 2000, 64, [1, 2000, 1]), (2, 1000, 70, 128, [1, 1])])
+def test_one_key(B, Sq, Sk, dh, klen):
+    """Its probability is 1 whatever the score: dq and dk are exactly zero."""
+    q, k, v, do, n = _inputs(13, B, Sq, Sk, 4, 2, dh, klen)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    q[0, 3] = float("nan")
+    length = torch.tensor(klen, dtype=torch.int32).cuda() if klen is not None else None
+    out, lse2 = kernels.cross_attention_fwd(q, k, v, 4, 2, length)
+    dq, dk, dv = kernels.cross_attention_bwd(q, k, v, out, do, lse2, 4, 2, length)
+    rows = torch.ones(B, Sq, dtype=torch.bool)
+    rows[0, 3] = False
+    for b in range(B):
+        if n[b] == 1:
+            assert not dq[b][rows[b].cuda()].any()
+            assert not dk[b, 1:].any()
+            if b:
+                assert not dk[b].any()
+    assert bool(torch.isnan(dq[0, 3]).all()) and bool(torch.isnan(dk[0, 0]).all())
+    assert bool(torch.isfinite(dv[1:]).all())
