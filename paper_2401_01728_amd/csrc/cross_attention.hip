@@ -770,7 +770,8 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128)) return false;
   if (B > (1 << 20) || Sq > (1 << 24) || Sk > (1 << 24) || H > (1 << 16)) return false;
   const int64_t U = B * Hkv, R = H / Hkv * Sq;
-  if (R > (1ll << 30) || U * up(R, OWN) > (1ll << 30) || U * up(Sk, OWN) > (1ll << 30) || U * R * dh / 8 > (1ll << 38) || U * Sk * dh / 8 > (1ll << 38)) return false;
+  if (R > (1ll << 30) || U * up(R, OWN) > (1ll << 30) || U * up(Sk, OWN) > (1ll << 30)) return false;
+  if (U * R * dh / 8 > (1ll << 38) || U * Sk * dh / 8 > (1ll << 38)) return false;
   p.R = (int)R; p.Rp = (int)(up(R, TILE) * TILE);
   p.token = R <= OWN;
   p.fwd_parts = p.token ? parts_for(U, up(Sk, TOKEN_KEYS), kTokenGrid, 8) : parts_for(U * up(R, OWN * 4), up(Sk, TILE), 512, 4);

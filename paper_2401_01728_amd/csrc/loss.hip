@@ -525,7 +525,8 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
 
 // ---- dW ----------------------------------------------------------------------
 // 256x256 tiles, the contraction over the rows: 7783 rows, V 128000, d 2048 3.0 ms, 1.36 PFLOP/s; 2048, V 50257, d 1024 0.21 ms, 1.0 (788 tiles are
-// three rounds of the CUs and a twelfth, which is dealt out in halves); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update 74 us with dx, 4.7 TB/s.
+// three rounds of the CUs and a twelfth, which is dealt out in halves); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update
+// 74 us with dx, 4.7 TB/s.
 // KIND 0: bf16 dw.  1: the update of Eq. 2 on an fp32 master (w' = w - eta dW, one fused multiply-add) and its bf16 version.
 // 2: fp32 sums of one of S stretches of the rows (few tiles), or of the first piece.  3: added to those of the pieces before.
 constexpr int WB = 256, W_NS = 4, W_NW = 8;
