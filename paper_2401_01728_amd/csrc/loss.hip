@@ -451,7 +451,7 @@ struct GradArgs {
   int d, Vp;
   int S_dx, tiles_m, dx_grid;             // dx: stretches for all rows, their tile rows, workgroups
   const uint16_t* tail; float* part;
-  int S_w;                                // dW
+  int S_w, w_first;                       // dW; its workgroups in front of those of dx (both_grads_kernel)
   float* sums; uint16_t* dw; const float* master; float* master_out; uint16_t* version;
   float scale, eta;                       // eta: times scale
 };
@@ -580,10 +580,14 @@ template <int KIND>
 __global__ __launch_bounds__(512, 2) void weight_grad_kernel(GradArgs a) { weight_grad_body<KIND>(a, blockIdx.x); }
 // dx in tiles of 128 and dW in one launch, where neither keeps the chip busy for long.  (With dx in tiles of 256, which do, it costs: 8192 tokens,
 // V 128000, d 2048 10.64 ms apart, 10.81 together; 4096, V 32000 1.47 / 1.49; half of 4096, V 50257, d 1024 720 / 710 us.)
+// dW's workgroups, the longer ones, come first where there are few of them, or stretches of many rows, and dx's fill the chip beside them.  us,
+// dx / dW first: 600 tokens, V 10000, d 512 (80 workgroups of dW) 63 / 58; 6738, V 1347, d 320, update (12 tiles in stretches) 83 / 78; but 256,
+// V 30522, d 448 (240) 59.8 / 60.7, 100, V 32000, d 1024 (500) 67 / 71.
 template <int KIND>
 __global__ __launch_bounds__(512, 2) void both_grads_kernel(GradArgs a) {
-  if ((int)blockIdx.x < a.dx_grid) input_grad_body<128>(a, blockIdx.x);
-  else weight_grad_body<KIND>(a, blockIdx.x - a.dx_grid);
+  const int id = (int)blockIdx.x - a.w_first;
+  if (id >= 0 && id < a.dx_grid) input_grad_body<128>(a, id);
+  else weight_grad_body<KIND>(a, id < 0 ? blockIdx.x : id - a.dx_grid);
 }
 // fp32 sums of stretches or pieces -> dw, or the update
 __global__ __launch_bounds__(256) void weight_grad_join_kernel(const float* __restrict__ sums, int S, Rows rows, int pieces, int64_t n,
@@ -746,6 +750,7 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
     else RV_TRY((launch_512<input_grad_kernel<128>>(g, g.dx_grid, kSplitLds, st)));
   }
   if constexpr (KIND >= 0) {
+    g.w_first = w_grid <= (KIND == 2 ? 256 : 128) ? w_grid : 0;
     if (both) RV_TRY((launch_512<both_grads_kernel<KIND>>(g, g.dx_grid + w_grid, kBothLds, st)));
     else RV_TRY((launch_512<weight_grad_kernel<KIND>>(g, w_grid, kWeightLds, st)));
   }
