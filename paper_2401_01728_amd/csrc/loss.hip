@@ -8,13 +8,16 @@
 // Three products of 2 T V d flop each; the forward alone is one.
 //
 // The logits are never written.  A wave of the first product holds 64 columns of the vocabulary - a strip - of its rows; it takes
-// each row's maximum over the strip (fp32), m = max z log2 e - 15, and writes the pair (m, sum of exp2(z log2 e - m)) and, for the
+// each row's maximum over the strip, m, and writes the pair (m, sum of exp2((z - m) log2 e + 15)) in fp32 and, for the
 // gradients, the exponentials e themselves in fp16: they are at most 2^15 whatever the logits are, keep 11 bits down to 2^-29 of the
 // strip's largest and are off by less than 2^-40 of it below.  (Logits in 16 bits would move a probability by |z| 2^-9 of itself, e in
 // bf16 by 2^-8: with the rounding of dz the gradients were then 1.6 times as far from 64 bits as their own rounding, now 1.2.)  The pairs of
-// a row's strips are joined to its lse, and  dz = e exp2(m - lse2) r  overwrites e in place, rounded to bf16, which is what the matrix
-// instructions take.  The label's own column gets  r expm1(z_y - lse)  from the fp32 logit: where the model is nearly certain,
-// p - 1 from a rounded p would have no digits left.
+// a row's strips are joined to its largest logit, top, and the sum of its exponentials, and  dz = e exp2((m - top) log2 e) r / sum  overwrites e
+// in place, rounded to bf16, which is what the matrix instructions take.
+// Maximum and sum stay two numbers: differences are formed of logits, before anything is multiplied or added, so that what they lose
+// does not grow with the logits (m log2 e or lse in ONE fp32 number is off by 2^-24 of itself, and a probability by that many powers of e).
+// loss = (top - z_y) + ln sum has two terms that are not negative, and the label's own column of dz is  r expm1(-loss):
+// p - 1 from a rounded p would have fewer digits where the model is nearly certain.
 // Computing z again for the gradients instead of keeping e would be a fourth product: 2 bytes of e written and 4 moved by the pass
 // that makes dz of it are 1.2 ps a logit at 5 TB/s, the product 2 d / 1.3 PFLOP/s = 1.6 ps at d 1024, 3.2 ps at 2048.
 // One piece of rows is kept at a time (e and strips of `rows` rows, at most 2 GiB of e where the caller leaves the choice), so the work
@@ -29,13 +32,13 @@
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int STRIP = 64;
 constexpr int kTop = 15;                 // a strip's largest exponential is 2^15
 constexpr int64_t kMostE = 1ll << 30;    // elements of e, of a piece's rows: offsets in a product are 31 bits, and 2 GiB of work memory
 
 // what a row of the piece needs in the backward
-struct RowInfo { float lse2, g, at_label; int label; };
+struct RowInfo { float top, g, at_label; int label; };    // largest logit; weight over the sum of exponentials; dz of the label
 
 struct CutForm { int tile, S; };
 struct Plan {
@@ -253,14 +256,14 @@ __device__ __forceinline__ void strip_epilogue(const f32x4 (&acc)[TM][TN], const
     for (int c = 0; c < TN; ++c)
 #pragma unroll
       for (int k = 0; k < 4; ++k) m = fmaxf(m, a[i][c][k]);
-    m = __fmaf_rn(quad_max(m), kLog2e, -(float)kTop);
+    m = quad_max(m);
     const float base = m == -INFINITY ? 0.f : m;           // (a strip of -inf alone: its sum is zero)
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < TN; ++c)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        a[i][c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[i][c][k], kLog2e, -base));
+        a[i][c][k] = __builtin_amdgcn_exp2f(__fmaf_rn(a[i][c][k] - base, kLog2e, (float)kTop));
         sum += a[i][c][k];
       }
     sum = quad_sum(sum);
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
   if ((int)blockIdx.x * 16 >= M) return;
   auto join = [](float2 a, float2 b) {
     const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.f : m;
-    return float2{m, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base)};
+    return float2{m, a.y * __builtin_amdgcn_exp2f((a.x - base) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - base) * kLog2e)};
   };
   float2 v = {-INFINITY, 0.f};
   if (row < M) {
@@ -339,12 +342,13 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
     if (info) info[row] = RowInfo{0.f, 0.f, 0.f, -1};
     return;
   }
-  const float lse2 = v.x + __builtin_amdgcn_logf(v.y), ln = lse2 * kLn2, at = target[row];   // v_log_f32 is log2
-  loss[t] = ln - at;
-  if (lse) lse[t] = ln;
+  // (the largest logit's own exponential is exactly 2^kTop and nothing is taken away from a sum: the log is not negative)
+  const float ln = logf(v.y * (1.0f / (1 << kTop))), each = (v.x - target[row]) + ln;
+  loss[t] = each;
+  if (lse) lse[t] = v.x + ln;
   if (info) {
     const float g = row_scale ? row_scale[t] : 1.0f;
-    info[row] = RowInfo{lse2, g, g * expm1f(at - ln), y};
+    info[row] = RowInfo{v.x, g / v.y, g * expm1f(-each), y};
   }
 }
 
@@ -406,7 +410,7 @@ __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const
   const RowInfo r = info[row];
 #pragma unroll 2
   for (int s = s0; s < s1; ++s) {
-    const float f = r.g * __builtin_amdgcn_exp2f(stat[(int64_t)s * P + row].x - r.lse2);
+    const float f = r.g * __builtin_amdgcn_exp2f((stat[(int64_t)s * P + row].x - r.top) * kLog2e);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       u32x4* at = reinterpret_cast<u32x4*>(base + (2 * s + h) * bs);

@@ -370,3 +370,77 @@ def test_last_round_in_halves(T, d, V):
     _check(x, w, label, g, loss, None, dx, None, master, 0.1, new, version)
     loss, dx, dw = rv.loss_step(x, w, label, scale=0.5, rows=128)
     _check(x, w, label, g, loss, None, dx, dw)
+
+
+def _exact_logits(level, T, V, d, seed):
+    """Operands whose logits fp32 holds exactly, of about the size `level`: x is zero but for +-A and +-B, powers of two, and a row of w has 1 or 1/2
+    against A and a whole number up to 127 against B.  Labels: a third are a row's largest logit, a third close to it, a third any."""
+    g = torch.Generator().manual_seed(seed)
+    A = 2.0 ** math.ceil(math.log2(level))
+    B = max(2.0 ** -2, A * 2.0 ** -23)
+    w = torch.randn(V, d, generator=g)
+    w[:, 0] = torch.where(torch.rand(V, generator=g) < 0.5, 1.0, 0.5)
+    w[:, 40] = torch.randint(-127, 128, (V,), generator=g).float()
+    x = torch.zeros(T, d)
+    x[:, 0] = A * (torch.randint(0, 2, (T,), generator=g) * 2 - 1)
+    x[:, 40] = B * (torch.randint(0, 2, (T,), generator=g) * 2 - 1)
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    z = x.double() @ w.double().T
+    assert torch.equal(z.float().double(), z)
+    order = torch.argsort(z, 1, descending=True)
+    rank = torch.where(torch.arange(T) % 3 == 0, 0, torch.where(torch.arange(T) % 3 == 1, torch.arange(T) % 7 % V, torch.randint(0, V, (T,), generator=g)))
+    return x, w, order.gather(1, rank[:, None])[:, 0], z
+
+
+@pytest.mark.parametrize("level", [30.0, 1e3, 1e5, 1e6, 1.2e7, 1e8])
+@pytest.mark.parametrize("T,V", [(70, 1), (70, 330), (400, 3001)])
+def test_logits_of_any_size(level, T, V):
+    """Where the logits are exact only the softmax is off, whatever their size.  Per row, relative to the exponential of its largest logit, `rest` the sum of the others':
+      an exponential's argument, up to 16, is rounded once (2^-21, times ln 2) behind a difference of two logits that is rounded with its product by log2 e (2^-23 of it;
+        what is 2^-40 or less counts as a whole), and exp2 is off by 2^-23: together below 2^-20 of the term, and the largest itself is exact;
+      a sum is a chain of 16 + 2 additions in a strip and 1 + 6 joins of three roundings each, 39 at most, of which one that adds t is off by t at most;
+      the log by 2^-23, top - at and the last addition by 2^-24 of themselves."""
+    d = 64
+    x, w, label, z = _exact_logits(level, T, V, d, 51)
+    top, at = z.max(1).values, z.gather(1, label[:, None])[:, 0]
+    rest = torch.exp(z - top[:, None]).sum(1) - 1.0
+    loss = (top - at) + torch.log1p(rest)
+    tol = rest * 2.0 ** -20 + torch.minimum(39 * 2.0 ** -24 * (1 + rest), rest) + 2.0 ** -22 * loss
+    got, lse = rv.loss_forward(x.cuda(), w.cuda(), label.cuda())
+    got2, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.5)
+    assert torch.equal(got, got2)
+    got, lse = got.cpu().double(), lse.cpu().double()
+    assert bool((got >= 0).all())
+    assert bool(((got - loss).abs() <= tol).all()), float(((got - loss).abs() - tol).max())
+    assert bool(((lse - (top + torch.log1p(rest))).abs() <= tol + 2.0 ** -23 * (top.abs() + 16)).all())
+    p = torch.exp(z - top[:, None]) / (1 + rest)[:, None]
+    dz = p.clone()
+    rows = torch.arange(T)
+    dz[rows, label] = torch.expm1(-loss)
+    # fp16 and bf16, and the sum and the factor of a strip: below 2^-10 with them; the label's entry: bf16 alone, of the loss above
+    off = dz.abs() * (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -12) + 2.0 ** -40
+    off[rows, label] = dz[rows, label].abs() * (2.0 ** -8 + 2.0 ** -20) + tol
+    x64, w64 = x.double(), w.double()
+    fp32 = 2.0 ** -24 * (T + V)
+    for a, ref, bound in ((dx, dz @ w64, (off + dz.abs() * fp32) @ w64.abs()), (dw, dz.T @ x64, (off + dz.abs() * fp32).T @ x64.abs())):
+        ref, bound = 0.5 * ref, 0.5 * bound
+        assert bool(((a.cpu().double() - ref).abs() <= bound * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + 1e-38).all())
+
+
+def test_losses_of_certain_tokens():
+    """Logits as a model has them: no loss is negative, and where the label has all but 2^-30 of the probability the loss is below 2^-22, its gradient, too."""
+    g = torch.Generator().manual_seed(52)
+    T, d, V = 300, 128, 900
+    w = torch.randn(V, d, generator=g)
+    label = torch.randint(0, V, (T,), generator=g)
+    x = torch.rand(T, 1, generator=g) * 1.2 * w[label]
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    loss, dx, _ = rv.loss_step(x.cuda(), w.cuda(), label.cuda())
+    z = x.double() @ w.double().T
+    ref = torch.logsumexp(z, 1) - z.gather(1, label[:, None])[:, 0]
+    sure = ref < 2.0 ** -30
+    assert int(sure.sum()) > 100
+    assert bool((loss >= 0).all())
+    assert float(loss.cpu()[sure].max()) < 2.0 ** -22
+    # of dz in such a row: the label's entry is the loss, all others together as much again
+    assert float(dx.cpu()[sure].double().abs().max()) <= 2.0 ** -20 * float(w.double().abs().max())
