@@ -273,7 +273,9 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *   master, master_out, version, eta   all three or none, in place of dw, device [V, d] without gaps: the update of Eq. 2 in the
  *             same call, master_out = master - eta * dz^T x (fp32), version = its bf16 rounding.  The product's fp32 sums are used,
  *             not their rounding.  master_out may be master, version may be w.
- * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16.
+ * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16: an element
+ * of dx, dw or the step is off by up to 2^-8 of its terms.  An update by T <= 256 rows, and dw of T <= 64, take dz in two bf16 parts, 16 bits of
+ * a label's entry and the 11 of their exponentials of the others: what a master gets is then no further off than that, whatever V and `rows`.
  *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 128 or a multiple of 256): bounds the work
  *             memory at about 2 V * rows bytes; with several such pieces dw is added up in fp32, 4 V d bytes more.
  *             0: as many as 2 GiB hold.  Outputs do not depend on it but for the order of those sums.

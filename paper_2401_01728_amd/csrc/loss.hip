@@ -25,8 +25,8 @@
 //
 // Rows whose label lies outside [0, V) - prompts, padding - take no part: a first kernel gathers the others, in order, into a copy of
 // x without gaps, in blocks of 32 columns (rv_mat), and all kernels behind it go by the number of rows it counted.  So a batch that is half
-// prompt costs half.  Up to 256 rows, whose products are bound by the weights, are not gathered: a launch less, and the rows that take no
-// part become zeros where dz and its copy of x are made.  Either way nothing such a row holds (NaN of an unwritten buffer) reaches an output.
+// prompt costs half.  A batch of up to 256 rows, whose products are bound by the weights, is not gathered: a launch less, and the rows that take
+// no part become zeros where dz and its copy of x are made.  Either way nothing such a row holds (NaN of an unwritten buffer) reaches an output.
 #include <math.h>
 #include "gemm_core.h"
 
@@ -35,7 +35,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int STRIP = 64;
 constexpr int kTop = 15;                 // a strip's largest exponential is 2^15
-constexpr int64_t kMostE = 1ll << 30;    // elements of e, of a piece's rows: offsets in a product are 31 bits, and 2 GiB of work memory
+constexpr int64_t kMostE = 1ll << 30;    // elements of e of a piece's rows, where the caller leaves the choice
 
 // what a row of the piece needs in the backward
 struct RowInfo { float top, g, at_label; int label; };    // largest logit; weight over the sum of exponentials; dz of the label
@@ -43,7 +43,7 @@ struct RowInfo { float top, g, at_label; int label; };    // largest logit; weig
 struct CutForm { int tile, S; };
 struct Plan {
   int T, d, V, Vp, P, R, pieces;         // V rounded up to whole strips; rows of a piece, of a block of e; number of pieces
-  bool grads, few;                       // few: rows are not gathered
+  bool grads, few;                       // few: up to kFewRows rows, not gathered
   int64_t ldw;
   CutForm dx;                            // tile and stretches of dx; stretches of dW
   int S_w;
@@ -53,8 +53,8 @@ struct Plan {
 __host__ __device__ inline int div_up(int a, int b) { return (a + b - 1) / b; }
 __host__ __device__ inline int round_up(int a, int b) { return div_up(a, b) * b; }
 
-// The rows that the kernels work on.  Gathered (count != null): *count rows without gaps, lab and idx their labels and places; pieces of P of
-// them.  Up to kFewRows rows stay where they are: one piece, and those that take no part become zeros where dz is made.
+// The rows that the kernels work on, in pieces of P.  Gathered (count != null): *count rows without gaps, lab and idx their labels and places.
+// Up to kFewRows rows stay where they are, and those that take no part become zeros where dz is made.
 struct Rows {
   const int* count; const int* lab; const int* idx; const int* pos;
   const int64_t* label;
@@ -69,11 +69,13 @@ __device__ __forceinline__ int rows_of(const Rows& r) {
 }
 // k-tiles of dW's product over them, one of zeros where there is none
 __device__ __forceinline__ int row_tiles(const Rows& r, int M) { return div_up(M > 0 ? M : 1, 32) << r.twice; }
-// the label of a row of the piece, -1: takes no part
-__device__ __forceinline__ int label_of(const Rows& r, int row) {
-  if (r.count) return r.lab[r.p * r.P + row];
-  const int64_t y = r.label[row];
+// the label of a token, of a row of the piece, -1: takes no part
+__device__ __forceinline__ int label_at(const Rows& r, int t) {
+  const int64_t y = r.label[t];
   return y >= 0 && y < r.V ? (int)y : -1;
+}
+__device__ __forceinline__ int label_of(const Rows& r, int row) {
+  return r.count ? r.lab[r.p * r.P + row] : label_at(r, r.p * r.P + row);
 }
 
 // row r of the tail of W: the rows from V / 32 * 32 on, zeros behind the last (see input_grad_body)
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
   }
   if (sl != 0 || row >= M) return;
   v = part[0][r];
-  const int t = rows.count ? rows.idx[rows.p * P + row] : row, y = label_of(rows, row);
+  const int at_piece = rows.p * P + row, t = rows.count ? rows.idx[at_piece] : at_piece, y = label_of(rows, row);
   if (y < 0) {                                    // (not gathered) whatever its logits were
     loss[t] = 0.f;
     if (lse) lse[t] = 0.f;
@@ -356,10 +358,10 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
 // Bound by memory: 7783 rows of V 128000 780 us, 5.1 TB/s, a large copy's rate.
 // 64 rows to a block, four lanes to a row's 64 bytes of a block of columns, `per` strips one after the other.  Rows that take no part, and those
 // from the last one up to whole tiles of 32, become zeros, of dz here and of the copy of x that the weight gradient's product walks over.
-// Two parts (`twice`: an update by up to 256 rows, dW of up to 64): what dz loses to bf16 is rounded itself and stands, with the same rows of x,
-// behind the rows, so that dW has 16 bits of the labels' entries, which are most of it, and the 11 of e of the others - the fp32 master would
-// otherwise be off by up to 2^-9 of a single token's whole step.  The product is bound by the weights there; with many rows it would take
-// twice as long, and what one of them is off by is small against the step of all.
+// Two parts (`twice`: an update by a batch of up to 256 rows, dW of up to 64, however they are cut into pieces): what dz loses to bf16 is rounded
+// itself and stands, with the same rows of x, behind the rows, so that dW has 16 bits of the labels' entries, which are most of it, and the 11
+// of e of the others - the fp32 master would otherwise be off by up to 2^-9 of a single token's whole step.  The product is bound by the weights
+// there.  Larger batches would pay for it with another product of dW's size, and have the one rounding that a stage's own gradients have.
 // Where rows are not gathered the copy is made here, by the blocks behind the strips', and the tail of W by those behind them.
 __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info, Rows rows,
                                                  int strips, int per, int strip_blocks, uint16_t* __restrict__ xw, int d, const uint16_t* __restrict__ x,
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
   const int per = d / 8;
   const bool in = chunk < (int64_t)rows.T * per;
   const int t = in ? (int)(chunk / per) : 0, c = in ? (int)(chunk - (int64_t)t * per) * 8 : 0;
-  const int j = !in ? -1 : rows.count ? rows.pos[t] : label_of(rows, t) >= 0 ? t : -1;
+  const int j = !in ? -1 : rows.count ? rows.pos[t] : label_at(rows, t) >= 0 ? t : -1;
   const bool here = j >= 0 && j / P == p;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   if (here) {
@@ -550,8 +552,9 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
   const int k0 = nk * s / parts, k1 = nk * (s + 1) / parts;
   auto tile = [&](auto rows_of_tile, int bm) {
     constexpr int BT = rows_of_tile;
-    auto own = [&](const auto& acc, int m0, int n0, int wm0, int wn0) {
+    auto own = [&](const auto& acc, int, int n0, int wm0, int wn0) {
       constexpr int TM = BT / 2 / 16, TN = WB / (W_NW / 2) / 16;
+      const int m0 = bm * BT;
       Epi o{};
       o.ldo = d;
       if constexpr (KIND == 0) {
@@ -573,9 +576,11 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
         f32_tile_through_lds<BT, WB, W_NW, f32x4, TM, TN, 3, false>(acc, o, m0, n0, wm0, wn0, V, d, dtl_smem);
       }
     };
-    // (the loads of dz run over whole strips, the results end at V)
-    gemm_dtl_body<BT, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)k0 * 32 * 32, 32, bs, a.xw + (int64_t)k0 * 32 * 32, 32, bs, Vp, d,
-                                                               (k1 - k0) * 32, bm, bn, Epi{}, nullptr, 0, own);
+    // (The loads of dz run over whole strips, the results end at V.  The tile's first column of dz is its base: offsets from the matrix's own
+    // would pass 31 bits from 2^31 elements of e on.)
+    gemm_dtl_body<BT, WB, 32, W_NS, W_NW, true, true, EPI_OWN>(a.dz + (int64_t)(bm * BT / 32) * bs + (int64_t)k0 * 32 * 32, 32, bs,
+                                                               a.xw + (int64_t)k0 * 32 * 32, 32, bs, Vp - bm * BT, d, (k1 - k0) * 32, 0, bn, Epi{},
+                                                               nullptr, 0, own);
   };
   if (!kHalves || half < 0) tile(std::integral_constant<int, WB>{}, bm);
   else if (kHalves && (2 * bm + half) * (WB / 2) < V) tile(std::integral_constant<int, WB / 2>{}, 2 * bm + half);
@@ -666,7 +671,7 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   const int64_t P = tiles((T + q.pieces - 1) / q.pieces);
   q.pieces = (int)((T + P - 1) / P);
   q.P = (int)P;
-  q.few = q.pieces == 1 && T <= kFewRows && 2 * P * q.Vp < (1ll << 31);   // (offsets, with dz in two parts)
+  q.few = T <= kFewRows;
   q.R = q.few && grads ? 2 * q.P : q.P;
   size_t at = 0;
   q.count = q.pos = q.idx = q.lab = q.xw = q.info = q.tail = q.e = q.part = q.acc = 0;
@@ -675,7 +680,7 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   if (!q.few) { q.count = take(4); q.pos = take(4 * all); q.idx = take(4 * all); q.lab = take(4 * all); }
   q.target = take(4 * P);
   q.stat = take((size_t)8 * (q.Vp / STRIP) * P);
-  if (!q.few || grads) q.xw = take((size_t)2 * q.pieces * q.R * d);
+  if (!q.few || grads) q.xw = take((size_t)2 * (q.few ? 1 : q.pieces) * q.R * d);
   if (grads) {
     q.info = take(sizeof(RowInfo) * P);
     q.tail = take((size_t)2 * 64 * ldw);
@@ -706,10 +711,15 @@ Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
   return r;
 }
 
+// the copy of the piece's rows of x
+uint16_t* copy_of_x(const Plan& q, char* work, int p) { return (uint16_t*)(work + q.xw) + (q.few ? 0 : (int64_t)p * q.P * q.d); }
+// its first row of x, where rows are not gathered
+const uint16_t* rows_of_x(const Plan& q, const rv_loss_desc& a, int p) { return (const uint16_t*)a.x + (int64_t)p * q.P * a.ldx; }
+
 template <bool STORE>
 rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const Rows& rows, hipStream_t st) {
   const uint16_t* w = (const uint16_t*)a.w;
-  const uint16_t* x = q.few ? (const uint16_t*)a.x : (const uint16_t*)(work + q.xw) + (int64_t)rows.p * q.P * q.d;
+  const uint16_t* x = q.few ? rows_of_x(q, a, rows.p) : copy_of_x(q, work, rows.p);
   const int64_t ldx = q.few ? a.ldx : 32, x_bs = q.few ? 32 : 32ll * q.P;
   const LogitsOut o{STORE ? (uint16_t*)(work + q.e) : nullptr, (float2*)(work + q.stat), (float*)(work + q.target), q.P, q.R, q.V, q.Vp};
   const int most = q.T < q.P ? q.T : q.P;
@@ -736,7 +746,7 @@ rv_status launch_512(const GradArgs& g, int grid, int lds, hipStream_t st) {
 template <int KIND>
 rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const Rows& rows, hipStream_t st) {
   GradArgs g{};
-  g.dz = (const uint16_t*)(work + q.e); g.xw = (const uint16_t*)(work + q.xw) + (int64_t)rows.p * q.P * q.d; g.w = (const uint16_t*)a.w;
+  g.dz = (const uint16_t*)(work + q.e); g.xw = copy_of_x(q, work, rows.p); g.w = (const uint16_t*)a.w;
   g.ldw = q.ldw; g.rows = rows; g.d = q.d; g.Vp = q.Vp;
   // (fewer tile rows than all rows have, more stretches: never more workgroups than this, nor more memory)
   g.S_dx = q.dx.S; g.tiles_m = div_up(q.T < q.P ? q.T : q.P, q.dx.tile);
@@ -814,7 +824,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
     const int per_dz = dz_blocks < 1 ? 1 : dz_blocks < 8 ? (int)dz_blocks : 8, strip_blocks = div_up(strips, per_dz);
     hipLaunchKernelGGL(dz_kernel, dim3(div_up(most, 64), strip_blocks + (q.few ? div_up(q.d / 32, 8) + tail_rows : 0)), dim3(256), 0, st,
                        (uint16_t*)(work + q.e), (const float2*)(work + q.stat), info, rows, strips, per_dz, strip_blocks,
-                       (uint16_t*)(work + q.xw) + (int64_t)p * q.P * q.d, q.d, (const uint16_t*)a.x, a.ldx, w, q.ldw, (uint16_t*)(work + q.tail));
+                       copy_of_x(q, work, p), q.d, rows_of_x(q, a, p), a.ldx, w, q.ldw, (uint16_t*)(work + q.tail));
     RV_TRY(rv_launch_status());
     if (!a.dw && !update) RV_TRY(launch_grads<-1>(q, work, a, rows, st));
     else if (p > 0) RV_TRY(launch_grads<3>(q, work, a, rows, st));

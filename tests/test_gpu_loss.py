@@ -444,3 +444,45 @@ def test_losses_of_certain_tokens():
     assert float(loss.cpu()[sure].max()) < 2.0 ** -22
     # of dz in such a row: the label's entry is the loss, all others together as much again
     assert float(dx.cpu()[sure].double().abs().max()) <= 2.0 ** -20 * float(w.double().abs().max())
+
+
+@pytest.mark.parametrize("T,d,V,rows", [(200, 128, 700, 128), (129, 64, 5000, 1), (256, 1024, 3000, 128), (130, 64, 1000, 64), (200, 192, 333, 0),
+                                         (140, 64, (1 << 22) + 100, 0), (3, 64, (1 << 24) - 1, 0)])
+def test_update_is_as_exact_however_it_is_cut(T, d, V, rows):
+    """The same bound as of few rows in one piece (test_update_of_few_rows_is_as_exact_as_its_master) where the rows are cut into pieces, by the caller or for
+    a long vocabulary; the chains of the softmax sum as in test_offsets_behind_31_bits, of the pieces' sums one addition more."""
+    g = torch.Generator(device="cuda").manual_seed(61)
+    master = torch.randn(V, d, generator=g, device="cuda") * 0.05
+    w = master.to(torch.bfloat16)
+    label = torch.randint(0, V, (T,), generator=g, device="cuda")
+    x = (torch.randn(T, d, generator=g, device="cuda") + torch.rand(T, 1, generator=g, device="cuda") * 6.0 / (0.05 * d) * (master[label] / 0.05)).to(torch.bfloat16)
+    label[T // 2], x[T // 2] = -1, float("nan")
+    loss, dx, new, version = rv.loss_step(x, w, label, scale=0.37, master=master, eta=2.0, rows=rows)
+    assert torch.equal(version, new.to(torch.bfloat16))
+    takes = label >= 0
+    x64 = torch.where(takes[:, None], x.double(), 0.0)
+    parts = [(v, min(v + (1 << 18), V)) for v in range(0, V, 1 << 18)]
+    lse, zmax = torch.full((T,), -math.inf, dtype=torch.float64, device="cuda"), 0.0
+    for a, b in parts:
+        w64 = w[a:b].double()
+        lse = torch.logaddexp(lse, torch.logsumexp(x64 @ w64.T, 1))
+        zmax = max(zmax, float((x64.abs() @ w64.abs().T).max()))
+    slack = 2 * (d + 8) * 2.0 ** -24 * zmax + (80 + V / 1024) * 2.0 ** -24 + 2.0 ** -22 * float(lse.abs().max())
+    weight = torch.where(takes, 0.37, 0.0).double()
+    ref_dx = torch.zeros_like(x64)
+    for a, b in parts:
+        z = x64 @ w[a:b].double().T
+        dz = torch.exp(z - lse[:, None])
+        rows_here = torch.nonzero((label >= a) & (label < b))[:, 0]
+        off = dz * (2.0 ** -11 + 2.0 ** -16 + 2 * slack) + 2.0 ** -40
+        dz[rows_here, label[rows_here] - a] -= 1.0
+        off[rows_here, label[rows_here] - a] = dz[rows_here, label[rows_here] - a].abs() * 2.0 ** -16 + slack
+        dz *= weight[:, None]
+        off *= weight[:, None]
+        step = dz.T @ x64
+        bound = 2.0 * ((off + dz.abs() * (T + 8) * 2.0 ** -23).T @ x64.abs()) + 2.0 ** -22 * (master[a:b].double().abs() + 2.0 * step.abs())
+        assert bool(((new[a:b].double() - (master[a:b].double() - 2.0 * step)).abs() <= bound).all()), (a, b)
+        ref_dx += dz @ w[a:b].double()
+    assert not dx[~takes].any() and not loss[~takes].any()
+    # dx has one rounding of dz and of itself: normwise far below 2^-7 of the terms
+    assert float((dx.double() - ref_dx).norm()) <= 2.0 ** -7 * float(ref_dx.norm())
