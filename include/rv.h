@@ -276,10 +276,13 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16: an element
  * of dx, dw or the step is off by up to 2^-8 of its terms.  An update by T <= 256 rows, and dw of T <= 64, take dz in two bf16 parts, 16 bits of
  * a label's entry and the 11 of their exponentials of the others: what a master gets is then no further off than that, whatever V and `rows`.
- *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 128 or a multiple of 256): bounds the work
- *             memory at about 2 V * rows bytes; with several such pieces dw is added up in fp32, 4 V d bytes more.
- *             0: as many as 2 GiB hold.  Outputs do not depend on it but for the order of those sums.
- *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).
+ *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 128 or a multiple of 256), which
+ *             bounds the work memory.  0: 2^30 / max(V, d), at least 128.  Outputs do not depend on it but for the order of fp32 sums.
+ *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).  With r rows at a
+ *             time that is up to V r / 8 bytes of softmax pairs and, where rows are gathered (T > 256), 2 T d of a copy of x and 12 T of places; a step takes
+ *             2 V r more for the exponentials (up to 4 V r if T <= 256: room for dz in two parts, and 4 d r for that copy of x), 4 d r for dx's fp32
+ *             sums, up to 1.25 GiB more where its product is cut into stretches of the vocabulary, 128 ldw for the last rows of w, and 4 V d if there are
+ *             several pieces of r rows.
  *             Nothing in it has to be kept between calls; calls that may run at one time need one each, and so do graphs
  *             that may be replayed at one time.
  * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8, ldx and ldw at most 2^20.  Outputs must not share memory

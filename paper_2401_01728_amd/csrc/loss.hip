@@ -20,8 +20,9 @@
 // p - 1 from a rounded p would have fewer digits where the model is nearly certain.
 // Computing z again for the gradients instead of keeping e would be a fourth product: 2 bytes of e written and 4 moved by the pass
 // that makes dz of it are 1.2 ps a logit at 5 TB/s, the product 2 d / 1.3 PFLOP/s = 1.6 ps at d 1024, 3.2 ps at 2048.
-// One piece of rows is kept at a time (e and strips of `rows` rows, at most 2 GiB of e where the caller leaves the choice), so the work
-// memory has a bound that does not grow with T; from the second piece on the weight gradient is added up in fp32.
+// One piece of rows is kept at a time (e, strips and dx's sums of `rows` rows; where the caller leaves the choice 2^30 elements of e or of dx at
+// most, but 128 rows at least, and twice that of e where a batch of up to 256 rows may need its dz in two parts), so what grows with T
+// is the copy of x alone; from the second piece on the weight gradient is added up in fp32.
 //
 // Rows whose label lies outside [0, V) - prompts, padding - take no part: a first kernel gathers the others, in order, into a copy of
 // x without gaps, in blocks of 32 columns (rv_mat), and all kernels behind it go by the number of rows it counted.  So a batch that is half
@@ -35,7 +36,7 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int STRIP = 64;
 constexpr int kTop = 15;                 // a strip's largest exponential is 2^15
-constexpr int64_t kMostE = 1ll << 30;    // elements of e of a piece's rows, where the caller leaves the choice
+constexpr int64_t kMostE = 1ll << 30;    // elements of e, and of dx, of a piece's rows, where the caller leaves the choice
 
 // what a row of the piece needs in the backward
 struct RowInfo { float top, g, at_label; int label; };    // largest logit; weight over the sum of exponentials; dz of the label
@@ -59,7 +60,7 @@ struct Rows {
   const int* count; const int* lab; const int* idx; const int* pos;
   const int64_t* label;
   int T, V, p, P;
-  int R;                                   // rows of a block of columns of e and of the copy of x: P, or 2 P for dz in two parts
+  int R;                                   // rows of a block of columns of e and of the copy of x: P, or more where dz may have two parts
   int twice;                               // dW of dz in two parts (dz_kernel)
 };
 constexpr int kFewRows = 256;
@@ -672,7 +673,9 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
   q.pieces = (int)((T + P - 1) / P);
   q.P = (int)P;
   q.few = T <= kFewRows;
-  q.R = q.few && grads ? 2 * q.P : q.P;
+  const int most_rows = q.T < q.P ? q.T : q.P;
+  const int both_parts = q.few && grads ? 2 * round_up(most_rows, 32) : 0;   // (rows of dz in two parts)
+  q.R = both_parts > q.P ? both_parts : q.P;
   size_t at = 0;
   q.count = q.pos = q.idx = q.lab = q.xw = q.info = q.tail = q.e = q.part = q.acc = 0;
   auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
@@ -685,10 +688,9 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
     q.info = take(sizeof(RowInfo) * P);
     q.tail = take((size_t)2 * 64 * ldw);
     q.e = take((size_t)2 * q.R * q.Vp);
-    const int most_rows = q.T < q.P ? q.T : q.P;
     q.dx = cut_form(most_rows, q.d, q.Vp / 32, true);
     q.part = take((size_t)div_up(most_rows, q.dx.tile) * q.dx.S * q.dx.tile * q.d * 4);
-    q.S_w = q.pieces > 1 ? 1 : cut_form(q.V, q.d, q.R / 32, false).S;
+    q.S_w = q.pieces > 1 ? 1 : cut_form(q.V, q.d, (q.few ? both_parts : q.P) / 32, false).S;
     q.acc = q.pieces > 1 || q.S_w > 1 ? take((size_t)4 * q.S_w * V * d) : 0;
   }
   q.bytes = at;
@@ -715,6 +717,9 @@ Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
 uint16_t* copy_of_x(const Plan& q, char* work, int p) { return (uint16_t*)(work + q.xw) + (q.few ? 0 : (int64_t)p * q.P * q.d); }
 // its first row of x, where rows are not gathered
 const uint16_t* rows_of_x(const Plan& q, const rv_loss_desc& a, int p) { return (const uint16_t*)a.x + (int64_t)p * q.P * a.ldx; }
+
+// stretches of dW's rows (the plan's are those of dz in two parts; the up to eight k-tiles of up to 256 rows in one part are one: cut_form)
+int weight_stretches(const Plan& q, const Rows& rows) { return q.few && !rows.twice ? 1 : q.S_w; }
 
 template <bool STORE>
 rv_status launch_logits(const Plan& q, char* work, const rv_loss_desc& a, const Rows& rows, hipStream_t st) {
@@ -752,10 +757,10 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
   g.S_dx = q.dx.S; g.tiles_m = div_up(q.T < q.P ? q.T : q.P, q.dx.tile);
   g.dx_grid = a.dx ? g.tiles_m * div_up(q.d, q.dx.tile) * q.dx.S : 0;
   g.tail = (const uint16_t*)(work + q.tail); g.part = (float*)(work + q.part);
-  g.S_w = q.S_w; g.sums = (float*)(work + q.acc);
+  g.S_w = weight_stretches(q, rows); g.sums = (float*)(work + q.acc);
   g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version;
   g.scale = a.scale; g.eta = a.eta * a.scale;
-  const int w_tiles = div_up(q.V, WB) * div_up(q.d, WB), w_grid = KIND == 2 ? w_tiles * q.S_w : halved_grid(w_tiles);
+  const int w_tiles = div_up(q.V, WB) * div_up(q.d, WB), w_grid = KIND == 2 ? w_tiles * g.S_w : halved_grid(w_tiles);
   // together, but for an update in place: dx reads the weights that it overwrites
   const bool both = KIND >= 0 && a.dx && q.dx.tile == 128 &&
                     !(KIND == 1 && rv_overlap(a.w, 2 * (size_t)q.V * q.ldw, a.version, 2 * (size_t)q.V * q.d));
@@ -809,7 +814,8 @@ rv_status run(const rv_loss_desc& a, bool grads) {
     RV_TRY(rv_launch_status());
   }
   const int strips = q.Vp / STRIP, most = q.T < q.P ? q.T : q.P;
-  const bool cut = q.pieces > 1 || (grads && q.S_w > 1);      // dW through fp32 sums
+  const int S_w = grads ? weight_stretches(q, rows_at(q, work, a, 0)) : 1;
+  const bool cut = q.pieces > 1 || S_w > 1;                   // dW through fp32 sums
   for (int p = 0; p < q.pieces; ++p) {
     const Rows rows = rows_at(q, work, a, p);
     if (grads) RV_TRY(launch_logits<true>(q, work, a, rows, st));
@@ -834,7 +840,7 @@ rv_status run(const rv_loss_desc& a, bool grads) {
   }
   if (grads && (a.dw || update) && cut) {
     const int64_t n = (int64_t)q.V * q.d;
-    hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, (const float*)(work + q.acc), q.S_w,
+    hipLaunchKernelGGL(weight_grad_join_kernel, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, (const float*)(work + q.acc), S_w,
                        rows_at(q, work, a, 0), q.pieces, n, (uint16_t*)a.dw, a.master, a.master_out, (uint16_t*)a.version, a.scale, a.eta * a.scale);
     RV_TRY(rv_launch_status());
   }

@@ -486,3 +486,14 @@ def test_update_is_as_exact_however_it_is_cut(T, d, V, rows):
     assert not dx[~takes].any() and not loss[~takes].any()
     # dx has one rounding of dz and of itself: normwise far below 2^-7 of the terms
     assert float((dx.double() - ref_dx).norm()) <= 2.0 ** -7 * float(ref_dx.norm())
+
+
+@pytest.mark.parametrize("T,d,V", [(256, 128, 700), (241, 320, 1300), (97, 64, 300), (65, 192, 1000)])
+def test_room_for_two_parts(T, d, V):
+    """Blocks of as many rows as two parts need (192 and more), an update whose walk over them is cut and the gradient alone, whose is not."""
+    x, w, label, master = _inputs(71, T, d, V, 0.2)
+    g = torch.full((T,), 0.5)
+    loss, dx, dw = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.5)
+    _check(x, w, label, g, loss, None, dx, dw)
+    loss, dx, new, version = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.5, master=master.cuda(), eta=0.1)
+    _check(x, w, label, g, loss, None, dx, None, master, 0.1, new, version)

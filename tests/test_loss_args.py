@@ -71,3 +71,35 @@ def test_too_little_work_memory():
 
 def test_null_description():
     assert _lib.lib().rv_loss_step(None) == INVAL and _lib.lib().rv_loss_forward(None) == INVAL
+
+
+def _documented(T, d, V, rows, gradients):
+    """What rv.h says the work memory is at most, but for the rounding of each of 14 parts to 256 bytes."""
+    most = max(128, (1 << 30) // max(V, d))
+    r = min(most if rows == 0 else rows, T)
+    r = 128 if r <= 128 else (r + 255) // 256 * 256
+    n = (V + 63) // 8 * r
+    if T > 256:
+        n += (T + r) * (2 * d + 12)
+    if gradients:
+        n += (4 if T <= 256 else 2) * (V + 63) * r + (4 * d * r if T <= 256 else 0) + 4 * d * r + (5 << 28) + 128 * d + 24 * r
+        n += 4 * V * d if r < T else 0
+    return n + 24 * r + 14 * 256
+
+
+@pytest.mark.parametrize("T,d,V,rows", [
+    (1, 64, 1, 0), (3, 64, 5_000_000, 0), (256, 64, 4_000_000, 0), (200, 64, 4_000_000, 128), (130, 64, (1 << 24) - 1, 0), (256, 16384, 131071, 0), (257, 16384, 131071, 0),
+    (1 << 18, 4096, 1000, 0), (1 << 20, 16384, 64, 0), (827556, 16192, 112020, 0), (5000, 2048, 128000, 1000), (1 << 20, 64, 1 << 20, 1 << 20)])
+def test_work_memory_is_what_the_header_says(T, d, V, rows):
+    for gradients in (0, 1):
+        st, n = _work(T, d, V, d, rows, gradients)
+        assert st == OK and n <= _documented(T, d, V, rows, gradients), (gradients, n, _documented(T, d, V, rows, gradients))
+
+
+@pytest.mark.parametrize("T", [1, 3, 64])
+def test_few_rows_do_not_take_twice_the_exponentials(T):
+    """Two parts of 64 rows have room in the 128 of a tile."""
+    V, d = 5_000_000, 64
+    assert _work(T, d, V, d)[1] <= (2 * V + V // 8) * 128 + (5 << 28)
+    n = [_work(t, d, V, d)[1] for t in (64, 128)]
+    assert n[1] - n[0] >= 2 * V * 128
