@@ -44,10 +44,17 @@ struct CrossArgs {
   float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
 };
 
-__device__ __forceinline__ int keys_of(const CrossArgs& a, int b) {
+__device__ __forceinline__ int keys_at(const CrossArgs& a, int b) {
   if (!a.klen) return a.Sk;
-  const int n = __builtin_amdgcn_readfirstlane(a.klen[b]);
+  const int n = a.klen[b];
   return n < 0 ? 0 : n < a.Sk ? n : a.Sk;
+}
+__device__ __forceinline__ int keys_of(const CrossArgs& a, int b) { return __builtin_amdgcn_readfirstlane(keys_at(a, b)); }   // (b: wave-uniform)
+// What the sums over n keys end with, from their running maximum m and sum tot: the factor of the output and the row's log2-sum.  Without
+// keys 0 and -inf; keys whose scores are all -inf have no softmax, 0 / 0, and the backward has to see that.
+__device__ __forceinline__ float inverse(int n, float tot) { return n == 0 ? 0.f : 1.0f / tot; }
+__device__ __forceinline__ float log2_sum(int n, float m, float tot) {
+  return n == 0 ? -INFINITY : tot == 0.f ? NAN : m + __builtin_amdgcn_logf(tot);   // v_log_f32 is log2
 }
 // element offset of row r of (b, hkv) in a matrix of tokens whose rows are ld apart, heads of DH columns
 template <int DH>
@@ -258,7 +265,7 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, int k
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
   mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-  const float mn = fmaxf(m, mx * c2), base = mn == -INFINITY ? 0.f : mn;   // (scores of -inf alone: no probability, no NaN)
+  const float mn = fmaxf(m, mx * c2), base = mn == -INFINITY ? 0.f : mn;   // (scores of -inf alone so far: nothing yet)
   const float alpha = __builtin_amdgcn_exp2f(m - base);
   m = mn;
   float ps = 0.f;
@@ -344,8 +351,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
   if (!active || r >= a.R) return;
   const float tot = lsum + __shfl_xor(lsum, 32, 64);
   if (parts == 1) {
-    store_owned<DH>(o, tot == 0.f ? 0.f : 1.0f / tot, a.out + row_at<DH>(a, w.b, w.h, r, a.ldo));
-    if (grp == 0) a.lse2[(int64_t)w.unit * a.R + r] = m + __builtin_amdgcn_logf(tot);     // v_log_f32 is log2
+    store_owned<DH>(o, inverse(n, tot), a.out + row_at<DH>(a, w.b, w.h, r, a.ldo));
+    if (grp == 0) a.lse2[(int64_t)w.unit * a.R + r] = log2_sum(n, m, tot);
   } else {
     const int64_t at = ((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r;
     store_owned32<DH>(o, a.part + at * DH);
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
   }
   if (r >= a.R) return;
   const int64_t at = ((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + r;
-  const float inv = tot == 0.f ? 0.f : 1.0f / tot;
+  const float inv = inverse(n, tot);
   uint16_t* out = a.out + row_at<DH>(a, w.b, w.h, r, a.ldo);
   constexpr int PER = DH / 2 / TOKEN_NW;                 // registers of a wave's share
 #pragma unroll
@@ -457,7 +464,7 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
   }
   if (wave != 0 || grp != 0) return;
   if (parts > 1) a.part_ml[at] = float2{top, tot};
-  else a.lse2[(int64_t)w.unit * a.R + r] = top + __builtin_amdgcn_logf(tot);
+  else a.lse2[(int64_t)w.unit * a.R + r] = log2_sum(n, top, tot);
 }
 
 // parts -> out, lse2.  Eight columns to a lane; LANES lanes share the parts of one (a chain of up to 64 round trips else: single tokens of 8
@@ -498,17 +505,17 @@ __global__ __launch_bounds__(256) void cross_join_kernel(CrossArgs a) {
     for (int x = 1; x < LANES; ++x) add(pairs[threadIdx.x + x * W], sums[0][threadIdx.x + x * W], sums[1][threadIdx.x + x * W]);
   }
   if (row >= rows) return;
-  const float inv = tot == 0.f ? 0.f : 1.0f / tot;
+  const int unit = (int)(row / a.R), r = (int)(row - (int64_t)unit * a.R), n = keys_at(a, unit / a.Hkv);
+  const float inv = inverse(n, tot);
   v[0] *= inv; v[1] *= inv;
-  const int unit = (int)(row / a.R), r = (int)(row - (int64_t)unit * a.R);
   *reinterpret_cast<u32x4*>(a.out + row_at<DH>(a, unit / a.Hkv, unit % a.Hkv, r, a.ldo) + c) = f32_to_bf16x8(v);
-  if (c == 0) a.lse2[row] = m + __builtin_amdgcn_logf(tot);
+  if (c == 0) a.lse2[row] = log2_sum(n, m, tot);
 }
 
 // ---- backward ----------------------------------------------------------------------------------
 // What the accumulators of the scores and of do v^T begin with, for every row in the order of the list: -lse / c2, so that a probability is
-// exp2(c2 acc), and -D = -rowsum(do o), so that acc is dp - D.  Behind the last row, for a row without keys and for one with scores of -inf
-// alone -inf, which makes the probabilities zero, and 0.
+// exp2(c2 acc), and -D = -rowsum(do o), so that acc is dp - D.  Behind the last row and for a row without keys -inf, which makes the
+// probabilities zero, and 0.
 template <int DH>
 __global__ __launch_bounds__(256) void cross_stat_kernel(CrossArgs a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (DH / 8);

@@ -299,3 +299,86 @@ def test_one_key(B, Sq, Sk, dh, klen):
                 assert not dk[b].any()
     assert bool(torch.isnan(dq[0, 3]).all()) and bool(torch.isnan(dk[0, 0]).all())
     assert bool(torch.isfinite(dv[1:]).all())
+
+
+def _near_where_finite(got, ref, bound):
+    got = got.to(ref.device).double()
+    there = torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), there)
+    assert bool(((got - ref).abs() <= bound)[there].all())
+
+
+def _run(q, k, v, do, H, Hkv, klen):
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    length = torch.tensor(klen, dtype=torch.int32).cuda() if klen is not None else None
+    out, lse2 = kernels.cross_attention_fwd(q, k, v, H, Hkv, length)
+    return (out, lse2) + kernels.cross_attention_bwd(q, k, v, out, do, lse2, H, Hkv, length)
+
+
+# single tokens in one walk and in parts; few and many rows, in parts and not; both widths of a head
+INFINITE = [(2, 1, 40, 4, 2, 64), (2, 1, 40, 4, 2, 128), (2, 1, 3000, 4, 2, 64), (2, 2, 3000, 4, 2, 128), (2, 50, 200, 4, 2, 64), (2, 50, 200, 4, 2, 128),
+            (2, 70, 3000, 4, 2, 64), (2, 300, 1500, 4, 2, 128)]
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh", INFINITE)
+@pytest.mark.parametrize("at", ["first", "middle", "last"])
+def test_a_key_of_scores_of_minus_infinity(B, Sq, Sk, H, Hkv, dh, at):
+    """Every score of one key of the first head is -inf: what is finite is what it is without that key."""
+    klen = [Sk - 3, Sk]
+    q, k, v, do, n = _inputs(21, B, Sq, Sk, H, Hkv, dh, klen)
+    j, share = {"first": 0, "middle": n[0] // 2, "last": n[0] - 1}[at], H // Hkv
+    q, k = q.clone(), k.clone()
+    for h in range(share):
+        q[0, :, h * dh + 5] = q[0, :, h * dh + 5].abs() + 0.125
+    others = [x for x in range(Sk) if x != j]
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q[:1], k[:1, others], v[:1, others], do[:1], [n[0] - 1], H, Hkv)
+    k[0, j, 5] = -math.inf
+    got_out, got_lse, got_dq, got_dk, got_dv = _run(q, k, v, do, H, Hkv, klen)
+    first = slice(0, share * dh)                         # (the other heads have that key)
+    _near_where_finite(got_out[:1, :, first], out[..., first], e_out[..., first])
+    assert float((got_lse[:1, :share].cpu().double() - lse2[:, :share]).abs().max()) <= 2.0 ** -12
+    for h in range(share):
+        dq[..., h * dh + 5] = math.nan                  # 0 times -inf
+    _near_where_finite(got_dq[:1, :, first], dq[..., first], e_dq[..., first])
+    for got, ref, bound in ((got_dk, dk, e_dk), (got_dv, dv, e_dv)):
+        _near_where_finite(got[:1, others, :dh], ref[..., :dh], bound[..., :dh])
+        assert not got[0, j, :dh].any()
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh", INFINITE)
+def test_a_row_of_scores_of_minus_infinity(B, Sq, Sk, H, Hkv, dh):
+    """It has no softmax: NaN, for itself and, in the backward, for the keys it shares with others; other rows, heads and sequences are what they were."""
+    klen = [Sk - 3, Sk]
+    q, k, v, do, n = _inputs(22, B, Sq, Sk, H, Hkv, dh, klen)
+    q, k = q.clone(), k.clone()
+    k[0, :, 5] = -k[0, :, 5].abs() - 0.125
+    r = Sq // 2
+    q[0, r, 5] = 0.0
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    q[0, r, 5] = math.inf
+    got_out, got_lse, got_dq, got_dk, got_dv = _run(q, k, v, do, H, Hkv, klen)
+    out[0, r, :dh], lse2[0, 0, r], dq[0, r, :dh] = math.nan, math.nan, math.nan
+    for t in (dk, dv):
+        t[0, :n[0], :dh] = math.nan
+    _near_where_finite(got_out, out, e_out)
+    _near_where_finite(got_lse, lse2, torch.full_like(lse2, 2.0 ** -12))
+    for got, ref, bound in ((got_dq, dq, e_dq), (got_dk, dk, e_dk), (got_dv, dv, e_dv)):
+        _near_where_finite(got, ref, bound)
+    assert bool(torch.isnan(got_out[0, r, :dh]).all()) and bool(torch.isnan(got_lse[0, 0, r])) and bool(torch.isnan(got_dq[0, r, :dh]).all())
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh", INFINITE)
+def test_an_infinite_value(B, Sq, Sk, H, Hkv, dh):
+    """Its column is not finite, for all rows of its heads; the others are what they were."""
+    klen = [Sk - 3, Sk]
+    q, k, v, do, n = _inputs(23, B, Sq, Sk, H, Hkv, dh, klen)
+    v = v.clone()
+    j = n[0] - 1
+    # (not so far behind that its probability is zero in fp32)
+    (out, lse2, _, _, _), (e_out, _, _, _) = _reference(q, k, v, do, n, H, Hkv)
+    v[0, j, dh + 9] = math.inf
+    got, got_lse = _run(q, k, v, do, H, Hkv, klen)[:2]
+    for h in range(H // Hkv, 2 * (H // Hkv)):
+        out[0, :, h * dh + 9] = math.inf
+    _near_where_finite(got, out, e_out)
+    assert float((got_lse.cpu().double() - lse2).abs().max()) <= 2.0 ** -12
