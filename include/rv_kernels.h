@@ -171,7 +171,7 @@ rv_status rv_k_attention_bwd_static(const void* qkv, const void* out, const void
  * A score of -inf is a probability of zero; a row with keys whose scores are all -inf, or one of +inf or NaN among them, has no softmax: out and
  * lse2 are NaN, and so is what the backward forms with them.  With an infinite operand a result that is infinite by definition may be NaN.
  * d_head is 64 or 128; the scale is 1 / sqrt(d_head); B, Sq, Sk are at least 1, of any size (B <= 2^20, Sq and Sk <= 2^24,
- * n_heads <= 2^16).  Pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (lse2, klen: 4).  The backward writes all of dq, dk
+ * n_heads <= 2^16, of a sequence's q and k up to 2^34 elements).  Pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (lse2, klen: 4).  The backward writes all of dq, dk
  * and dv, zeros for keys behind a sequence's; out and lse2 are the forward's.  Outputs must not share memory with inputs or one
  * another (but dk and dv may be columns of one matrix, and so may dq of a matrix with others).  No atomics: results do not vary.
  *   work               device, 256-byte aligned, rv_k_cross_attention_work bytes (0 in some forwards: NULL is fine then); nothing in it is

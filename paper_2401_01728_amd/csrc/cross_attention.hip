@@ -767,13 +767,17 @@ int parts_for(int64_t blocks, int64_t tiles, int64_t want, int64_t least) {
   return (int)(p < 1 ? 1 : p > kMostParts ? kMostParts : p);
 }
 
+// A launch of the runtime has fewer than 2^32 threads; a call of more is made for some of its sequences at a time.
+constexpr int64_t kMostThreads = 3ll << 30;
+
 struct CrossPlan {
   bool token;                              // up to 32 rows to a key/value head
   int R, Rp, fwd_parts, q_parts, kv_parts;
+  int at_once;                             // sequences
   size_t fwd_ml, fwd_bytes;                // forward: [sums][pairs]
   size_t d, part, kv_part, bwd_bytes;      // backward: [lse][D][sums of dq][of dk and dv]
 };
-bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh) {
+bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh, bool backward) {
   if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128)) return false;
   if (B > (1 << 20) || Sq > (1 << 24) || Sk > (1 << 24) || H > (1 << 16)) return false;
   const int64_t U = B * Hkv, R = H / Hkv * Sq;
@@ -787,6 +791,21 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   // 128, 2048 keys 250 / 231; 1500 of 12 heads over 400 60 / 53; 512 of 16 over 4, 577 keys, 8 sequences 91 / 97.  (256 for dQ, too: 162 rows
   // over up to 6893 keys 194 / 233.)
   p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(R, TILE), 256, 4);
+  // threads of the largest launch, a sequence; of blocks that are dealt out in groups (deal) up to eight for seven more
+  auto dealt = [&](int64_t blocks, int parts) { const int64_t n = blocks * parts; return Hkv * (n + (n < 8 ? n : 8) - 1); };
+  auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
+  int64_t threads;
+  if (backward) {
+    threads = larger(256 * (dealt(up(Sk, OWN * 4), p.kv_parts) + dealt(up(R, OWN * 4), p.q_parts)),
+                     512 * (dealt(up(Sk, OWN * 8), p.kv_parts) + dealt(up(R, OWN * 8), p.q_parts)));
+    threads = larger(threads, Hkv * p.Rp * (dh / 8));
+    if (p.kv_parts > 1) threads = larger(threads, Hkv * Sk * (dh / 4));
+  } else {
+    threads = 256 * (p.token ? dealt(1, p.fwd_parts) : dealt(up(R, OWN * 4), p.fwd_parts));
+    if (p.fwd_parts > 1) threads = larger(threads, Hkv * R * dh);
+  }
+  if (threads > kMostThreads) return false;
+  p.at_once = (int)(B < kMostThreads / threads ? B : kMostThreads / threads);
   auto round = [](size_t b) { return (b + 255) / 256 * 256; };
   const bool parts = p.fwd_parts > 1;
   p.fwd_ml = parts ? round((size_t)4 * p.fwd_parts * U * R * dh) : 0;
@@ -800,7 +819,7 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
 
 template <auto Kern>
 rv_status launch(const CrossArgs& a, int64_t grid, int threads, int lds, hipStream_t st) {
-  if (grid > 0x7FFFFFFF || rv_allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
+  if (rv_allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
   hipLaunchKernelGGL(Kern, dim3((unsigned)grid), dim3(threads), lds, st, a);
   return rv_launch_status();
 }
@@ -816,6 +835,18 @@ CrossArgs common_args(const CrossPlan& p, const void* q, int64_t ldq, const void
   a.B = B; a.Sq = Sq; a.Sk = Sk; a.share = H / Hkv; a.Hkv = Hkv; a.R = p.R; a.Rp = p.Rp;
   a.scale = 1.0f / sqrtf((float)dh);
   a.c2 = 1.4426950408889634f * a.scale;
+  return a;
+}
+
+// the sequences from b0 on, as many as go into a launch; the work memory of those before is free when they are done
+CrossArgs sequences(CrossArgs a, const CrossPlan& p, int b0) {
+  const int64_t q = (int64_t)b0 * a.Sq, k = (int64_t)b0 * a.Sk;
+  a.B = a.B - b0 < p.at_once ? a.B - b0 : p.at_once;
+  a.q += q * a.ldq; a.k += k * a.ldk; a.v += k * a.ldv;
+  if (a.klen) a.klen += b0;
+  a.lse2 += (int64_t)b0 * a.Hkv * a.R;
+  if (a.out) a.out += q * a.ldo;
+  if (a.o) { a.o += q * a.ldo; a.dout += q * a.lddo; a.dq += q * a.lddq; a.dk += k * a.lddk; a.dv += k * a.lddv; }
   return a;
 }
 
@@ -852,7 +883,6 @@ rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) 
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
   RV_TRY((launch<cross_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
   const int64_t kv = deal(a.bkv, a, up(a.Sk, OWN * NW), p.kv_parts), q = deal(a.bq, a, up(a.R, OWN * NW), p.q_parts);
-  if (kv > 0x3FFFFFFF || q > 0x3FFFFFFF) return RV_E_INVAL;
   a.kv_grid = (int)kv;
   RV_TRY((launch<cross_bwd_kernel<DH, NW, NS_KV>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, NS_KV>, st)));
   if (p.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
@@ -864,7 +894,7 @@ rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) 
 
 extern "C" rv_status rv_k_cross_attention_work(int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, int backward, size_t* bytes) {
   CrossPlan p;
-  if (!bytes || !make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  if (!bytes || !make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head, backward != 0)) return RV_E_INVAL;
   *bytes = backward ? p.bwd_bytes : p.fwd_bytes;
   return RV_OK;
 }
@@ -873,14 +903,18 @@ extern "C" rv_status rv_k_cross_attention_fwd(const void* q, int64_t ldq, const 
                                               void* out, int64_t ldo, float* lse2, int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head,
                                               void* work, size_t work_bytes, void* stream) {
   CrossPlan p;
-  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head, false)) return RV_E_INVAL;
   const int64_t cols = (int64_t)n_heads * d_head, kcols = (int64_t)n_kv_heads * d_head;
   if (bad(q, 16) || bad(k, 16) || bad(v, 16) || bad(out, 16) || bad(lse2, 4) || ((uintptr_t)klen & 3)) return RV_E_INVAL;
   if (bad_pitch(ldq, cols) || bad_pitch(ldk, kcols) || bad_pitch(ldv, kcols) || bad_pitch(ldo, cols)) return RV_E_INVAL;
   if (p.fwd_bytes && (bad(work, 256) || work_bytes < p.fwd_bytes)) return RV_E_INVAL;
   CrossArgs a = common_args(p, q, ldq, k, ldk, v, ldv, klen, B, Sq, Sk, n_heads, n_kv_heads, d_head);
   a.out = (uint16_t*)out; a.ldo = ldo; a.lse2 = lse2;
-  return d_head == 64 ? forward<64>(a, p, (char*)work, (hipStream_t)stream) : forward<128>(a, p, (char*)work, (hipStream_t)stream);
+  for (int b = 0; b < B; b += p.at_once) {
+    const CrossArgs some = sequences(a, p, b);
+    RV_TRY(d_head == 64 ? forward<64>(some, p, (char*)work, (hipStream_t)stream) : forward<128>(some, p, (char*)work, (hipStream_t)stream));
+  }
+  return RV_OK;
 }
 
 extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* klen,
@@ -888,7 +922,7 @@ extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const 
                                               void* dk, int64_t lddk, void* dv, int64_t lddv, int B, int Sq, int Sk, int n_heads, int n_kv_heads,
                                               int d_head, void* work, size_t work_bytes, void* stream) {
   CrossPlan p;
-  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head)) return RV_E_INVAL;
+  if (!make_cross_plan(p, B, Sq, Sk, n_heads, n_kv_heads, d_head, true)) return RV_E_INVAL;
   const int64_t cols = (int64_t)n_heads * d_head, kcols = (int64_t)n_kv_heads * d_head;
   if (bad(q, 16) || bad(k, 16) || bad(v, 16) || bad(out, 16) || bad(dout, 16) || bad(lse2, 4) || bad(dq, 16) || bad(dk, 16) || bad(dv, 16) ||
       ((uintptr_t)klen & 3)) return RV_E_INVAL;
@@ -903,7 +937,13 @@ extern "C" rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const 
   // two workgroups of four with a slot each where one is short of work or ends early.  us, eight / four: 4 x 4096 x 4096 tokens, 16 heads (2048
   // workgroups of eight) 1711 / 1830; 162 tokens of 32 heads over 16 and up to 6893 keys (1184) 223 / 195; 1024 of 16 over 4 and up to 2048
   // (384) 219 / 193.  Heads of 64 are faster with four: three waves to a SIMD, 4 x 4096 x 4096 892 / 979.
-  if (d_head == 64) return backward<64, 4, 2>(a, p, (char*)work, st);
   const int64_t eights = (int64_t)B * n_kv_heads * (up(Sk, 8 * OWN) * p.kv_parts + up(p.R, 8 * OWN) * p.q_parts);
-  return p.R > 4 * OWN && Sk > 4 * OWN && eights >= 1536 ? backward<128, 8, 2>(a, p, (char*)work, st) : backward<128, 4, 1>(a, p, (char*)work, st);
+  const bool by_eight = p.R > 4 * OWN && Sk > 4 * OWN && eights >= 1536;
+  for (int b = 0; b < B; b += p.at_once) {
+    const CrossArgs some = sequences(a, p, b);
+    RV_TRY(d_head == 64 ? (backward<64, 4, 2>(some, p, (char*)work, st))
+           : by_eight   ? (backward<128, 8, 2>(some, p, (char*)work, st))
+                        : (backward<128, 4, 1>(some, p, (char*)work, st)));
+  }
+  return RV_OK;
 }

@@ -54,3 +54,16 @@ def test_too_little_work_memory():
     assert _lib.lib().rv_k_cross_attention_fwd(*(dict(token, work=None)[n] for n in NAMES)) == INVAL
     need = _work(backward=1)[1]
     assert _lib.lib().rv_k_cross_attention_bwd(*(dict(GOOD, bytes=need - 1)[n] for n in BWD)) == INVAL
+
+
+def test_a_sequence_larger_than_a_launch():
+    """Its statistics would be 2^34 threads: refused for the backward, with the size of the work memory already.  Up to 2^34 elements all is taken,
+    and so are sequences that are too many for one launch."""
+    large = dict(B=1, Sq=1 << 24, Sk=100, H=64, Hkv=64, dh=128)
+    assert _work(**large)[0] == OK and _work(backward=1, **large) == (INVAL, 0)
+    args = dict(GOOD, B=1, Sq=1 << 24, H=64, Hkv=64, dh=128, ldq=8192, ldk=8192, ldv=8192, ldo=8192, lddo=8192, lddq=8192, lddk=8192, lddv=8192, bytes=1 << 62)
+    assert _lib.lib().rv_k_cross_attention_bwd(*(args[n] for n in BWD)) == INVAL
+    for some in (dict(B=1, Sq=1 << 24, Sk=1 << 24, H=8, Hkv=8, dh=128), dict(B=1, Sq=1 << 11, Sk=1 << 11, H=1 << 16, Hkv=1 << 16, dh=128),
+                 dict(B=1, Sq=1 << 12, Sk=1 << 12, H=1 << 16, Hkv=1 << 16, dh=64), dict(B=1 << 20, Sq=1, Sk=1, H=16, Hkv=16, dh=64),
+                 dict(B=1 << 20, Sq=1, Sk=1, H=64, Hkv=8, dh=128)):
+        assert _work(**some)[0] == OK and _work(backward=1, **some)[0] == OK, some

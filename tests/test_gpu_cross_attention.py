@@ -382,3 +382,28 @@ def test_an_infinite_value(B, Sq, Sk, H, Hkv, dh):
         out[0, :, h * dh + 9] = math.inf
     _near_where_finite(got, out, e_out)
     assert float((got_lse.cpu().double() - lse2).abs().max()) <= 2.0 ** -12
+
+
+@pytest.mark.parametrize("lengths", [False, True])
+def test_more_sequences_than_a_launch_takes(lengths):
+    """2^20 sequences of one key and 16 heads are 2^32 threads and more.  A probability of 1 makes out the values, dv the output's gradient, dq and dk
+    zero, bit for bit; a score is off by (dh + 8) 2^-24 of its products' absolute sum, and by two roundings more in base 2."""
+    B, H, dh = 1 << 20, 16, 64
+    g = torch.Generator(device="cuda").manual_seed(24)
+    q, k, v, do = (torch.randn(B, 1, H * dh, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    n = torch.randint(0, 2, (B,), generator=g, device="cuda", dtype=torch.int32) if lengths else None
+    out, lse2 = kernels.cross_attention_fwd(q, k, v, H, H, n)
+    dq, dk, dv = kernels.cross_attention_bwd(q, k, v, out, do, lse2, H, H, n)
+    step = 1 << 16
+    for b in range(0, B, step):
+        part = slice(b, b + step)
+        here = torch.ones(step, dtype=torch.bool, device="cuda") if n is None else n[part] > 0
+        keep = here[:, None, None]
+        assert torch.equal(out[part], torch.where(keep, v[part], 0.0)), b
+        assert torch.equal(dv[part], torch.where(keep, do[part], 0.0)), b
+        assert not dq[part].any() and not dk[part].any(), b
+        x = (q[part].double() * k[part].double()).view(step, H, dh)
+        c2 = math.log2(math.e) / math.sqrt(dh)
+        ref, off = x.sum(-1) * c2, x.abs().sum(-1) * c2 * (dh + 8) * 2.0 ** -24 + 2.0 ** -22
+        got = lse2[part, :, 0].double()
+        assert bool(((got - ref).abs() <= off)[here].all()) and bool((got[~here] == -math.inf).all()), b
