@@ -407,3 +407,39 @@ def test_more_sequences_than_a_launch_takes(lengths):
         ref, off = x.sum(-1) * c2, x.abs().sum(-1) * c2 * (dh + 8) * 2.0 ** -24 + 2.0 ** -22
         got = lse2[part, :, 0].double()
         assert bool(((got - ref).abs() <= off)[here].all()) and bool((got[~here] == -math.inf).all()), b
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh,klen", [
+    (1, 50, 500, 2, 2, 64, None), (2, 1, 700, 4, 1, 128, [700, 412]), (2, 150, 900, 4, 2, 64, [500, 900]), (1, 300, 600, 4, 4, 128, None), (2, 64, 2000, 2, 1, 128, [2000, 413])])
+def test_gradients_of_scores_without_bounds(B, Sq, Sk, H, Hkv, dh, klen):
+    """Scores of thousands, where the backward's accumulators begin with as much of the other sign.  The bounds are those of ordinary scores: `slack` has
+    (dh + 8) 2^-24 of the largest sum of a score's absolute products, twice - of the score in the forward's lse and in the backward - which the
+    rounding of lse / c2 and of what begins with it, two of the sums' own, are inside."""
+    q, k, v, do, n = _inputs(25, B, Sq, Sk, H, Hkv, dh, klen)
+    k = k.clone()
+    k[:, 411] *= 400.0
+    k[:, 70] *= 100.0
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    got = _run(q, k, v, do, H, Hkv, klen)
+    for a, ref, bound in zip(got[:1] + got[2:], (out, dq, dk, dv), (e_out, e_dq, e_dk, e_dv)):
+        _near(a, ref, bound)
+    assert float(lse2.abs().max()) > 300.0
+    qh, kh = q.double().view(B, Sq, H, dh).transpose(1, 2), k.double().nan_to_num().reshape(B, Sk, Hkv, dh).transpose(1, 2).repeat_interleave(H // Hkv, 1)
+    off = (dh + 8) * 2.0 ** -24 * float((qh.abs() @ kh.abs().transpose(-1, -2)).max()) * math.log2(math.e) / math.sqrt(dh)
+    assert float((got[1].cpu().double() - lse2).abs().max()) <= 2.0 ** -12 + off
+
+
+# eight waves to a workgroup of the backward of heads of 128 (2400 of them and more; 1536 are enough): lengths that end everywhere, none, shared heads, rows that
+# end inside a wave's
+@pytest.mark.parametrize("Sq,Sk,H,Hkv", [(300, 1200, 32, 16), (777, 600, 24, 24), (90, 700, 160, 20)])
+def test_eight_waves_over_lengths(Sq, Sk, H, Hkv):
+    klen = [Sk, 0, 1, 63, 64, 65, 127, 128, 129, 255, 256, 257, Sk - 1, Sk // 2, 31, 32, 33, 2, Sk - 255, 511]
+    B, dh = len(klen), 128
+    share = H // Hkv
+    assert share * Sq > 128 and B * Hkv * (-(-Sk // 256) + -(-share * Sq // 256)) >= 2400
+    q, k, v, do, n = _inputs(26, B, Sq, Sk, H, Hkv, dh, klen)
+    q, k, v, do = q.cuda(), k.cuda().contiguous(), v.cuda().contiguous(), do.cuda()
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(q, k, v, do, n, H, Hkv)
+    got = _run(q, k, v, do, H, Hkv, klen)
+    for a, ref, bound in zip(got[:1] + got[2:], (out, dq, dk, dv), (e_out, e_dq, e_dk, e_dv)):
+        _near(a, ref, bound)
