@@ -497,3 +497,29 @@ def test_room_for_two_parts(T, d, V):
     _check(x, w, label, g, loss, None, dx, dw)
     loss, dx, new, version = rv.loss_step(x.cuda(), w.cuda(), label.cuda(), scale=0.5, master=master.cuda(), eta=0.1)
     _check(x, w, label, g, loss, None, dx, None, master, 0.1, new, version)
+
+
+@pytest.mark.parametrize("T,rows", [(200, 128), (130, 1), (256, 0), (600, 256)])
+def test_everything_over_its_input(T, rows):
+    """dx over x, the new master over the old and the version over w, the rows in one piece and in several."""
+    x, w, label, master = (t.cuda() for t in _inputs(81, T, 192, 1300, 0.2))
+    ref = rv.loss_step(x, w, label, master=master, eta=0.3, rows=rows)
+    got = rv.loss_step(x, w, label, master=master, eta=0.3, rows=rows, dx=x, master_out=master, version=w)
+    assert got[1] is x and got[2] is master and got[3] is w
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
+
+
+def test_no_row_of_a_few_takes_part():
+    """A batch that is not gathered, in two pieces, and one whose second piece alone takes part."""
+    T, d, V = 200, 64, 500
+    x, w, label, master = (t.cuda() for t in _inputs(82, T, d, V, 1.0))
+    loss, dx, new, version = rv.loss_step(x, w, label, master=master, eta=0.5, rows=128)
+    assert not loss.any() and not dx.any()
+    assert torch.equal(new, master) and torch.equal(version, master.to(torch.bfloat16))
+    x[150:] = 1.0
+    label[150:] = 7
+    ref = rv.loss_step(x, w, label, master=master, eta=0.5)
+    got = rv.loss_step(x, w, label, master=master, eta=0.5, rows=128)
+    assert torch.equal(got[0], ref[0]) and not got[1][:150].any() and bool(got[1][150:].any())
+    assert float((got[2] - ref[2]).abs().max()) <= 2.0 ** -20 * float(ref[2].abs().max())
