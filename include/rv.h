@@ -274,8 +274,8 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *             same call, master_out = master - eta * dz^T x (fp32), version = its bf16 rounding.  The product's fp32 sums are used,
  *             not their rounding.  master_out may be master, version may be w.
  * Products take bf16 operands with fp32 accumulation, as a decoder stage's; logits and softmax statistics are fp32, dz is bf16: an element
- * of dx, dw or the step is off by up to 2^-8 of its terms.  An update by T <= 256 rows, and dw of T <= 64, take dz in two bf16 parts, 16 bits of
- * a label's entry and the 11 of their exponentials of the others: what a master gets is then no further off than that, whatever V and `rows`.
+ * of dx or dw is off by up to 2^-8 of its terms.  Of an update the labels' entries of dz, which are most of it, have two bf16 parts, 16 bits; the
+ * others, too, where T <= 256 (and in dw where T <= 64): the 11 bits of their exponentials.  This does not depend on V or `rows`.
  *   rows      0, or the largest number of rows whose exponentials are kept at one time (rounded up to 128 or a multiple of 256), which
  *             bounds the work memory.  0: 2^30 / max(V, d), at least 128.  Outputs do not depend on it but for the order of fp32 sums.
  *   work      device, 256-byte aligned, of at least the size that rv_loss_work gives (gradients: nonzero for rv_loss_step).  With r rows at a

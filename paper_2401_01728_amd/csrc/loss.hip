@@ -362,7 +362,8 @@ __global__ __launch_bounds__(1024) void join_kernel(const float2* __restrict__ s
 // Two parts (`twice`: an update by a batch of up to 256 rows, dW of up to 64, however they are cut into pieces): what dz loses to bf16 is rounded
 // itself and stands, with the same rows of x, behind the rows, so that dW has 16 bits of the labels' entries, which are most of it, and the 11
 // of e of the others - the fp32 master would otherwise be off by up to 2^-9 of a single token's whole step.  The product is bound by the weights
-// there.  Larger batches would pay for it with another product of dW's size, and have the one rounding that a stage's own gradients have.
+// there.  Larger batches would pay for it with another product of dW's size; an update by them has the labels' entries alone in two parts
+// (labels_rest), the others with the one rounding that a stage's own gradients have.
 // Where rows are not gathered the copy is made here, by the blocks behind the strips', and the tail of W by those behind them.
 __global__ __launch_bounds__(256) void dz_kernel(uint16_t* __restrict__ e, const float2* __restrict__ stat, const RowInfo* __restrict__ info, Rows rows,
                                                  int strips, int per, int strip_blocks, uint16_t* __restrict__ xw, int d, const uint16_t* __restrict__ x,
@@ -461,6 +462,7 @@ struct GradArgs {
   int S_w, w_first;                       // dW; its workgroups in front of those of dx (both_grads_kernel)
   float* sums; uint16_t* dw; const float* master; float* master_out; uint16_t* version;
   float scale, eta;                       // eta: times scale
+  const RowInfo* info;                    // of an update by gathered rows (labels_rest), else null
 };
 // BM 256: tiles of 256x256, eight waves, in order of k; 128: of 128x128, the walk split over two groups of four waves.  The last k-tiles, which
 // end behind the last row of W, come from its copy with zeros behind (there is nothing behind W that could be read).  7783 rows, V 128000,
@@ -531,6 +533,115 @@ __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __res
 }
 
 // ---- dW ----------------------------------------------------------------------
+// What dz loses to bf16 at the labels, given back to an update of a master (gathered rows; up to 256 have all of dz in two parts).  A label's entry is
+// near -r, the others of its row add up to r: in the W row of a token that few others share its rounding is nearly all of the error, 2^-9 of
+// that token's step.  (The master of 257 rows of V 1000, d 128: 1.6e-5 of itself off without, 6e-7 with, update by 1 / 257 of 0.1.)
+// The tile's rows of W are the labels of a few rows only.  They are looked up, SEG rows at a time, in order; then a product of the usual
+// kind goes over them alone, 64 at a time: of a matrix that has the rest of dz, rounded to bf16, where the label is and zeros elsewhere, with the
+// same rows of x.  The first rows' labels are asked for ahead of the tile's walk, the next 64 rows of x ahead of the product of those before.
+// Bound by its chain of round trips, 2 to 3 us a tile.  The step without / with it, us: 4096 rows, V 32000, d 2048 1464 / 1474; 600, V 10000, d 512
+// 65.6 / 67.2; 2048, V 1000, d 512, a tile of which has 512 of the rows, 49.6 / 55.2.
+constexpr int SEG = 4096, REST = 64;
+template <int BT> constexpr int kRestLds = REST * (BT + 256) * 2 + SEG * 6 + 64;
+struct Labels { int label[SEG / 512]; float dz[SEG / 512]; };           // of a lane's rows of a segment
+__device__ __forceinline__ Labels ask_labels(const RowInfo* __restrict__ info, int seg0, int end) {
+  Labels s;
+#pragma unroll
+  for (int i = 0; i < SEG / 512; ++i) {
+    const int row = seg0 + ((threadIdx.x >> 6) * (SEG / 512) + i) * 64 + (threadIdx.x & 63);
+    s.label[i] = -1; s.dz[i] = 0.f;
+    if (row < end) { s.label[i] = info[row].label; s.dz[i] = info[row].at_label; }
+  }
+  return s;
+}
+template <int BT, int TM, int TN>
+__device__ __forceinline__ void labels_rest(const GradArgs& a, Labels seg, f32x4 (&acc)[TM][TN], int m0, int n0, int wm0, int wn0, int first, int end) {
+  char* const A = dtl_smem;
+  char* const B = A + REST * BT * 2;
+  int* const list = reinterpret_cast<int*>(B + REST * 256 * 2);         // row of the tile * SEG + row of the segment
+  uint16_t* const rest = reinterpret_cast<uint16_t*>(list + SEG);
+  int* const found = reinterpret_cast<int*>(rest + SEG);                // by the waves
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  const int64_t bs = 32ll * a.rows.R;
+  for (int seg0 = first; seg0 < end; seg0 += SEG) {
+    constexpr int PER = SEG / 512;
+    if (seg0 != first) seg = ask_labels(a.info, seg0, end);
+    int count = 0;
+    uint64_t who[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      who[i] = __builtin_amdgcn_ballot_w64((unsigned)(seg.label[i] - m0) < (unsigned)BT);
+      count += __popcll(who[i]);
+    }
+    __syncthreads();                                                    // the operands' ring, or the segment before, is done with
+    if (l == 0) found[wave] = count;
+    __syncthreads();
+    int to = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const int n = found[w];
+      to += w < wave ? n : 0;
+      total += n;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (who[i] >> l & 1) {
+        const int k = to + __popcll(who[i] & ((1ull << l) - 1));
+        list[k] = (seg.label[i] - m0) * SEG + (wave * PER + i) * 64 + l;
+        rest[k] = rv_f32_to_bf16(seg.dz[i] - __uint_as_float((uint32_t)rv_f32_to_bf16(seg.dz[i]) << 16));
+      }
+      to += __popcll(who[i]);
+    }
+    __syncthreads();
+    constexpr int XS = REST * 256 / 8 / 512;
+    u32x4 x[XS];
+    auto ask_rows = [&](int h0) {
+#pragma unroll
+      for (int i = 0; i < XS; ++i) {
+        const int c = (i * 512 + tid) % 32, k = h0 + (i * 512 + tid) / 32;
+        int col = n0 + c * 8;
+        col = col < a.d ? col : a.d - 8;
+        x[i] = u32x4{0u, 0u, 0u, 0u};
+        if (k < total) x[i] = *reinterpret_cast<const u32x4*>(a.xw + (col >> 5) * bs + (int64_t)(seg0 + list[k] % SEG) * 32 + (col & 31));
+      }
+    };
+    ask_rows(0);
+    for (int h0 = 0; h0 < total; h0 += REST) {
+      if (h0) __syncthreads();                                          // the 64 before are done with
+#pragma unroll
+      for (int i = 0; i < REST * BT / 8 / 512; ++i) {
+        const int c = (i * 512 + tid) % (BT / 8), k = (i * 512 + tid) / (BT / 8), col = h0 + k < total ? list[h0 + k] / SEG : -1;
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (col >> 3 == c) {
+          const uint32_t r = (uint32_t)rest[h0 + k] << 16 * (col & 1);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (col & 7) >> 1 == e ? r : 0u;
+        }
+        *reinterpret_cast<u32x4*>(A + k * (BT * 2) + ((c ^ km_swizzle<BT>(k & 31)) << 4)) = v;
+      }
+#pragma unroll
+      for (int i = 0; i < XS; ++i) {
+        const int c = (i * 512 + tid) % 32, k = (i * 512 + tid) / 32;
+        *reinterpret_cast<u32x4*>(B + k * 512 + ((c ^ km_swizzle<256>(k & 31)) << 4)) = x[i];
+      }
+      __syncthreads();
+      if (h0 + REST < total) ask_rows(h0 + REST);
+#pragma unroll 1
+      for (int k = 0; k < REST && h0 + k < total; k += 32) {
+        bf16x8 fa[TM], fb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = dtl_frag<true, BT, 32>(A + k * (BT * 2), wm0 + i * 16, 0);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) fb[j] = dtl_frag<true, 256, 32>(B + k * 512, wn0 + j * 16, 0);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      }
+    }
+  }
+}
+
 // 256x256 tiles, the contraction over the rows: 7783 rows, V 128000, d 2048 3.0 ms, 1.36 PFLOP/s; 2048, V 50257, d 1024 0.21 ms, 1.0 (788 tiles are
 // three rounds of the CUs and a twelfth, which is dealt out in halves); few rows are bound by writing dW: 5 rows of V 41302, d 704 with the update
 // 74 us with dx, 4.7 TB/s.
@@ -551,11 +662,15 @@ __device__ __forceinline__ void weight_grad_body(const GradArgs& a, int id) {
   const int s = id / tiles;
   const int in = id - s * tiles, bn = in % vn, bm = in / vn;
   const int k0 = nk * s / parts, k1 = nk * (s + 1) / parts;
+  const int first = k0 * 32, end = k1 * 32 < M ? k1 * 32 : M;
+  const bool labels = KIND != 0 && a.info;
+  const Labels seg = ask_labels(a.info, first, labels ? end : 0);
   auto tile = [&](auto rows_of_tile, int bm) {
     constexpr int BT = rows_of_tile;
-    auto own = [&](const auto& acc, int, int n0, int wm0, int wn0) {
+    auto own = [&](auto& acc, int, int n0, int wm0, int wn0) {
       constexpr int TM = BT / 2 / 16, TN = WB / (W_NW / 2) / 16;
       const int m0 = bm * BT;
+      if (labels) labels_rest<BT>(a, seg, acc, m0, n0, wm0, wn0, first, end);
       Epi o{};
       o.ldo = d;
       if constexpr (KIND == 0) {
@@ -700,7 +815,7 @@ bool make_plan(Plan& q, int64_t T, int64_t d, int64_t V, int64_t ldw, int64_t ro
 constexpr int kBigLds = 4 * 2 * dtl_tile_bytes(256, 32), kMidLds = 4 * 2 * dtl_tile_bytes(128, 32), kSplitLds = split_lds<128, 128, 2, 4>();
 constexpr int kWeightLds = WB * stage_pitch(WB) > upd_image_bytes(WB, WB) ? WB * stage_pitch(WB) : upd_image_bytes(WB, WB);
 constexpr int kBothLds = kSplitLds > kWeightLds ? kSplitLds : kWeightLds;
-static_assert(kWeightLds >= kBigLds && kBothLds <= 160 * 1024, "LDS of one CU");
+static_assert(kWeightLds >= kBigLds && kWeightLds >= kRestLds<WB> && kBothLds <= 160 * 1024, "LDS of one CU");
 
 Rows rows_at(const Plan& q, char* work, const rv_loss_desc& a, int p) {
   Rows r{};
@@ -760,6 +875,7 @@ rv_status launch_grads(const Plan& q, char* work, const rv_loss_desc& a, const R
   g.S_w = weight_stretches(q, rows); g.sums = (float*)(work + q.acc);
   g.dw = (uint16_t*)a.dw; g.master = a.master; g.master_out = a.master_out; g.version = (uint16_t*)a.version;
   g.scale = a.scale; g.eta = a.eta * a.scale;
+  g.info = a.master && rows.count ? (const RowInfo*)(work + q.info) : nullptr;
   const int w_tiles = div_up(q.V, WB) * div_up(q.d, WB), w_grid = KIND == 2 ? w_tiles * g.S_w : halved_grid(w_tiles);
   // together, but for an update in place: dx reads the weights that it overwrites
   const bool both = KIND >= 0 && a.dx && q.dx.tile == 128 &&

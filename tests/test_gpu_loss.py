@@ -523,3 +523,37 @@ def test_no_row_of_a_few_takes_part():
     got = rv.loss_step(x, w, label, master=master, eta=0.5, rows=128)
     assert torch.equal(got[0], ref[0]) and not got[1][:150].any() and bool(got[1][150:].any())
     assert float((got[2] - ref[2]).abs().max()) <= 2.0 ** -20 * float(ref[2].abs().max())
+
+
+# tiles of 256 and, where they are a last round, of 128; walks over the rows that are cut; several pieces; more labels of a tile than are looked up at a time;
+# one label for all; rows that take no part
+@pytest.mark.parametrize("T,d,V,rows,labels,out", [
+    (257, 128, 700, 0, "any", 0.0), (300, 64, 5000, 0, "any", 0.4), (600, 192, 9000, 256, "any", 0.1), (2000, 128, 300, 0, "few", 0.0), (5000, 64, 300, 0, "one", 0.0),
+    (10000, 64, 5000, 0, "any", 0.3), (10000, 64, 5000, 4500, "any", 0.0), (400, 4096, 4400, 0, "any", 0.2), (9000, 128, 600, 1024, "few", 0.0), (700, 64, 20, 0, "any", 0.0)])
+def test_labels_of_an_update_have_16_bits(T, d, V, rows, labels, out):
+    """Every row of x has one entry, 4, at a column that T / d rows share: logits are single products, and an element of the step has so many terms that are not zero.
+    Of dz an entry of a label is off by 2^-16 (two roundings to bf16) and what the loss is (39 additions of 2^-24 and 2^-20, see
+    test_logits_of_any_size), the others by 2^-8 and 2^-10 (bf16 behind fp16, with sum and factor); the weights of the rows are no powers of two."""
+    g = torch.Generator(device="cuda").manual_seed(91)
+    master = torch.randn(V, d, generator=g, device="cuda") * 0.5
+    w = master.to(torch.bfloat16)
+    x = torch.zeros(T, d, device="cuda")
+    t = torch.arange(T, device="cuda")
+    x[t, t * 7 % d] = 4.0
+    label = {"any": torch.randint(0, V, (T,), generator=g, device="cuda"), "few": t * 5 % 3 * (V // 4) + V // 8, "one": t * 0 + 7}[labels]
+    gone = torch.rand(T, generator=g, device="cuda") < out
+    label, x = torch.where(gone, -1, label), torch.where(gone[:, None], math.nan, x).to(torch.bfloat16)
+    weight = torch.rand(T, generator=g, device="cuda") + 0.5
+    _, _, new, version = rv.loss_step(x, w, label, scale=0.5, row_scale=weight, master=master, eta=2.0, rows=rows)
+    assert torch.equal(version, new.to(torch.bfloat16))
+    x64 = torch.where(gone[:, None], 0.0, x.double())
+    dz = torch.softmax(x64 @ w.double().T, 1)
+    off = dz * (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -12) + 2.0 ** -40
+    kept = torch.nonzero(~gone)[:, 0]
+    dz[kept, label[kept]] -= 1.0
+    off[kept, label[kept]] = dz[kept, label[kept]].abs() * 2.0 ** -16 + 39 * 2.0 ** -24 + 2.0 ** -20
+    r = torch.where(gone, 0.0, weight.double())[:, None]
+    dz, off = dz * r, off * r
+    step = dz.T @ x64
+    bound = (off + dz.abs() * (T // d + 40) * 2.0 ** -23).T @ x64.abs() + 2.0 ** -22 * (master.double().abs() + step.abs())
+    assert bool(((new.double() - (master.double() - step)).abs() <= bound).all()), float(((new.double() - (master.double() - step)).abs() / bound).max())
