@@ -285,6 +285,7 @@ rv_status rv_cluster_average_v(float* const* replicas, int C, size_t n, const in
  *             several pieces of r rows.
  *             Nothing in it has to be kept between calls; calls that may run at one time need one each, and so do graphs
  *             that may be replayed at one time.
+ * A logit of -inf is a probability of zero; one of +inf or NaN makes its row's loss, lse and gradients NaN.  Finite logits may be of any size.
  * All pointers 16-byte aligned (loss, lse, row_scale 4, label 8), ldx, ldw, lddx multiples of 8, ldx and ldw at most 2^20.  Outputs must not share memory
  * with inputs or one another but as said.  Allocates nothing; RV_E_INVAL, before anything is enqueued, on what is not covered.
  */

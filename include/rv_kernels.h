@@ -168,6 +168,8 @@ rv_status rv_k_attention_bwd_static(const void* qkv, const void* out, const void
  *   klen               device int32 [B]: keys of each sequence, taken as 0 below 0 and as Sk above; NULL: Sk for all.  What lies behind a
  *                      sequence's keys is not read.  A sequence without keys gives out 0, lse2 -inf and dq 0.
  *   lse2               fp32 [B, n_heads, Sq]: log2 of the softmax denominator in the scaled base-2 domain (kept for the backward).
+ * The backward forms its probabilities from that one fp32 number: they are off by up to 2^-20 |lse2| of themselves, less than their rounding to bf16 for
+ * scores of thousands.
  * A score of -inf is a probability of zero; a row with keys whose scores are all -inf, or one of +inf or NaN among them, has no softmax: out and
  * lse2 are NaN, and so is what the backward forms with them.  With an infinite operand a result that is infinite by definition may be NaN.
  * d_head is 64 or 128; the scale is 1 / sqrt(d_head); B, Sq, Sk are at least 1, of any size (B <= 2^20, Sq and Sk <= 2^24,

@@ -360,8 +360,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void cross_fwd_kernel(CrossArgs a)
   }
 }
 
-// Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the four waves walks over tiles of 32
-// keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.  Rings of 64 KB, so that two
+// Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the waves (two for heads of 128, four for
+// 64) walks over tiles of 32 keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.  Rings of 64 KB, so that two
 // workgroups share a CU: two tokens of 32 heads over 8 and 100001 keys 145 us, 5.7 TB/s (a large copy 5.0); 16 tokens of 16 heads of 64, up to
 // 1500 keys, 17 us.
 constexpr int TOKEN_KEYS = 32, kTokenGrid = 256;
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void cross_token_kernel(Cross
     }
   }
   lsum += __shfl_xor(lsum, 32, 64);
-  // four waves' sums: registers through LDS, a quarter of them to each wave
+  // the waves' sums: registers through LDS, an equal share of them to each wave
   __syncthreads();
   float* image = reinterpret_cast<float*>(dtl_smem);     // [wave][DH / 2][64], then the pairs
   float2* ml = reinterpret_cast<float2*>(image + TOKEN_NW * (DH / 2) * 64);

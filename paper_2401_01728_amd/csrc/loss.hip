@@ -493,7 +493,8 @@ template <int BM>
 __global__ __launch_bounds__(512, 2) void input_grad_kernel(GradArgs a) { input_grad_body<BM>(a, blockIdx.x); }
 // the stretches' sums, added in a fixed order and rounded, to the rows they belong to; zeros to the rows that take no part.  LANES lanes share
 // eight columns of a row: with dozens of stretches one lane's walk over them is a chain of round trips (256 rows of 448
-// columns, 64 stretches: 25 us with one lane).
+// columns, 64 stretches: 25 us with one lane).  The host chooses by the stretches for all rows; where few of them take part the device makes
+// more and one lane may walk over up to 64 sums, but of that many rows less.
 template <int LANES>
 __global__ __launch_bounds__(256) void input_grad_join_kernel(const float* __restrict__ part, Rows rows, int d, int nk, int bm, int S_all, int tiles_m,
                                                               float scale, uint16_t* __restrict__ dx, int64_t lddx) {

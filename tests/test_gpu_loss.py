@@ -557,3 +557,18 @@ def test_labels_of_an_update_have_16_bits(T, d, V, rows, labels, out):
     step = dz.T @ x64
     bound = (off + dz.abs() * (T // d + 40) * 2.0 ** -23).T @ x64.abs() + 2.0 ** -22 * (master.double().abs() + step.abs())
     assert bool(((new.double() - (master.double() - step)).abs() <= bound).all()), float(((new.double() - (master.double() - step)).abs() / bound).max())
+
+
+@pytest.mark.parametrize("T", [40, 300])
+def test_a_row_of_infinite_logits(T):
+    """+inf among them: the row is not a number, the others are what they were; of dw, which every row is in, nothing is."""
+    x, w, label, _ = (t.cuda() for t in _inputs(95, T, 128, 900))
+    loss, lse = rv.loss_forward(x, w, label)
+    ref = rv.loss_step(x, w, label)
+    x[17, 3] = math.inf
+    bad, bad_lse = rv.loss_forward(x, w, label)
+    got = rv.loss_step(x, w, label)
+    other = torch.arange(T, device="cuda") != 17
+    for a, b in ((bad, loss), (bad_lse, lse), (got[0], ref[0]), (got[1], ref[1])):
+        assert torch.equal(a[other], b[other]) and bool(torch.isnan(a[17]).all())
+    assert bool(torch.isnan(got[2]).all())
