@@ -181,7 +181,7 @@ __device__ __forceinline__ int dealt_tile(int id, int tiles, int& half) {
 }
 
 // ---- the logits' product ----------------------------------------------------------------------
-// Bound by the matrix cores at the board's power cap: 7783 rows, V 128000, d 2048 3.35 ms, 1.22 PFLOP/s (a library product of 8192^3 1.37); of that
+// Bound by the matrix cores at the board's power cap: 7783 rows, V 128000, d 2048 3.37 ms, 1.21 PFLOP/s (a library product of 8192^3 1.37); of that
 // 0.35 ms are the epilogue, exponentials and stores about half each.  (Tiles of 128x256, two to a CU, whose epilogues run beside walks: the whole
 // step 11.03 ms to 10.77.)
 // (The tiles are dealt out over the tile rows that are there: a map over the rows of all tokens would leave whole XCDs without work where half
