@@ -572,3 +572,17 @@ def test_a_row_of_infinite_logits(T):
     for a, b in ((bad, loss), (bad_lse, lse), (got[0], ref[0]), (got[1], ref[1])):
         assert torch.equal(a[other], b[other]) and bool(torch.isnan(a[17]).all())
     assert bool(torch.isnan(got[2]).all())
+
+
+@pytest.mark.parametrize("T,d,V,rows", [(300, 128, 700, 0), (300, 128, 700, 128), (2000, 64, 300, 0), (5000, 64, 70000, 256)])
+def test_none_or_one_of_many_rows_takes_part(T, d, V, rows):
+    """Gathered rows: none, in one piece and in several and with walks that are cut, and the last one alone."""
+    x, w, label, master = (t.cuda() for t in _inputs(96, T, d, V, 1.0))
+    loss, dx, dw = rv.loss_step(x, w, label, rows=rows)
+    assert not loss.any() and not dx.any() and not dw.any()
+    _, _, new, version = rv.loss_step(x, w, label, rows=rows, master=master, eta=0.5)
+    assert torch.equal(new, master) and torch.equal(version, master.to(torch.bfloat16))
+    x[T - 1], label[T - 1] = 0.5, V - 1
+    g = torch.ones(T, device="cuda")
+    loss, dx, new, version = rv.loss_step(x, w, label, rows=rows, master=master, eta=0.5)
+    _check(x, w, label, g, loss, None, dx, None, master, 0.5, new, version)
