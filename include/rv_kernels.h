@@ -1,8 +1,8 @@
 /*
  * rv_kernels.h - per-kernel entry points of librv.so, for parity tests and profiling of
  * the individual steps of the decoder stage.  The product API is rv.h; these calls expose
- * the same kernels the stage launches, one at a time.  Cross-attention (at the end) is an operator that a peer's owner
- * runs between stages; no stage launches it.  All pointers are device memory,
+ * the same kernels the stage launches, one at a time.  Cross-attention, rotary positions and attention over a window (at
+ * the end) are operators that a peer's owner runs between stages; no stage launches them.  All pointers are device memory,
  * 16-byte aligned; every call enqueues on `stream` and returns without synchronising;
  * RV_E_INVAL on shapes the kernels do not cover.
  */
@@ -188,6 +188,86 @@ rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, in
                                    const float* lse2, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, int B,
                                    int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, void* work, size_t work_bytes,
                                    void* stream);
+
+/*
+ * Positions as rotations of queries and keys, with a norm of each head in the same pass.  Token i of sequence b (of B, S tokens each) is row
+ * b * S + i of every matrix, head h its columns h * d_head on; a call's live tokens are i < length[b], at positions start[b] + i.
+ *   q, k, v            bf16, rows ldq, ldk, ldv elements apart; n_heads heads of q, n_kv_heads of k and v.  Either number may be 0: no queries
+ *                      (keys) then.  v may be NULL.  They may be columns of one matrix.
+ *   start, length      device int32 [B] or NULL: 0, S for all.  Taken as 0 below 0, and length as S above.
+ *   pos                device int32 [B, S] or NULL: positions for the angles in place of start[b] + i; of any sign.
+ *   freq               device fp64 [rot / 2], radians a position (rv_k_rotary_frequencies); NULL with rot 0.
+ *   rot                columns of a head that are turned, its first ones; a multiple of 16 up to d_head.  layout: RV_ROT_HALF, pairs (c, c + rot/2)
+ *                      share frequency c; RV_ROT_PAIRS, (2 c, 2 c + 1).  (a, b) -> amplitude (a cos - b sin, b cos + a sin).
+ *   gamma_q, gamma_k   bf16 [d_head] or NULL (no norm): a head x becomes x / sqrt(mean(x^2) + eps) * gamma before it is turned.
+ *   q_out, k_out, v_out  bf16, rows ldq_out, ldk_out, ldv_out apart, heads likewise; v_out is a copy of v.  q_out may be q with its pitch, k_out may be k.
+ *                      Rows behind a sequence's live tokens become zero.
+ *   rows, sinks        rows > 0: k_out and v_out are a cache of `rows` rows for each sequence (sequence b's begin at row b * rows), a ring
+ *                      behind its first `sinks` rows: position p (start[b] + i, whatever pos says) is row p below sinks, else
+ *                      sinks + (p - sinks) mod (rows - sinks); sinks counts as rows - 1 at most.  Of two tokens of a call with one row the
+ *                      later is kept; no other row is touched.
+ * Backward: dq_out, dk_out are the gradients of q_out and k_out (without a cache), dq, dk those of q and k, rows lddq_out .. apart; dq may be
+ * dq_out and dk dk_out.  q and k are the forward's inputs, read with a norm only (NULL else; dq and dk may not be q and k unless
+ * dq_out and dk_out are others).  dgamma_q, dgamma_k fp32 [d_head] or NULL.  v, *_out, rows, sinks are not looked at.
+ *   work               of the backward with dgamma_q or dgamma_k: device, 256-byte aligned, rv_k_rotary_work bytes; calls that may run at one time
+ *                      need one each.
+ * A result is computed in 32 bits and rounded once; an angle is off by less than 2^-24 turns.  No atomics: results do not vary.  d_head is 64 or 128;
+ * B <= 2^20, S <= 2^24, B * S <= 2^30, up to 2^12 heads; pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (start, length, pos, dgamma:
+ * 4, freq: 8).  Outputs must not share memory with inputs or one another but as said (columns of one matrix do not).
+ */
+enum { RV_ROT_HALF = 0, RV_ROT_PAIRS = 1 };
+typedef struct {
+  int32_t B, S, n_heads, n_kv_heads, d_head, rot, layout;
+  float amplitude, eps;
+  const double* freq;
+  const int32_t* pos;
+  const int32_t* start;
+  const int32_t* length;
+  const void* gamma_q;
+  const void* gamma_k;
+  const void* q;
+  int64_t ldq;
+  const void* k;
+  int64_t ldk;
+  const void* v;
+  int64_t ldv;
+  void* q_out;
+  int64_t ldq_out;
+  void* k_out;
+  int64_t ldk_out;
+  void* v_out;
+  int64_t ldv_out;
+  int32_t rows, sinks;
+  const void* dq_out;
+  int64_t lddq_out;
+  const void* dk_out;
+  int64_t lddk_out;
+  void* dq;
+  int64_t lddq;
+  void* dk;
+  int64_t lddk;
+  float* dgamma_q;
+  float* dgamma_k;
+  void* work;
+  size_t work_bytes;
+  void* stream;
+} rv_rotary_desc;
+
+/*
+ * Frequencies of rot / 2 pairs, base^(-2 c / rot), and how they are changed for contexts longer than a model was trained on; freq (host fp64 [rot / 2])
+ * and amplitude (host) are what a call takes.  rot is even, up to 1024.
+ *   RV_FREQ_PLAIN   as they are.
+ *   RV_FREQ_LINEAR  positions closer together: divided by factor.
+ *   RV_FREQ_BASE    the base times factor^(rot / (rot - 2)): the fastest stays, the slowest is divided by factor.
+ *   RV_FREQ_PARTS   by the turns that a pair makes within `context` positions: `high` and more stay, `low` and less are divided by factor, linear in
+ *                   the turns between; the amplitude is 1 + 0.1 ln factor.
+ */
+enum { RV_FREQ_PLAIN = 0, RV_FREQ_LINEAR = 1, RV_FREQ_BASE = 2, RV_FREQ_PARTS = 3 };
+rv_status rv_k_rotary_frequencies(int rot, double base, int rule, double factor, double context, double low, double high,
+                                  double* freq, float* amplitude);
+rv_status rv_k_rotary_work(int B, int S, int n_heads, int n_kv_heads, int d_head, size_t* bytes);
+rv_status rv_k_rotary_fwd(const rv_rotary_desc* desc);
+rv_status rv_k_rotary_bwd(const rv_rotary_desc* desc);
 
 #ifdef __cplusplus
 }

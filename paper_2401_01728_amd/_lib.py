@@ -25,6 +25,17 @@ class LossDesc(ctypes.Structure):
                 ("eta", c_float), ("work", c_void_p), ("work_bytes", c_size_t), ("stream", c_void_p)]
 
 
+c_double = ctypes.c_double
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("B", "S", "n_heads", "n_kv_heads", "d_head", "rot", "layout")] + [("amplitude", c_float), ("eps", c_float)] + [
+        (n, c_void_p) for n in ("freq", "pos", "start", "length", "gamma_q", "gamma_k")] + [
+        f for n in ("q", "k", "v", "q_out", "k_out", "v_out") for f in ((n, c_void_p), ("ld" + n, c_int64))] + [("rows", c_int32), ("sinks", c_int32)] + [
+        f for n in ("dq_out", "dk_out", "dq", "dk") for f in ((n, c_void_p), ("ld" + n, c_int64))] + [
+        ("dgamma_q", c_void_p), ("dgamma_k", c_void_p), ("work", c_void_p), ("work_bytes", c_size_t), ("stream", c_void_p)]
+
+
 # every symbol include/rv.h declares: name -> (restype, argtypes)
 SYMBOLS = {
     "rv_stage_create": (c_int, [ctypes.POINTER(StageDesc), ctypes.POINTER(c_void_p)]),
@@ -89,6 +100,10 @@ KERNEL_SYMBOLS = {
                                  + [c_void_p, c_size_t, c_void_p]),
     "rv_k_cross_attention_bwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p] + [c_void_p, c_int64] * 2 + [c_void_p]
                                  + [c_void_p, c_int64] * 3 + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]),
+    "rv_k_rotary_frequencies": (c_int, [c_int, c_double, c_int, c_double, c_double, c_double, c_double, c_void_p, c_void_p]),
+    "rv_k_rotary_work": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
+    "rv_k_rotary_fwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
+    "rv_k_rotary_bwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
     "rv_k_attention_bwd_static": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                           c_int, c_void_p]),
 }

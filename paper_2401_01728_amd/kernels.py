@@ -185,3 +185,92 @@ def cross_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, klen=None
             _ptr(dout), _tokens(dout, B, Sq, H * dh), _ptr(_flat(lse2, torch.float32, (B, H, Sq))), _ptr(dq), _tokens(dq, B, Sq, H * dh),
             _ptr(dk), _tokens(dk, B, Sk, Hkv * dh), _ptr(dv), _tokens(dv, B, Sk, Hkv * dh), *sizes, _ptr(work), n, _stream_handle(stream)))
     return dq, dk, dv
+
+
+ROT_LAYOUT = {"half": 0, "pairs": 1}
+FREQ_RULE = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rotary_frequencies(rot, base=10000.0, rule="plain", factor=1.0, context=0.0, low=1.0, high=32.0):
+    """rv_k_rotary_frequencies: (fp64 [rot / 2] in host memory, amplitude)."""
+    freq, amplitude = torch.empty(max(1, rot // 2), dtype=torch.float64), ctypes.c_float(0.0)
+    _check(_lib.lib().rv_k_rotary_frequencies(rot, base, FREQ_RULE[rule], factor, context, low, high, freq.data_ptr(), ctypes.byref(amplitude)))
+    return freq, amplitude.value
+
+
+def _address(t, dtype=None, shape=None):
+    return (_flat(t, dtype, shape) if dtype else t).data_ptr() if t is not None else None
+
+
+def _rotary_desc(q, k, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream):
+    """What both directions share; q and k: any two of the call's matrices [B, S, columns], one of which may be None."""
+    some, heads = (q, n_heads) if q is not None else (k, n_kv_heads)
+    assert some.dim() == 3 and heads >= 1 and some.shape[2] % heads == 0, (tuple(some.shape), heads)
+    assert (q is None) == (n_heads == 0) and (k is None) == (n_kv_heads == 0), (n_heads, n_kv_heads)
+    B, S, cols = some.shape
+    dh = cols // heads
+    rot = 0 if freq is None else 2 * freq.numel()
+    d = _lib.RotaryDesc(B=B, S=S, n_heads=n_heads, n_kv_heads=n_kv_heads, d_head=dh, rot=rot, layout=ROT_LAYOUT[layout], amplitude=amplitude, eps=eps,
+                        freq=_address(freq, torch.float64, (rot // 2,)), pos=_address(pos, torch.int32, (B, S)), start=_address(start, torch.int32, (B,)),
+                        length=_address(length, torch.int32, (B,)), gamma_q=_address(gamma_q, torch.bfloat16, (dh,)),
+                        gamma_k=_address(gamma_k, torch.bfloat16, (dh,)), stream=stream.cuda_stream)
+    return d, B, S, dh
+
+
+def _matrix(d, name, t, B, S, cols):
+    if t is not None:
+        setattr(d, name, t.data_ptr())
+        setattr(d, "ld" + name, _tokens(t, B, S, cols))
+
+
+def rotary_fwd(q, k, freq, n_heads, n_kv_heads, *, v=None, layout="half", amplitude=1.0, gamma_q=None, gamma_k=None, eps=1e-6, pos=None, start=None,
+               length=None, q_out=None, k_out=None, v_out=None, cache=None, sinks=0, stream=None):
+    """rv_k_rotary_fwd: q bf16 [B, S, n_heads * d_head], k and v bf16 [B, S, n_kv_heads * d_head] (columns of a wider matrix or not; q or k None with no
+    heads of it), freq device fp64 [rot / 2] or None, start and length int32 [B], pos int32 [B, S] -> (q_out, k_out) or, with v, (q_out, k_out, v_out).
+    cache: (keys, values) bf16 [B, rows, n_kv_heads * d_head] in place of k_out and v_out (values None without v)."""
+    stream, context = _on(stream, *(t for t in (q, k) if t is not None), freq, v, gamma_q, gamma_k, pos, start, length, q_out, k_out, v_out, *(cache or ()))
+    d, B, S, dh = _rotary_desc(q, k, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream)
+    kcols = n_kv_heads * dh
+    with context:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if q_out is None and q is not None else q_out
+        if cache is not None:
+            assert k is not None and k_out is None and v_out is None
+            (k_out, v_out), d.rows, d.sinks = cache, cache[0].shape[1], sinks
+            assert (v is None) == (v_out is None) and (v is None or v_out.shape == k_out.shape)
+        else:
+            k_out, v_out = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) if o is None and t is not None else o
+                            for t, o in ((k, k_out), (v, v_out)))
+        for name, t, cols in (("q", q, n_heads * dh), ("k", k, kcols), ("v", v, kcols), ("q_out", q_out, n_heads * dh)):
+            _matrix(d, name, t, B, S, cols)
+        for name, t in (("k_out", k_out), ("v_out", v_out)):
+            _matrix(d, name, t, B, d.rows or S, kcols)
+        _check(_lib.lib().rv_k_rotary_fwd(ctypes.byref(d)))
+    return (q_out, k_out) if v is None else (q_out, k_out, v_out)
+
+
+@lru_cache(maxsize=256)
+def _rotary_work(B, S, n_heads, n_kv_heads, dh):
+    n = ctypes.c_size_t(0)
+    _check(_lib.lib().rv_k_rotary_work(B, S, n_heads, n_kv_heads, dh, ctypes.byref(n)))
+    return n.value
+
+
+def rotary_bwd(dq_out, dk_out, freq, n_heads, n_kv_heads, *, q=None, k=None, layout="half", amplitude=1.0, gamma_q=None, gamma_k=None, eps=1e-6, pos=None,
+               start=None, length=None, dq=None, dk=None, weights=True, stream=None):
+    """rv_k_rotary_bwd: (dq, dk, dgamma_q, dgamma_k) of the above; q and k, the forward's inputs, with norms only.  weights False: no dgamma."""
+    stream, context = _on(stream, *(t for t in (dq_out, dk_out) if t is not None), freq, q, k, gamma_q, gamma_k, pos, start, length, dq, dk)
+    d, B, S, dh = _rotary_desc(dq_out, dk_out, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream)
+    with context:
+        dq, dk = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) if o is None and t is not None else o for t, o in ((dq_out, dq), (dk_out, dk)))
+        like = dq_out if dq_out is not None else dk_out
+        dgamma_q, dgamma_k = (torch.empty(dh, dtype=torch.float32, device=like.device) if weights and g is not None else None for g in (gamma_q, gamma_k))
+        for name, t, heads in (("q", q, n_heads), ("k", k, n_kv_heads), ("dq_out", dq_out, n_heads), ("dk_out", dk_out, n_kv_heads), ("dq", dq, n_heads),
+                               ("dk", dk, n_kv_heads)):
+            _matrix(d, name, t, B, S, heads * dh)
+        d.dgamma_q, d.dgamma_k = _address(dgamma_q), _address(dgamma_k)
+        if dgamma_q is not None or dgamma_k is not None:
+            n = _rotary_work(B, S, n_heads, n_kv_heads, dh)
+            work = torch.empty(n, dtype=torch.uint8, device=like.device)
+            d.work, d.work_bytes = work.data_ptr(), n
+        _check(_lib.lib().rv_k_rotary_bwd(ctypes.byref(d)))
+    return dq, dk, dgamma_q, dgamma_k
