@@ -269,6 +269,42 @@ rv_status rv_k_rotary_work(int B, int S, int n_heads, int n_kv_heads, int d_head
 rv_status rv_k_rotary_fwd(const rv_rotary_desc* desc);
 rv_status rv_k_rotary_bwd(const rv_rotary_desc* desc);
 
+/*
+ * Causal attention over a sliding window and the first tokens.  Sequence b has Sq tokens a call, of which i < length[b] are live, at positions
+ * p = start[b] + i; the token at p sees key j where j <= p and (j > p - window or j < sinks).
+ *   q, out, dout, dq   bf16, token i of sequence b at row b * Sq + i, rows ldq, ldo, lddo, lddq elements apart, head h at columns h * d_head on
+ *                      (n_heads of them).
+ *   k, v, dk, dv       bf16, Sk rows a sequence, n_kv_heads heads likewise; q, k and v may be columns of one matrix.  n_kv_heads divides n_heads: query
+ *                      head h reads key/value head h / (n_heads / n_kv_heads).  The rows are a cache, a ring behind the first `sinks` (rv_k_rotary_fwd
+ *                      fills it): key j is in row j below Sk, a further one in row sinks + (j - sinks) mod (Sk - sinks), sinks counting as Sk - 1 at most
+ *                      there.  It holds the keys below start[b] + length[b], the call's own among them; one whose row a later key has taken is
+ *                      seen by nobody, so rows for `window` + Sq - 1 keys behind the sinks lose none.
+ *   start, length      device int32 [B] or NULL: 0 (Sk >= Sq then), Sq for all.  Taken as 0 below 0, and length as Sq above.
+ *   lse2               fp32 [B, n_heads, Sq]: log2 of the softmax denominator in the scaled base-2 domain (kept for the backward).
+ * A token behind a sequence's length, or one that sees no key (its own row taken, no sinks), gives out 0, lse2 -inf and dq 0; rows that no live token
+ * sees are not read, and no value of a key reaches a token that does not see it, infinities and NaN included (a workgroup that meets them among what
+ * others of its tokens see is slower).
+ * Backward: of a call whose keys are the tokens' own, without start: S rows of each.  It writes all of dq, dk and dv, zeros behind a sequence's
+ * length; out and lse2 are the forward's.  Probabilities are formed from lse2: off by up to 2^-20 |lse2| of themselves.
+ * A score of -inf is a probability of zero; a token with keys whose scores are all -inf, or one of +inf or NaN among them, has no softmax: out and lse2
+ * are NaN, and so is what the backward forms with them.  With an infinite operand a result that is infinite by definition may be NaN.
+ * d_head is 64 or 128; the scale is 1 / sqrt(d_head); window is at least 1, any larger number sees all, sinks at least 0; B, Sq, Sk are at least 1, of
+ * any size (B <= 2^20, Sq and Sk <= 2^24, n_heads <= 2^16, n_heads / n_kv_heads * Sq < 2^30 - 64, of a sequence's q and k up to 2^34 elements).  Pitches are
+ * multiples of 8 up to 2^24, pointers 16-byte aligned (lse2, start, length: 4).  Outputs must not share memory with inputs or one another (but they may
+ * be columns of one matrix).  No atomics: results do not vary.
+ *   work               device, 256-byte aligned, rv_k_window_attention_work bytes (0 in some forwards: NULL is fine then); nothing in it is
+ *                      kept between calls, calls that may run at one time need one each, and so do graphs that may be replayed at one time.
+ */
+rv_status rv_k_window_attention_work(int B, int Sq, int Sk, int n_heads, int n_kv_heads, int d_head, int window, int sinks, int backward,
+                                     size_t* bytes);
+rv_status rv_k_window_attention_fwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* start,
+                                    const int32_t* length, void* out, int64_t ldo, float* lse2, int B, int Sq, int Sk, int n_heads,
+                                    int n_kv_heads, int d_head, int window, int sinks, void* work, size_t work_bytes, void* stream);
+rv_status rv_k_window_attention_bwd(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* length,
+                                    const void* out, int64_t ldo, const void* dout, int64_t lddo, const float* lse2, void* dq, int64_t lddq,
+                                    void* dk, int64_t lddk, void* dv, int64_t lddv, int B, int S, int n_heads, int n_kv_heads, int d_head,
+                                    int window, int sinks, void* work, size_t work_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -104,6 +104,11 @@ KERNEL_SYMBOLS = {
     "rv_k_rotary_work": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
     "rv_k_rotary_fwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
     "rv_k_rotary_bwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
+    "rv_k_window_attention_work": (c_int, [c_int] * 9 + [ctypes.POINTER(c_size_t)]),
+    "rv_k_window_attention_fwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p, c_void_p, c_void_p, c_int64, c_void_p] + [c_int] * 8
+                                  + [c_void_p, c_size_t, c_void_p]),
+    "rv_k_window_attention_bwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p] + [c_void_p, c_int64] * 2 + [c_void_p]
+                                  + [c_void_p, c_int64] * 3 + [c_int] * 7 + [c_void_p, c_size_t, c_void_p]),
     "rv_k_attention_bwd_static": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                           c_int, c_void_p]),
 }

@@ -164,4 +164,71 @@ __device__ __forceinline__ void store_owned32(const f32x16 (&acc)[DH / 32], floa
           f32x4{acc[dt][4 * rg], acc[dt][4 * rg + 1], acc[dt][4 * rg + 2], acc[dt][4 * rg + 3]};
 }
 
+// A row of one key: its probability is 1 whatever the score, so the score's gradient is zero; what stands here is the difference of one sum
+// formed in two orders.  (Times zero: what is not a number stays none.)
+template <int N>
+__device__ __forceinline__ void of_one_key(f32x16 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] *= 0.f;
+}
+
+// blocks of rows or keys of a (sequence, key/value head), parts of the streamed side, and how the list of them is dealt out (where)
+struct Grid { int blocks, parts, groups; };
+
+// Workgroup -> (sequence, key/value head, part, block): ids go to the 8 XCDs in turn; each takes a contiguous range of a list in which the
+// blocks of one (head, sequence), which read the same keys, are neighbours.  Where sequences have lengths of their own a range has to hold as
+// much of each as any other: the list then goes through the heads, or through `groups` equal shares of a head's blocks where
+// there are fewer than eight heads or no multiple of it, and has a share's blocks of every sequence behind one another (16 heads over 4, lengths of
+// 2048 .. 0: 238 us with whole heads, 232 with halves).
+__host__ __device__ inline int share_of(const Grid& g) { return (g.blocks * g.parts + g.groups - 1) / g.groups; }
+struct Where { int b, h, part, block, unit; };
+template <typename Args>
+__device__ __forceinline__ bool where(const Args& a, const Grid& g, int id, int total, Where& w) {
+  const int base = total / 8, rem = total % 8, x = id % 8, share = share_of(g);
+  const int v = x * base + (x < rem ? x : rem) + id / 8;
+  int u = v / share;
+  w.b = u % a.B; u /= a.B;
+  w.h = u / g.groups;
+  const int i = u % g.groups * share + v % share;
+  w.part = i / g.blocks;
+  w.block = i - w.part * g.blocks;
+  w.unit = w.b * a.Hkv + w.h;
+  return w.part < g.parts;
+}
+
+// ---- host ----
+inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int kMostParts = 64;
+
+// Parts of the streamed side: as many as give `want` workgroups, each with `least` tiles or more.
+int parts_for(int64_t blocks, int64_t tiles, int64_t want, int64_t least) {
+  int64_t p = want / (blocks > 0 ? blocks : 1);
+  if (p > tiles / least) p = tiles / least;
+  return (int)(p < 1 ? 1 : p > kMostParts ? kMostParts : p);
+}
+
+// A launch of the runtime has fewer than 2^32 threads; a call of more is made for some of its sequences at a time.
+constexpr int64_t kMostThreads = 3ll << 30;
+
+template <auto Kern, typename Args>
+rv_status launch(const Args& a, int64_t grid, int threads, int lds, hipStream_t st) {
+  if (rv_allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
+  hipLaunchKernelGGL(Kern, dim3((unsigned)grid), dim3(threads), lds, st, a);
+  return rv_launch_status();
+}
+
+bool bad(const void* p, uintptr_t to) { return !p || ((uintptr_t)p & (to - 1)); }
+bool bad_pitch(int64_t ld, int64_t cols) { return ld < cols || ld % 8 || ld > (1 << 24); }
+
+// the launch of `blocks` x parts per (sequence, key/value head); unequal: sequences may have lengths of their own
+template <typename Args>
+int64_t deal(Grid& g, const Args& a, bool unequal, int64_t blocks, int parts) {
+  g.blocks = (int)blocks; g.parts = parts; g.groups = 1;
+  if (unequal && a.B > 1) {
+    while (g.groups < 8 && a.Hkv * g.groups % 8) g.groups *= 2;
+    if (g.groups > blocks * parts) g.groups = (int)(blocks * parts);
+  }
+  return (int64_t)a.B * a.Hkv * g.groups * share_of(g);
+}
+
 }  // namespace

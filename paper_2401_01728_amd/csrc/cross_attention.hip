@@ -21,8 +21,6 @@
 
 namespace {
 
-// blocks of rows or keys of a (sequence, key/value head), parts of the streamed side, and how the list of them is dealt out (where)
-struct Grid { int blocks, parts, groups; };
 struct CrossArgs {
   const uint16_t* q; const uint16_t* k; const uint16_t* v;
   int64_t ldq, ldk, ldv;
@@ -58,34 +56,6 @@ template <int DH>
 __device__ __forceinline__ int64_t row_at(const CrossArgs& a, int b, int h, int r, int64_t ld) {
   const int g = r / a.Sq, t = r - g * a.Sq;
   return ((int64_t)b * a.Sq + t) * ld + (h * a.share + g) * DH;
-}
-
-// Workgroup -> (sequence, key/value head, part, block): ids go to the 8 XCDs in turn; each takes a contiguous range of a list in which the
-// blocks of one (head, sequence), which read the same keys, are neighbours.  Where sequences have lengths of their own a range has to hold as
-// much of each as any other: the list then goes through the heads, or through `groups` equal shares of a head's blocks where
-// there are fewer than eight heads or no multiple of it, and has a share's blocks of every sequence behind one another (16 heads over 4, lengths of
-// 2048 .. 0: 238 us with whole heads, 232 with halves).
-__host__ __device__ inline int share_of(const Grid& g) { return (g.blocks * g.parts + g.groups - 1) / g.groups; }
-struct Where { int b, h, part, block, unit; };
-__device__ __forceinline__ bool where(const CrossArgs& a, const Grid& g, int id, int total, Where& w) {
-  const int base = total / 8, rem = total % 8, x = id % 8, share = share_of(g);
-  const int v = x * base + (x < rem ? x : rem) + id / 8;
-  int u = v / share;
-  w.b = u % a.B; u /= a.B;
-  w.h = u / g.groups;
-  const int i = u % g.groups * share + v % share;
-  w.part = i / g.blocks;
-  w.block = i - w.part * g.blocks;
-  w.unit = w.b * a.Hkv + w.h;
-  return w.part < g.parts;
-}
-
-// A sequence of one key: its probability is 1 whatever the score, so the score's gradient is zero; what stands here is the difference of one sum
-// formed in two orders.  (Times zero: what is not a number stays none.)
-template <int N>
-__device__ __forceinline__ void of_one_key(f32x16 (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] *= 0.f;
 }
 
 // Softmax of a tile of scores s (SUBS x 32 keys from k0 on) with the running maximum m and sum l of a lane's row, in base 2: s becomes
@@ -604,19 +574,6 @@ __global__ __launch_bounds__(256) void cross_bwd_join_kernel(CrossArgs a) {
 }
 
 // ---- host ----------------------------------------------------------------------------------
-inline int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int kMostParts = 64;
-
-// Parts of the streamed side: as many as give `want` workgroups, each with `least` tiles or more.
-int parts_for(int64_t blocks, int64_t tiles, int64_t want, int64_t least) {
-  int64_t p = want / (blocks > 0 ? blocks : 1);
-  if (p > tiles / least) p = tiles / least;
-  return (int)(p < 1 ? 1 : p > kMostParts ? kMostParts : p);
-}
-
-// A launch of the runtime has fewer than 2^32 threads; a call of more is made for some of its sequences at a time.
-constexpr int64_t kMostThreads = 3ll << 30;
-
 struct CrossPlan {
   bool token;                              // up to 32 rows to a key/value head
   int R, Rp, fwd_parts, q_parts, kv_parts;
@@ -664,16 +621,6 @@ bool make_cross_plan(CrossPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H,
   return true;
 }
 
-template <auto Kern>
-rv_status launch(const CrossArgs& a, int64_t grid, int threads, int lds, hipStream_t st) {
-  if (rv_allow_lds<Kern>(lds) != hipSuccess) return RV_E_DEVICE;
-  hipLaunchKernelGGL(Kern, dim3((unsigned)grid), dim3(threads), lds, st, a);
-  return rv_launch_status();
-}
-
-bool bad(const void* p, uintptr_t to) { return !p || ((uintptr_t)p & (to - 1)); }
-bool bad_pitch(int64_t ld, int64_t cols) { return ld < cols || ld % 8 || ld > (1 << 24); }
-
 CrossArgs common_args(const CrossPlan& p, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* klen, int B, int Sq,
                       int Sk, int H, int Hkv, int dh) {
   CrossArgs a{};
@@ -697,26 +644,16 @@ CrossArgs sequences(CrossArgs a, const CrossPlan& p, int b0) {
   return a;
 }
 
-// the launch of `blocks` x parts per (sequence, key/value head)
-int64_t deal(Grid& g, const CrossArgs& a, int64_t blocks, int parts) {
-  g.blocks = (int)blocks; g.parts = parts; g.groups = 1;
-  if (a.klen && a.B > 1) {
-    while (g.groups < 8 && a.Hkv * g.groups % 8) g.groups *= 2;
-    if (g.groups > blocks * parts) g.groups = (int)(blocks * parts);
-  }
-  return (int64_t)a.B * a.Hkv * g.groups * share_of(g);
-}
-
 template <int DH>
 rv_status forward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.part = (float*)work; a.part_ml = (float2*)(work + p.fwd_ml);
   if (p.token) {
     constexpr int waves = kTokenWaves<DH>, ring = waves * kTokenRing<DH>, image = waves * (DH / 2 * 64 * 4 + 32 * 8);
-    const int64_t grid = deal(a.fwd, a, 1, p.fwd_parts);
+    const int64_t grid = deal(a.fwd, a, a.klen != nullptr, 1, p.fwd_parts);
     RV_TRY((launch<cross_token_kernel<DH>>(a, grid, 64 * waves, ring > image ? ring : image, st)));
   } else {
-    const int64_t grid = deal(a.fwd, a, up(a.R, OWN * 4), p.fwd_parts);
+    const int64_t grid = deal(a.fwd, a, a.klen != nullptr, up(a.R, OWN * 4), p.fwd_parts);
     RV_TRY((launch<cross_fwd_kernel<DH, 4, 2>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
   }
   if (p.fwd_parts == 1) return RV_OK;
@@ -729,7 +666,7 @@ rv_status backward(CrossArgs a, const CrossPlan& p, char* work, hipStream_t st) 
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
   RV_TRY((launch<cross_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
-  const int64_t kv = deal(a.bkv, a, up(a.Sk, OWN * NW), p.kv_parts), q = deal(a.bq, a, up(a.R, OWN * NW), p.q_parts);
+  const int64_t kv = deal(a.bkv, a, a.klen != nullptr, up(a.Sk, OWN * NW), p.kv_parts), q = deal(a.bq, a, a.klen != nullptr, up(a.R, OWN * NW), p.q_parts);
   a.kv_grid = (int)kv;
   RV_TRY((launch<cross_bwd_kernel<DH, NW, NS_KV>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, NS_KV>, st)));
   if (p.q_parts > 1) RV_TRY((launch<cross_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));

@@ -274,3 +274,46 @@ def rotary_bwd(dq_out, dk_out, freq, n_heads, n_kv_heads, *, q=None, k=None, lay
             d.work, d.work_bytes = work.data_ptr(), n
         _check(_lib.lib().rv_k_rotary_bwd(ctypes.byref(d)))
     return dq, dk, dgamma_q, dgamma_k
+
+
+@lru_cache(maxsize=256)
+def _window_work(sizes, backward):
+    n = ctypes.c_size_t(0)
+    _check(_lib.lib().rv_k_window_attention_work(*sizes, backward, ctypes.byref(n)))
+    return n.value
+
+
+def window_attention_fwd(q, k, v, n_heads, n_kv_heads, window, sinks=0, start=None, length=None, out=None, stream=None):
+    """rv_k_window_attention_fwd: q bf16 [B, Sq, n_heads * d_head], k and v bf16 [B, Sk, n_kv_heads * d_head] (columns of a wider matrix or not), start and
+    length int32 [B] or None -> (out like q, lse2 fp32 [B, n_heads, Sq])."""
+    B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
+    sizes = B, Sq, Sk, H, Hkv, dh, window, sinks
+    stream, context = _on(stream, q, k, v, start, length, out)
+    with context:
+        out = torch.empty(B, Sq, H * dh, dtype=torch.bfloat16, device=q.device) if out is None else out
+        lse2 = torch.empty(B, H, Sq, dtype=torch.float32, device=q.device)
+        n = _window_work(sizes, 0)
+        work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        _check(_lib.lib().rv_k_window_attention_fwd(
+            _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
+            _address(start, torch.int32, (B,)), _address(length, torch.int32, (B,)), _ptr(out), _tokens(out, B, Sq, H * dh), _ptr(lse2), *sizes,
+            _ptr(work), n, _stream_handle(stream)))
+    return out, lse2
+
+
+def window_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, window, sinks=0, length=None, dq=None, dk=None, dv=None, stream=None):
+    """rv_k_window_attention_bwd: (dq, dk, dv) of the above without start; out and lse2 are the forward's."""
+    B, S, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
+    assert S == Sk, (S, Sk)
+    sizes = B, S, H, Hkv, dh, window, sinks
+    stream, context = _on(stream, q, k, v, length, out, dout, lse2, dq, dk, dv)
+    with context:
+        dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v)))
+        n = _window_work((B, S, S, H, Hkv, dh, window, sinks), 1)
+        work = torch.empty(n, dtype=torch.uint8, device=q.device)
+        _check(_lib.lib().rv_k_window_attention_bwd(
+            _ptr(q), _tokens(q, B, S, H * dh), _ptr(k), _tokens(k, B, S, Hkv * dh), _ptr(v), _tokens(v, B, S, Hkv * dh),
+            _address(length, torch.int32, (B,)), _ptr(out), _tokens(out, B, S, H * dh), _ptr(dout), _tokens(dout, B, S, H * dh),
+            _ptr(_flat(lse2, torch.float32, (B, H, S))), _ptr(dq), _tokens(dq, B, S, H * dh), _ptr(dk), _tokens(dk, B, S, Hkv * dh),
+            _ptr(dv), _tokens(dv, B, S, Hkv * dh), *sizes, _ptr(work), n, _stream_handle(stream)))
+    return dq, dk, dv
