@@ -102,8 +102,8 @@ KERNEL_SYMBOLS = {
                                  + [c_void_p, c_int64] * 3 + [c_int] * 6 + [c_void_p, c_size_t, c_void_p]),
     "rv_k_rotary_frequencies": (c_int, [c_int, c_double, c_int, c_double, c_double, c_double, c_double, c_void_p, c_void_p]),
     "rv_k_rotary_work": (c_int, [c_int] * 5 + [ctypes.POINTER(c_size_t)]),
-    "rv_k_rotary_fwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
-    "rv_k_rotary_bwd": (c_int, [ctypes.POINTER(RotaryDesc)]),
+    "rv_k_rotary_fwd": (c_int, [c_void_p]),       # RotaryDesc, by reference or as bytes
+    "rv_k_rotary_bwd": (c_int, [c_void_p]),
     "rv_k_window_attention_work": (c_int, [c_int] * 9 + [ctypes.POINTER(c_size_t)]),
     "rv_k_window_attention_fwd": (c_int, [c_void_p, c_int64] * 3 + [c_void_p, c_void_p, c_void_p, c_int64, c_void_p] + [c_int] * 8
                                   + [c_void_p, c_size_t, c_void_p]),

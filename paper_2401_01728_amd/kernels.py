@@ -1,5 +1,7 @@
 """Thin binding of include/rv_kernels.h (per-kernel entry points; marshalling only)."""
 import ctypes
+import struct
+from contextlib import nullcontext
 from functools import lru_cache
 
 import torch
@@ -135,9 +137,10 @@ def attention_bwd_static(qkv, out, dout, lse2, dqkv, mb, S, d, H, stream=None):
 
 def _tokens(t, B, S, cols):
     """bf16 [B, S, cols], sequences one behind the other; the pitch of a token's row."""
-    assert t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (B, S, cols), (t.dtype, tuple(t.shape), (B, S, cols))
-    ld = t.stride(1) if S > 1 else t.stride(0) if B > 1 else cols
-    assert t.stride(2) == 1 and (B == 1 or t.stride(0) == S * ld), "tokens one pitch apart, columns neighbours: strides %s" % (t.stride(),)
+    assert t.is_cuda and t.dtype is torch.bfloat16 and t.shape == (B, S, cols), (t.dtype, tuple(t.shape), (B, S, cols))
+    per_sequence, per_token, per_column = t.stride()
+    ld = per_token if S > 1 else per_sequence if B > 1 else cols
+    assert per_column == 1 and (B == 1 or per_sequence == S * ld), "tokens one pitch apart, columns neighbours: strides %s" % (t.stride(),)
     return ld
 
 
@@ -187,8 +190,42 @@ def cross_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, klen=None
     return dq, dk, dv
 
 
+_HERE = nullcontext()
+
+
+def _handle(stream, first, *others):
+    """As _on, for calls that take less time than it does: (the stream's handle, the context for memory)."""
+    index = first.get_device()
+    assert index >= 0, first.device
+    for t in others:
+        assert t is None or t.get_device() == index, "tensors of several devices: %s, %s" % (first.device, t.device)
+    if stream is None:
+        if index == torch.cuda.current_device():
+            return torch._C._cuda_getCurrentRawStream(index), _HERE
+        stream = torch.cuda.current_stream(index)
+    assert stream.device_index == index, "a stream of %s for tensors of %s" % (stream.device, first.device)
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _address(t, dtype, shape):
+    """Of a small tensor without gaps; 0 for None."""
+    if t is None:
+        return 0
+    assert t.dtype is dtype and t.shape == shape and t.is_contiguous(), (t.dtype, tuple(t.shape), shape)
+    return t.data_ptr()
+
+
+def _matrix(t, B, S, cols):
+    """(address, pitch); of None zeros."""
+    return (0, 0) if t is None else (t.data_ptr(), _tokens(t, B, S, cols))
+
+
 ROT_LAYOUT = {"half": 0, "pairs": 1}
 FREQ_RULE = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+# rv_rotary_desc as C lays it out: one call of pack() is a third of the time of filling in a ctypes structure
+_ROTARY_DESC = struct.Struct("@7i2f6P" + "Pq" * 6 + "2i" + "Pq" * 4 + "3PNP")
+assert _ROTARY_DESC.size == ctypes.sizeof(_lib.RotaryDesc)
+_NONE = (0, 0)
 
 
 def rotary_frequencies(rot, base=10000.0, rule="plain", factor=1.0, context=0.0, low=1.0, high=32.0):
@@ -198,29 +235,21 @@ def rotary_frequencies(rot, base=10000.0, rule="plain", factor=1.0, context=0.0,
     return freq, amplitude.value
 
 
-def _address(t, dtype=None, shape=None):
-    return (_flat(t, dtype, shape) if dtype else t).data_ptr() if t is not None else None
-
-
-def _rotary_desc(q, k, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream):
-    """What both directions share; q and k: any two of the call's matrices [B, S, columns], one of which may be None."""
-    some, heads = (q, n_heads) if q is not None else (k, n_kv_heads)
-    assert some.dim() == 3 and heads >= 1 and some.shape[2] % heads == 0, (tuple(some.shape), heads)
+def _rotary_sizes(q, k, n_heads, n_kv_heads):
+    """(B, S, d_head) of any two of a call's matrices [B, S, columns], one of which may be None."""
     assert (q is None) == (n_heads == 0) and (k is None) == (n_kv_heads == 0), (n_heads, n_kv_heads)
-    B, S, cols = some.shape
-    dh = cols // heads
-    rot = 0 if freq is None else 2 * freq.numel()
-    d = _lib.RotaryDesc(B=B, S=S, n_heads=n_heads, n_kv_heads=n_kv_heads, d_head=dh, rot=rot, layout=ROT_LAYOUT[layout], amplitude=amplitude, eps=eps,
-                        freq=_address(freq, torch.float64, (rot // 2,)), pos=_address(pos, torch.int32, (B, S)), start=_address(start, torch.int32, (B,)),
-                        length=_address(length, torch.int32, (B,)), gamma_q=_address(gamma_q, torch.bfloat16, (dh,)),
-                        gamma_k=_address(gamma_k, torch.bfloat16, (dh,)), stream=stream.cuda_stream)
-    return d, B, S, dh
+    B, S, cols = (q if q is not None else k).shape
+    heads = n_heads or n_kv_heads
+    assert heads >= 1 and cols % heads == 0, (cols, heads)
+    return B, S, cols // heads
 
 
-def _matrix(d, name, t, B, S, cols):
-    if t is not None:
-        setattr(d, name, t.data_ptr())
-        setattr(d, "ld" + name, _tokens(t, B, S, cols))
+def _rotary_head(B, S, n_heads, n_kv_heads, dh, freq, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length):
+    """What a description of either direction begins with."""
+    half = 0 if freq is None else freq.numel()
+    return (B, S, n_heads, n_kv_heads, dh, 2 * half, ROT_LAYOUT[layout], amplitude, eps, _address(freq, torch.float64, (half,)), _address(pos, torch.int32, (B, S)),
+            _address(start, torch.int32, (B,)), _address(length, torch.int32, (B,)), _address(gamma_q, torch.bfloat16, (dh,)),
+            _address(gamma_k, torch.bfloat16, (dh,)))
 
 
 def rotary_fwd(q, k, freq, n_heads, n_kv_heads, *, v=None, layout="half", amplitude=1.0, gamma_q=None, gamma_k=None, eps=1e-6, pos=None, start=None,
@@ -228,23 +257,25 @@ def rotary_fwd(q, k, freq, n_heads, n_kv_heads, *, v=None, layout="half", amplit
     """rv_k_rotary_fwd: q bf16 [B, S, n_heads * d_head], k and v bf16 [B, S, n_kv_heads * d_head] (columns of a wider matrix or not; q or k None with no
     heads of it), freq device fp64 [rot / 2] or None, start and length int32 [B], pos int32 [B, S] -> (q_out, k_out) or, with v, (q_out, k_out, v_out).
     cache: (keys, values) bf16 [B, rows, n_kv_heads * d_head] in place of k_out and v_out (values None without v)."""
-    stream, context = _on(stream, *(t for t in (q, k) if t is not None), freq, v, gamma_q, gamma_k, pos, start, length, q_out, k_out, v_out, *(cache or ()))
-    d, B, S, dh = _rotary_desc(q, k, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream)
-    kcols = n_kv_heads * dh
+    B, S, dh = _rotary_sizes(q, k, n_heads, n_kv_heads)
+    rows, qcols, kcols = 0, n_heads * dh, n_kv_heads * dh
+    if cache is not None:
+        assert k is not None and k_out is None and v_out is None
+        k_out, v_out = cache
+        rows = k_out.shape[1]
+        assert (v is None) == (v_out is None)
+    handle, context = _handle(stream, q if q is not None else k, k, freq, v, gamma_q, gamma_k, pos, start, length, q_out, k_out, v_out)
     with context:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if q_out is None and q is not None else q_out
-        if cache is not None:
-            assert k is not None and k_out is None and v_out is None
-            (k_out, v_out), d.rows, d.sinks = cache, cache[0].shape[1], sinks
-            assert (v is None) == (v_out is None) and (v is None or v_out.shape == k_out.shape)
-        else:
-            k_out, v_out = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) if o is None and t is not None else o
-                            for t, o in ((k, k_out), (v, v_out)))
-        for name, t, cols in (("q", q, n_heads * dh), ("k", k, kcols), ("v", v, kcols), ("q_out", q_out, n_heads * dh)):
-            _matrix(d, name, t, B, S, cols)
-        for name, t in (("k_out", k_out), ("v_out", v_out)):
-            _matrix(d, name, t, B, d.rows or S, kcols)
-        _check(_lib.lib().rv_k_rotary_fwd(ctypes.byref(d)))
+        if q_out is None and q is not None:
+            q_out = q.new_empty(B, S, qcols)
+        if k_out is None and k is not None:
+            k_out = k.new_empty(B, S, kcols)
+        if v_out is None and v is not None:
+            v_out = v.new_empty(B, S, kcols)
+        _check(_lib.lib().rv_k_rotary_fwd(_ROTARY_DESC.pack(
+            *_rotary_head(B, S, n_heads, n_kv_heads, dh, freq, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length), *_matrix(q, B, S, qcols),
+            *_matrix(k, B, S, kcols), *_matrix(v, B, S, kcols), *_matrix(q_out, B, S, qcols), *_matrix(k_out, B, rows or S, kcols),
+            *_matrix(v_out, B, rows or S, kcols), rows, sinks, *_NONE, *_NONE, *_NONE, *_NONE, 0, 0, 0, 0, handle)))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
@@ -258,21 +289,25 @@ def _rotary_work(B, S, n_heads, n_kv_heads, dh):
 def rotary_bwd(dq_out, dk_out, freq, n_heads, n_kv_heads, *, q=None, k=None, layout="half", amplitude=1.0, gamma_q=None, gamma_k=None, eps=1e-6, pos=None,
                start=None, length=None, dq=None, dk=None, weights=True, stream=None):
     """rv_k_rotary_bwd: (dq, dk, dgamma_q, dgamma_k) of the above; q and k, the forward's inputs, with norms only.  weights False: no dgamma."""
-    stream, context = _on(stream, *(t for t in (dq_out, dk_out) if t is not None), freq, q, k, gamma_q, gamma_k, pos, start, length, dq, dk)
-    d, B, S, dh = _rotary_desc(dq_out, dk_out, freq, n_heads, n_kv_heads, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length, stream)
+    B, S, dh = _rotary_sizes(dq_out, dk_out, n_heads, n_kv_heads)
+    qcols, kcols = n_heads * dh, n_kv_heads * dh
+    like = dq_out if dq_out is not None else dk_out
+    handle, context = _handle(stream, like, dk_out, freq, q, k, gamma_q, gamma_k, pos, start, length, dq, dk)
     with context:
-        dq, dk = (torch.empty(t.shape, dtype=torch.bfloat16, device=t.device) if o is None and t is not None else o for t, o in ((dq_out, dq), (dk_out, dk)))
-        like = dq_out if dq_out is not None else dk_out
-        dgamma_q, dgamma_k = (torch.empty(dh, dtype=torch.float32, device=like.device) if weights and g is not None else None for g in (gamma_q, gamma_k))
-        for name, t, heads in (("q", q, n_heads), ("k", k, n_kv_heads), ("dq_out", dq_out, n_heads), ("dk_out", dk_out, n_kv_heads), ("dq", dq, n_heads),
-                               ("dk", dk, n_kv_heads)):
-            _matrix(d, name, t, B, S, heads * dh)
-        d.dgamma_q, d.dgamma_k = _address(dgamma_q), _address(dgamma_k)
-        if dgamma_q is not None or dgamma_k is not None:
+        if dq is None and dq_out is not None:
+            dq = like.new_empty(B, S, qcols)
+        if dk is None and dk_out is not None:
+            dk = like.new_empty(B, S, kcols)
+        n, work, dgamma_q, dgamma_k = 0, None, None, None
+        if weights and (gamma_q is not None or gamma_k is not None):
             n = _rotary_work(B, S, n_heads, n_kv_heads, dh)
-            work = torch.empty(n, dtype=torch.uint8, device=like.device)
-            d.work, d.work_bytes = work.data_ptr(), n
-        _check(_lib.lib().rv_k_rotary_bwd(ctypes.byref(d)))
+            work = like.new_empty(n, dtype=torch.uint8)
+            dgamma_q, dgamma_k = (like.new_empty(dh, dtype=torch.float32) if g is not None else None for g in (gamma_q, gamma_k))
+        address = lambda t: t.data_ptr() if t is not None else 0  # noqa: E731
+        _check(_lib.lib().rv_k_rotary_bwd(_ROTARY_DESC.pack(
+            *_rotary_head(B, S, n_heads, n_kv_heads, dh, freq, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length), *_matrix(q, B, S, qcols),
+            *_matrix(k, B, S, kcols), *_NONE, *_NONE, *_NONE, *_NONE, 0, 0, *_matrix(dq_out, B, S, qcols), *_matrix(dk_out, B, S, kcols), *_matrix(dq, B, S, qcols),
+            *_matrix(dk, B, S, kcols), address(dgamma_q), address(dgamma_k), address(work), n, handle)))
     return dq, dk, dgamma_q, dgamma_k
 
 
@@ -287,17 +322,17 @@ def window_attention_fwd(q, k, v, n_heads, n_kv_heads, window, sinks=0, start=No
     """rv_k_window_attention_fwd: q bf16 [B, Sq, n_heads * d_head], k and v bf16 [B, Sk, n_kv_heads * d_head] (columns of a wider matrix or not), start and
     length int32 [B] or None -> (out like q, lse2 fp32 [B, n_heads, Sq])."""
     B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
-    sizes = B, Sq, Sk, H, Hkv, dh, window, sinks
-    stream, context = _on(stream, q, k, v, start, length, out)
+    cols, kcols, sizes = H * dh, Hkv * dh, (B, Sq, Sk, H, Hkv, dh, window, sinks)
+    handle, context = _handle(stream, q, k, v, start, length, out)
     with context:
-        out = torch.empty(B, Sq, H * dh, dtype=torch.bfloat16, device=q.device) if out is None else out
-        lse2 = torch.empty(B, H, Sq, dtype=torch.float32, device=q.device)
+        if out is None:
+            out = q.new_empty(B, Sq, cols)
+        lse2 = q.new_empty((B, H, Sq), dtype=torch.float32)
         n = _window_work(sizes, 0)
-        work = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        work = q.new_empty(n, dtype=torch.uint8).data_ptr() if n else 0
         _check(_lib.lib().rv_k_window_attention_fwd(
-            _ptr(q), _tokens(q, B, Sq, H * dh), _ptr(k), _tokens(k, B, Sk, Hkv * dh), _ptr(v), _tokens(v, B, Sk, Hkv * dh),
-            _address(start, torch.int32, (B,)), _address(length, torch.int32, (B,)), _ptr(out), _tokens(out, B, Sq, H * dh), _ptr(lse2), *sizes,
-            _ptr(work), n, _stream_handle(stream)))
+            *_matrix(q, B, Sq, cols), *_matrix(k, B, Sk, kcols), *_matrix(v, B, Sk, kcols), _address(start, torch.int32, (B,)),
+            _address(length, torch.int32, (B,)), *_matrix(out, B, Sq, cols), lse2.data_ptr(), *sizes, work, n, handle))
     return out, lse2
 
 
@@ -305,15 +340,16 @@ def window_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, window, 
     """rv_k_window_attention_bwd: (dq, dk, dv) of the above without start; out and lse2 are the forward's."""
     B, S, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
     assert S == Sk, (S, Sk)
-    sizes = B, S, H, Hkv, dh, window, sinks
-    stream, context = _on(stream, q, k, v, length, out, dout, lse2, dq, dk, dv)
+    cols, kcols = H * dh, Hkv * dh
+    handle, context = _handle(stream, q, k, v, length, out, dout, lse2, dq, dk, dv)
     with context:
-        dq, dk, dv = (torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) if g is None else g for g, t in ((dq, q), (dk, k), (dv, v)))
+        dq = q.new_empty(B, S, cols) if dq is None else dq
+        dk = q.new_empty(B, S, kcols) if dk is None else dk
+        dv = q.new_empty(B, S, kcols) if dv is None else dv
         n = _window_work((B, S, S, H, Hkv, dh, window, sinks), 1)
-        work = torch.empty(n, dtype=torch.uint8, device=q.device)
+        work = q.new_empty(n, dtype=torch.uint8)
         _check(_lib.lib().rv_k_window_attention_bwd(
-            _ptr(q), _tokens(q, B, S, H * dh), _ptr(k), _tokens(k, B, S, Hkv * dh), _ptr(v), _tokens(v, B, S, Hkv * dh),
-            _address(length, torch.int32, (B,)), _ptr(out), _tokens(out, B, S, H * dh), _ptr(dout), _tokens(dout, B, S, H * dh),
-            _ptr(_flat(lse2, torch.float32, (B, H, S))), _ptr(dq), _tokens(dq, B, S, H * dh), _ptr(dk), _tokens(dk, B, S, Hkv * dh),
-            _ptr(dv), _tokens(dv, B, S, Hkv * dh), *sizes, _ptr(work), n, _stream_handle(stream)))
+            *_matrix(q, B, S, cols), *_matrix(k, B, S, kcols), *_matrix(v, B, S, kcols), _address(length, torch.int32, (B,)), *_matrix(out, B, S, cols),
+            *_matrix(dout, B, S, cols), _address(lse2, torch.float32, (B, H, S)), *_matrix(dq, B, S, cols), *_matrix(dk, B, S, kcols),
+            *_matrix(dv, B, S, kcols), B, S, H, Hkv, dh, window, sinks, work.data_ptr(), n, handle))
     return dq, dk, dv
