@@ -31,8 +31,9 @@ struct WinArgs {
   int64_t lddq, lddk, lddv;
   float* stat_lse; float* stat_d;        // [B][Hkv][Rp], in the order of the list
   float* part; float2* part_ml;          // forward: sums of the parts
-  float* q_part; float* kv_part;         // backward
-  int B, Sq, Sk, share, Hkv, R, Rp, kv_grid;
+  float* q_part; float* kv_part; float* sink_part;   // backward
+  int B, Sq, Sk, share, Hkv, R, Rp, kv_grid, sink_grid;
+  int sink_blocks, sink_parts;           // workgroups that add up what tokens whose window has left the sinks leave to them
   int window, sinks, ring;               // sinks < Sk, ring = Sk - sinks
   Grid fwd, bq, bkv;
   float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
@@ -617,7 +618,7 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   else store_owned32<DH>(dq, a.q_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + own.r) * DH);
 }
 
-// dK, dV: a wave owns 32 keys, the rows (queries and do) of the tokens that see any of a workgroup's keys stream.
+// dK, dV of the window: a wave owns 32 keys, the rows (queries and do) of the tokens whose windows hold any of a workgroup's keys stream.
 template <int DH, int NW, int NS>
 __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) {
   char* smem = dtl_smem;
@@ -628,17 +629,16 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
   const int n = live_of(a, w.b), j0 = w.block * OWN * NW;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int j = j0 + wave * OWN + (l & 31);
-  // rows that see key x: x share .. end(x) - 1
-  auto end = [&](int x) { return (x < a.sinks || n - x < a.window ? n : x + a.window) * a.share; };
+  // rows whose window holds key x: x share .. end(x) - 1
+  auto end = [&](int x) { return (n - x < a.window ? n : x + a.window) * a.share; };
   const int jl = (j0 + OWN * NW < n ? j0 + OWN * NW : n) - 1;                 // the workgroup's last key
-  const int from = j0 * a.share, to_row = j0 < n ? (end(j0) > end(jl) ? end(j0) : end(jl)) : from;
+  const int from = j0 * a.share, to_row = j0 < n ? end(jl) : from;
   const int nt = (to_row - from + TILE - 1) / TILE;         // keys behind the sequence: zeros
   const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const bool active = j0 + wave * OWN < n;
   const int jc = j < n ? j : n > 0 ? n - 1 : 0, w0 = __builtin_amdgcn_readfirstlane(jc), w1 = __builtin_amdgcn_readlane(jc, 31);
   const int my_first = jc * a.share, my_end = end(jc);
-  const int all_first = w1 * a.share, all_end = (w1 < a.sinks || n - w0 < a.window ? n : w0 + a.window) * a.share;
-  const int any_first = w0 * a.share, any_end = end(w0) > end(w1) ? end(w0) : end(w1);
+  const int all_first = w1 * a.share, all_end = end(w0), any_first = w0 * a.share, any_end = end(w1);
   // Heads of 128: keys, values, their two gradients and the scores are 256 registers by themselves; the values stay in LDS
   constexpr bool kValuesInLds = DH == 128;
   Frag* vl = reinterpret_cast<Frag*>(smem + NS * SLOT + wave * OWN * DH * 2) + l;
@@ -748,29 +748,161 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
   if (j >= a.Sk) return;
   if (one_key(a, n)) of_one_key(dk);
   if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
-  if (parts == 1) {
+  const bool more = a.sink_parts && j < a.sinks;            // rows behind the window see it, too
+  if (parts == 1 && !more) {
     store_owned<DH>(dk, a.scale, a.dk + ((int64_t)w.b * a.Sk + j) * a.lddk + w.h * DH);
     store_owned<DH>(dv, 1.0f, a.dv + ((int64_t)w.b * a.Sk + j) * a.lddv + w.h * DH);
   } else {
-    float* to = a.kv_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.Sk + j) * 2 * DH;
+    float* to = a.kv_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * (parts == 1 ? a.sinks : a.Sk) + j) * 2 * DH;
     store_owned32<DH>(dk, to);
     store_owned32<DH>(dv, to + DH);
   }
 }
+
+// dK, dV of the sinks from the tokens whose windows have left them: 32 keys, thousands of rows.  The four waves of a workgroup own the same keys and
+// walk over 32 rows each in turn, in slots of their own and without barriers; their sums meet in LDS and leave as a part of the workgroup's own.
+// (The first block of keys had all the rows at first, one workgroup's walk: 4 x 4096 tokens, 16 heads over 2 of 128, a window of 1024, 1568 us.)
+template <int DH>
+__device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
+  constexpr int ROWS = 32, HALF = ROWS * DH * 2, SLOT = 2 * HALF;
+  const int part = id % a.sink_parts, block = id / a.sink_parts % a.sink_blocks, unit = id / a.sink_parts / a.sink_blocks;
+  const int b = unit / a.Hkv, h = unit - b * a.Hkv;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
+  const int n = live_of(a, b), j0 = block * OWN, j = j0 + (l & 31);
+  const int last = a.sinks - 1 < n - 1 ? a.sinks - 1 : n - 1, jc = j < last ? j : last > 0 ? last : 0;
+  const int from = (n - j0 < a.window ? n : j0 + a.window) * a.share, to_row = n * a.share;
+  const int nt = (to_row - from + ROWS - 1) / ROWS;
+  const int t0 = (int)((int64_t)nt * part / a.sink_parts), t1 = (int)((int64_t)nt * (part + 1) / a.sink_parts);
+  const int my_first = (n - jc < a.window ? n : jc + a.window) * a.share, all_first = __builtin_amdgcn_readlane(my_first, 31);
+  char* slot = dtl_smem + wave * SLOT;
+  Frag* vl = reinterpret_cast<Frag*>(dtl_smem + 4 * SLOT) + l;                // the values, one copy for all waves
+  Frag kf[DH / 16];
+  const uint16_t* V = a.v + ((int64_t)b * a.Sk + jc) * a.ldv + h * DH;
+  load_owned<DH>(kf, a.k + ((int64_t)b * a.Sk + jc) * a.ldk + h * DH);
+  if (wave == 0) {
+    Frag vf[DH / 16];
+    load_owned<DH>(vf, V);
+#pragma unroll
+    for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
+  }
+  settle(kf);
+  __syncthreads();
+  f32x16 dk[DH / 32], dv[DH / 32];
+  clear(dk); clear(dv);
+  const TileLoads<DH, 1, ROWS> loads(0);
+  const float* stat_lse = a.stat_lse + (int64_t)unit * a.Rp;
+  const float* stat_d = a.stat_d + (int64_t)unit * a.Rp;
+  const int first = t0 + wave;
+#pragma unroll 1
+  for (int i = first; i < t1; i += 4) {
+    const int r0 = from + i * ROWS;
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");      // the reads of the rows before have come back
+    loads.rows([&](int r, int64_t& tok, int& c) {
+      const int t = r / a.share, g = r - t * a.share;
+      tok = (int64_t)b * a.Sq + t;
+      c = (h * a.share + g) * DH;
+    }, to_row, a.q, a.ldq, a.dout, a.lddo, r0, slot, slot + HALF);
+    f32x16 s[1], dp[1];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        s[0][4 * q + x] = stat_lse[r0 + 8 * q + 4 * grp + x];
+        dp[0][4 * q + x] = stat_d[r0 + 8 * q + 4 * grp + x];
+      }
+    wait_loads<0>();
+    const char* Os = slot + HALF;
+    struct Two { Frag rows, values; };
+    in_a_row<DH / 8, DH == 128 ? 4 : 2>([&](int i) {
+                          Two t;
+                          t.rows = frag_rows<DH>(i % 2 ? Os : slot, 0, i / 2);
+                          if (i % 2) t.values = vl[i / 2 * 64];
+                          return t;
+                        },
+                        [&](int i, const Two& t) {
+                          if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.values, dp[0], 0, 0, 0);
+                          else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kf[i / 2], s[0], 0, 0, 0);
+                        });
+    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, r0 >= all_first && r0 + ROWS <= to_row, false};
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
+      dp[0][x] *= s[0][x];
+    }
+    if (!v.all) {
+      asm volatile("");
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (!sees(v, acc_row(x, 0))) s[0][x] = dp[0][x] = 0.f;
+    }
+    const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
+    add_product<DH, 1>(dv, Os, p);
+    add_product<DH, 1>(dk, slot, ds);
+  }
+  if (!(all_finite(dk) && all_finite(dv))) {
+    clear(dk); clear(dv);
+    Frag vf[DH / 16];
+    load_owned<DH>(vf, V);
+#pragma unroll 1
+    for (int i = first; i < t1; i += 4) {
+      const int r1 = from + (i + 1) * ROWS < to_row ? from + (i + 1) * ROWS : to_row;
+#pragma unroll 1
+      for (int r = from + i * ROWS; r < r1; ++r) {
+        const uint16_t* q = a.q + row_at<DH>(a, b, h, r, a.ldq);
+        const uint16_t* d = a.dout + row_at<DH>(a, b, h, r, a.lddo);
+        const float pr = __builtin_amdgcn_exp2f((stat_lse[r] + dot_row<DH>(kf, q)) * a.c2), dp = stat_d[r] + dot_row<DH>(vf, d);
+        if (r < my_first) continue;
+        add_row<DH>(dv, pr, d);
+        add_row<DH>(dk, pr * dp, q);
+      }
+    }
+  }
+  // the waves' sums, dk's and then dv's: registers through LDS, an equal share of them to each wave
+  float* image = reinterpret_cast<float*>(dtl_smem);          // [4][DH / 2][64]: the slots
+  float* to = a.sink_part + (((int64_t)part * a.B * a.Hkv + unit) * a.sinks + j) * 2 * DH;
+#pragma unroll
+  for (int what = 0; what < 2; ++what) {
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < DH / 32; ++dt)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) image[(wave * (DH / 2) + dt * 16 + x) * 64 + l] = what ? dv[dt][x] : dk[dt][x];
+    __syncthreads();
+    if (j < a.sinks) {
+#pragma unroll
+      for (int x = 0; x < DH / 8; x += 4) {
+        const int reg = wave * (DH / 8) + x;
+        f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[e] += image[(i * (DH / 2) + reg + e) * 64 + l];
+        }
+        *reinterpret_cast<f32x4*>(to + what * DH + (reg >> 4) * 32 + acc_row(reg & 15, grp)) = v;
+      }
+    }
+  }
+}
+template <int DH> constexpr int kSinkLds = 4 * 2 * 32 * DH * 2 + 32 * DH * 2;
 template <int DH, int NW, int NS> constexpr int kKvLds = NS * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
 template <int DH> constexpr int kQLds = 4 * kTileBytes<DH>;
-template <int DH, int NW, int NS> constexpr int kBwdLds = kKvLds<DH, NW, NS> > kQLds<DH> ? kKvLds<DH, NW, NS> : kQLds<DH>;
-// Both in one launch, the longer workgroups (dK and dV: four products to dQ's three) first.
+constexpr int most(int x, int y) { return x > y ? x : y; }
+template <int DH, int NW, int NS> constexpr int kBwdLds = most(kKvLds<DH, NW, NS>, most(kQLds<DH>, kSinkLds<DH>));
+// All in one launch, the longer workgroups (dK and dV: four products to dQ's three) first.
 template <int DH, int NW, int NS>
 __global__ __launch_bounds__(64 * NW, DH == 128 ? 2 : 3) void window_bwd_kernel(WinArgs a) {
-  if ((int)blockIdx.x < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, blockIdx.x, a.kv_grid);
-  else bwd_q_body<DH, NW, 2>(a, blockIdx.x - a.kv_grid, gridDim.x - a.kv_grid);
+  static_assert(NW == 4, "bwd_sink_body");
+  const int id = blockIdx.x, others = a.kv_grid + a.sink_grid;
+  if (id < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, id, a.kv_grid);
+  else if (id < others) bwd_sink_body<DH>(a, id - a.kv_grid);
+  else bwd_q_body<DH, NW, 2>(a, id - others, gridDim.x - others);
 }
-// parts -> dq (KV false), or dk and dv
+// parts -> dq (KV false), or dk and dv (of the sinks alone where the others' are no parts)
 template <int DH, bool KV>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinArgs a) {
   constexpr int W = KV ? 2 * DH : DH;
-  const int per = KV ? a.Sk : a.R, parts = KV ? a.bkv.parts : a.bq.parts;
+  const int parts = KV ? a.bkv.parts : a.bq.parts, per = !KV ? a.R : parts > 1 ? a.Sk : a.sinks;
   const float* sums = KV ? a.kv_part : a.q_part;
   const int64_t rows = (int64_t)a.B * a.Hkv * per;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
@@ -783,6 +915,15 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinArgs a) {
     v[0] += p[0]; v[1] += p[1];
   }
   const int unit = (int)(row / per), r = (int)(row - (int64_t)unit * per), b = unit / a.Hkv, h = unit % a.Hkv;
+  if (KV && r < a.sinks) {
+    const int64_t step = (int64_t)a.B * a.Hkv * a.sinks * W;
+    const float* from = a.sink_part + ((int64_t)unit * a.sinks + r) * W + c;
+#pragma unroll 4
+    for (int s = 0; s < a.sink_parts; ++s) {
+      const f32x4* p = reinterpret_cast<const f32x4*>(from + s * step);
+      v[0] += p[0]; v[1] += p[1];
+    }
+  }
   const bool values = KV && c >= DH;
   if (!values) { v[0] *= a.scale; v[1] *= a.scale; }
   uint16_t* to = !KV ? a.dq + row_at<DH>(a, b, h, r, a.lddq) + c
@@ -793,11 +934,11 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinArgs a) {
 // ---- host ----------------------------------------------------------------------------------
 struct WinPlan {
   bool token;                              // up to 32 rows to a key/value head
-  int R, Rp, fwd_parts, q_parts, kv_parts;
+  int R, Rp, fwd_parts, q_parts, kv_parts, sink_blocks, sink_parts;
   int window, sinks;                       // no more than the rows
   int at_once;                             // sequences
   size_t fwd_ml, fwd_bytes;                // forward: [sums][pairs]
-  size_t d, part, kv_part, bwd_bytes;      // backward: [lse][D][sums of dq][of dk and dv]
+  size_t d, part, kv_part, sink_part, bwd_bytes;   // backward: [lse][D][sums of dq][of dk and dv][of the sinks' from behind the window]
 };
 bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh, int64_t window, int64_t sinks, bool backward) {
   if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128) || window < 1 || sinks < 0) return false;
@@ -819,12 +960,16 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   p.q_parts = parts_for(U * up(R, OWN * 4), tiles(OWN * 4, TILE), 512, 4);
   const int64_t seen = (p.window + OWN * 4) * share < R ? (p.window + OWN * 4) * share : R;
   p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(seen, TILE), 256, 4);
+  // tokens whose window leaves sinks: 512 workgroups, each with 8 rounds of its waves' 32 rows or more
+  const int64_t behind = p.sinks && p.window < Sk ? (Sk - p.window) * share : 0;
+  p.sink_blocks = behind ? (int)up(p.sinks, OWN) : 0;
+  p.sink_parts = behind ? parts_for(U * p.sink_blocks, up(behind, 4 * OWN), 512, 8) : 0;
   // threads of the largest launch, a sequence; of blocks that are dealt out in groups (deal) up to eight for seven more
   auto dealt = [&](int64_t blocks, int parts) { const int64_t n = blocks * parts; return Hkv * (n + (n < 8 ? n : 8) - 1); };
   auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
   int64_t threads;
   if (backward) {
-    threads = 256 * (dealt(up(Sk, OWN * 4), p.kv_parts) + dealt(up(R, OWN * 4), p.q_parts));
+    threads = 256 * (dealt(up(Sk, OWN * 4), p.kv_parts) + dealt(up(R, OWN * 4), p.q_parts) + Hkv * p.sink_blocks * p.sink_parts);
     threads = larger(threads, Hkv * p.Rp * (dh / 8));
     if (p.kv_parts > 1) threads = larger(threads, Hkv * Sk * (dh / 4));
   } else {
@@ -840,7 +985,8 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   p.d = round((size_t)4 * U * p.Rp);
   p.part = 2 * p.d;
   p.kv_part = p.part + (p.q_parts > 1 ? round((size_t)4 * p.q_parts * U * R * dh) : 0);
-  p.bwd_bytes = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : 0);
+  p.sink_part = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : p.sink_parts ? round((size_t)8 * U * p.sinks * dh) : 0);
+  p.bwd_bytes = p.sink_part + round((size_t)8 * p.sink_parts * U * p.sinks * dh);
   return true;
 }
 
@@ -891,13 +1037,14 @@ template <int DH, int NW, int NS>
 rv_status backward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
+  a.sink_part = (float*)(work + p.sink_part); a.sink_blocks = p.sink_blocks; a.sink_parts = p.sink_parts;
   RV_TRY((launch<window_stat_kernel<DH>>(a, up(U * a.Rp * (DH / 8), 256), 256, 0, st)));
   const int64_t kv = deal(a.bkv, a, a.length != nullptr, up(a.Sk, OWN * NW), p.kv_parts);
   const int64_t q = deal(a.bq, a, a.length != nullptr, up(a.R, OWN * NW), p.q_parts);
-  a.kv_grid = (int)kv;
-  RV_TRY((launch<window_bwd_kernel<DH, NW, NS>>(a, kv + q, 64 * NW, kBwdLds<DH, NW, NS>, st)));
+  a.kv_grid = (int)kv; a.sink_grid = (int)(U * p.sink_blocks * p.sink_parts);
+  RV_TRY((launch<window_bwd_kernel<DH, NW, NS>>(a, kv + a.sink_grid + q, 64 * NW, kBwdLds<DH, NW, NS>, st)));
   if (p.q_parts > 1) RV_TRY((launch<window_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
-  if (p.kv_parts > 1) RV_TRY((launch<window_bwd_join_kernel<DH, true>>(a, up(U * a.Sk * (DH / 4), 256), 256, 0, st)));
+  if (p.kv_parts > 1 || p.sink_parts) RV_TRY((launch<window_bwd_join_kernel<DH, true>>(a, up(U * (p.kv_parts > 1 ? a.Sk : a.sinks) * (DH / 4), 256), 256, 0, st)));
   return RV_OK;
 }
 
