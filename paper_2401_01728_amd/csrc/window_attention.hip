@@ -86,9 +86,10 @@ __device__ __forceinline__ Walk walk_of(const WinArgs& a, int start, int n, int 
   w.row0 = uniform((int)(key < (unsigned)a.Sk ? key : a.sinks + (key - a.sinks) % (unsigned)a.ring));
   return w;
 }
-// Which rows of a tile, counted from its first, a lane sees: x <= up and (x > low or x < first).  all: every lane of the wave all of them; none: none.
-// The three are less 4 (lane / 32), so that the rows of a lane's registers (acc_row) are compared as constants: kept, they would be 32 registers.
-struct Sees { int up, low, first; bool all, none; };
+// Which streamed rows, counted from the first, a lane sees: x <= up and (x > low or x < first).  all: every lane of the wave all of 32 of them, those from
+// 0 or 32 on; none: none.  The three are less 4 (lane / 32), so that the rows of a lane's registers (acc_row) are compared as constants: kept, they
+// would be 16 registers or 32.
+struct Sees { int up, low, first; bool all[2], none[2]; };
 struct Tile { int row, keys; };                                   // its first key's row, and how many there are
 template <int T>
 __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) {
@@ -100,22 +101,27 @@ __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) 
   t.keys = left < T ? left : T;
   return t;
 }
-// a lane's token t; tokens first .. last are the wave's
+// of tile i, its keys from `at` on; a lane's token t; tokens first .. last are the wave's
 template <int T>
-__device__ __forceinline__ Sees sees_of(const WinArgs& a, const Walk& w, int i, int t, int first, int last) {
+__device__ __forceinline__ Sees sees_of(const WinArgs& a, const Walk& w, int i, int at, int t, int first, int last) {
   Sees s;
   const bool sink = i < w.sink_tiles;
-  const int off = (sink ? i : i - w.sink_tiles) * T, shift = w.shift - off;
-  // (a token in front of the last sink has the range apart where its own row has been taken)
-  const int top = w.start + t < a.sinks ? w.start + t : a.sinks - 1;
-  s.up = sink ? top - off : t + shift;
-  s.low = sink ? -1 : t + shift - a.window;
-  s.first = sink ? 0 : w.first - off;
-  const bool up_all = T - 1 <= first + shift, low_all = last + shift < a.window || T <= s.first;
-  s.all = sink ? a.sinks - off >= T && w.start + first >= off + T - 1 : up_all && low_all;
-  s.none = !sink && (last + shift < 0 || (first + shift - a.window >= T - 1 && s.first <= 0));
+  const int off = (sink ? i : i - w.sink_tiles) * T + at, shift = w.shift - off, sinks = w.first - off;
+#pragma unroll
+  for (int sub = 0; sub < 2; ++sub) {
+    const int x = 32 * sub;
+    s.all[sub] = sink ? a.sinks - off >= x + 32 && w.start + first >= off + x + 31
+                      : x + 31 <= first + shift && (last + shift - a.window < x || x + 32 <= sinks);
+    s.none[sub] = sink ? off + x >= a.sinks : last + shift < x || (first + shift - a.window >= x + 31 && sinks <= x);
+  }
   const int grp4 = (threadIdx.x & 32) >> 3;
-  s.up -= grp4; s.low -= grp4; s.first -= grp4;
+  if (sink) {
+    // (a token in front of the last sink has the range apart where its own row has been taken)
+    const int top = w.start + t < a.sinks ? w.start + t : a.sinks - 1;
+    s.up = top - off - grp4; s.low = -5; s.first = 0;
+  } else {
+    s.up = t + shift - grp4; s.low = s.up - a.window; s.first = sinks - grp4;
+  }
   return s;
 }
 __device__ __forceinline__ bool sees(const Sees& s, int x) { return x <= s.up && (x > s.low || x < s.first); }
@@ -202,7 +208,7 @@ __device__ __forceinline__ void one_by_one(const WinArgs& a, const Walk& w, int 
 #pragma unroll 1
   for (int i = t0; i < t1; i += step) {
     const Tile tile = tile_of<T>(a, w, i);
-    const Sees v = sees_of<T>(a, w, i, t, first, last);
+    const Sees v = sees_of<T>(a, w, i, 0, t, first, last);
 #pragma unroll 1
     for (int x = 0; x < tile.keys; ++x) use(tile.row + x < a.Sk ? tile.row + x : tile.row + x - a.ring, sees(v, x - grp4));
   }
@@ -211,15 +217,14 @@ __device__ __forceinline__ void one_by_one(const WinArgs& a, const Walk& w, int 
 // Softmax of a tile of scores as in cross_attention.hip: s becomes exp2(s c2 - m), the factor for what was summed before is returned.
 template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, const Sees& v, float& m, float& lsum) {
-  const int grp = (threadIdx.x & 63) >> 5;
-  if (!v.all) {                          // (wave-uniform)
-    asm volatile("");
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub)
+  for (int sub = 0; sub < SUBS; ++sub)
+    if (!v.all[sub]) {                   // (wave-uniform)
+      asm volatile("");
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (!sees(v, sub * 32 + acc_row(r, 0))) s[sub][r] = -INFINITY;
-  }
+    }
   float mx = s[0][0];
 #pragma unroll
   for (int sub = 0; sub < SUBS; ++sub)
@@ -271,7 +276,7 @@ struct Rows {
   __device__ __forceinline__ int clamped(int r_) const { return r_ < live ? r_ : live > 0 ? live - 1 : 0; }
 };
 
-template <int DH, int NW, int NS>
+template <int DH, int NW, int NS, int SUBS>
 __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) {
   char* smem = dtl_smem;
   constexpr int SLOT = 2 * kTileBytes<DH>;               // keys, values
@@ -302,23 +307,29 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   f32x16 o[DH / 32];
   clear(o);
   float m = -INFINITY, lsum = 0.f;
-  auto tile = [&](int i, const char* Ks) {
+  // SUBS x 32 keys of a tile
+  auto some = [&](const char* Ks, const Sees& v) {
     const char* Vs = Ks + kTileBytes<DH>;
-    const Sees v = sees_of<TILE>(a, walk, i, own.t, own.first, own.last);
-    if (v.none) return;
-    f32x16 s[2];
+    f32x16 s[SUBS];
     clear(s);
-    in_a_row<DH / 8, DH == 128 ? 6 : 3>([&](int i) { return frag_rows<DH>(Ks, i % 2 * 32, i / 2); },
-                        [&](int i, const Frag& f) { s[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / 2], s[i % 2], 0, 0, 0); });
+    in_a_row<SUBS * DH / 16, DH == 128 ? 6 : 3>([&](int i) { return frag_rows<DH>(Ks, i % SUBS * 32, i / SUBS); },
+                        [&](int i, const Frag& f) { s[i % SUBS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / SUBS], s[i % SUBS], 0, 0, 0); });
     const float alpha = softmax_tile(s, a.c2, v, m, lsum);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {    // maxima that have settled leave the sums as they are
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
     }
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+    for (int sub = 0; sub < SUBS; ++sub) {
       const Frag p[1][2] = {{pack_frag(s[sub], 0), pack_frag(s[sub], 1)}};
       add_product<DH, 1>(o, Vs + sub * 32 * DH * 2, p);
+    }
+  };
+  auto tile = [&](int i, const char* Ks) {
+#pragma unroll 1
+    for (int at = 0; at < TILE; at += 32 * SUBS) {
+      const Sees v = sees_of<TILE>(a, walk, i, at, own.t, own.first, own.last);
+      if (!(v.none[0] && (SUBS == 1 || v.none[1]))) some(Ks + at * DH * 2, v);
     }
   };
   for (int i = t0; i < t1; ++i) {
@@ -348,15 +359,14 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   }
 }
 
-// Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the waves (two for heads of 128, four for
-// 64) walks over tiles of 32 keys of its own, with a ring of its own and no barrier; their sums meet in LDS at the end.
-constexpr int TOKEN_KEYS = 32, kTokenGrid = 256;
-template <int DH> constexpr int kTokenWaves = DH == 128 ? 2 : 4;
+// Up to 32 rows to a key/value head - single tokens: bound by reading the keys and values once.  Each of the waves walks over tiles of 32 keys of its
+// own, with a ring of its own and no barrier; their sums meet in LDS at the end.
+constexpr int TOKEN_KEYS = 32;
 constexpr int kTokenSlots = 2;
 template <int DH> constexpr int kTokenRing = kTokenSlots * 2 * TOKEN_KEYS * DH * 2;   // of a wave
-template <int DH>
-__global__ __launch_bounds__(64 * kTokenWaves<DH>) void window_token_kernel(WinArgs a) {
-  constexpr int TOKEN_NW = kTokenWaves<DH>, NS = kTokenSlots, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
+template <int DH, int TOKEN_NW>
+__global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) {
+  constexpr int NS = kTokenSlots, HALF = TOKEN_KEYS * DH * 2, SLOT = 2 * HALF;
   const int parts = a.fwd.parts;
   Where w;
   if (!where(a, a.fwd, blockIdx.x, gridDim.x, w)) return;
@@ -391,7 +401,7 @@ __global__ __launch_bounds__(64 * kTokenWaves<DH>) void window_token_kernel(WinA
     if (i + NS - 1 < mine) { issue(i + NS - 1); wait_loads<LPT * (NS - 1)>(); }
     else wait_loads<0>();
     const char* Ks = ring + i % NS * SLOT;
-    const Sees v = sees_of<TOKEN_KEYS>(a, walk, t0 + wave + i * TOKEN_NW, own.t, own.first, own.last);
+    const Sees v = sees_of<TOKEN_KEYS>(a, walk, t0 + wave + i * TOKEN_NW, 0, own.t, own.first, own.last);
     f32x16 s[1];
     clear(s);
     in_a_row<DH / 16, 4>([&](int i) { return frag_rows<DH>(Ks, 0, i); },
@@ -572,10 +582,10 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   asm volatile("" : "+v"(lse), "+v"(D));
   auto tile = [&](int i, const char* Ks) {
     const char* Vs = Ks + kTileBytes<DH>;
-    const Sees v = sees_of<TILE>(a, walk, i, own.t, own.first, own.last);
-    if (v.none) return;
 #pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
+      const Sees v = sees_of<TILE>(a, walk, i, sub * 32, own.t, own.first, own.last);
+      if (v.none[0]) continue;
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int x = 0; x < 16; ++x) { s[0][x] = lse; dp[0][x] = D; }
@@ -586,11 +596,11 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
                           });
 #pragma unroll
       for (int x = 0; x < 16; ++x) dp[0][x] *= __builtin_amdgcn_exp2f(s[0][x] * a.c2);
-      if (!v.all) {
+      if (!v.all[0]) {
         asm volatile("");
 #pragma unroll
         for (int x = 0; x < 16; ++x)
-          if (!sees(v, sub * 32 + acc_row(x, 0))) dp[0][x] = 0.f;
+          if (!sees(v, acc_row(x, 0))) dp[0][x] = 0.f;
       }
       const Frag ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
       add_product<DH, 1>(dq, Ks + sub * 32 * DH * 2, ds);
@@ -672,11 +682,11 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
   auto tile = [&](int i, const char* Qs) {
     const char* Os = Qs + kTileBytes<DH>;
     const float* lse = reinterpret_cast<const float*>(Os + kTileBytes<DH>);
-    const int r0 = from + i * TILE;
-    if (r0 + TILE - 1 < any_first || r0 >= any_end) return;
-    const Sees v{my_end - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, 0 - 4 * grp, r0 >= all_first && r0 + TILE <= all_end, false};
 #pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
+      const int r0 = from + i * TILE + sub * 32;
+      if (r0 + 31 < any_first || r0 >= any_end) continue;
+      const Sees v{my_end - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, 0 - 4 * grp, {r0 >= all_first && r0 + 32 <= all_end, false}, {}};
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -701,11 +711,11 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
         s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
         dp[0][x] *= s[0][x];
       }
-      if (!v.all) {
+      if (!v.all[0]) {
         asm volatile("");
 #pragma unroll
         for (int x = 0; x < 16; ++x)
-          if (!sees(v, sub * 32 + acc_row(x, 0))) s[0][x] = dp[0][x] = 0.f;
+          if (!sees(v, acc_row(x, 0))) s[0][x] = dp[0][x] = 0.f;
       }
       const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
       const char* O = Os + sub * 32 * DH * 2;
@@ -775,17 +785,16 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
   const int t0 = (int)((int64_t)nt * part / a.sink_parts), t1 = (int)((int64_t)nt * (part + 1) / a.sink_parts);
   const int my_first = (n - jc < a.window ? n : jc + a.window) * a.share, all_first = __builtin_amdgcn_readlane(my_first, 31);
   char* slot = dtl_smem + wave * SLOT;
-  Frag* vl = reinterpret_cast<Frag*>(dtl_smem + 4 * SLOT) + l;                // the values, one copy for all waves
-  Frag kf[DH / 16];
+  // keys and values in LDS, one copy for all waves: with both gradients and the scores they are too many registers
+  Frag* own = reinterpret_cast<Frag*>(dtl_smem + 4 * SLOT) + l;
+  const uint16_t* K = a.k + ((int64_t)b * a.Sk + jc) * a.ldk + h * DH;
   const uint16_t* V = a.v + ((int64_t)b * a.Sk + jc) * a.ldv + h * DH;
-  load_owned<DH>(kf, a.k + ((int64_t)b * a.Sk + jc) * a.ldk + h * DH);
-  if (wave == 0) {
-    Frag vf[DH / 16];
-    load_owned<DH>(vf, V);
+  if (wave < 2) {
+    Frag f[DH / 16];
+    load_owned<DH>(f, wave ? V : K);
 #pragma unroll
-    for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
+    for (int kk = 0; kk < DH / 16; ++kk) own[(2 * kk + wave) * 64] = f[kk];
   }
-  settle(kf);
   __syncthreads();
   f32x16 dk[DH / 32], dv[DH / 32];
   clear(dk); clear(dv);
@@ -797,11 +806,14 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
   for (int i = first; i < t1; i += 4) {
     const int r0 = from + i * ROWS;
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");      // the reads of the rows before have come back
+    int same = 0;
+    asm volatile("" : "+s"(same));                            // (fragments' addresses are not kept over the loop: there are no registers for them)
+    char* Qs = slot + same;
     loads.rows([&](int r, int64_t& tok, int& c) {
       const int t = r / a.share, g = r - t * a.share;
       tok = (int64_t)b * a.Sq + t;
       c = (h * a.share + g) * DH;
-    }, to_row, a.q, a.ldq, a.dout, a.lddo, r0, slot, slot + HALF);
+    }, to_row, a.q, a.ldq, a.dout, a.lddo, r0, Qs, Qs + HALF);
     f32x16 s[1], dp[1];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -811,25 +823,27 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
         dp[0][4 * q + x] = stat_d[r0 + 8 * q + 4 * grp + x];
       }
     wait_loads<0>();
-    const char* Os = slot + HALF;
-    struct Two { Frag rows, values; };
-    in_a_row<DH / 8, DH == 128 ? 4 : 2>([&](int i) {
-                          Two t;
-                          t.rows = frag_rows<DH>(i % 2 ? Os : slot, 0, i / 2);
-                          if (i % 2) t.values = vl[i / 2 * 64];
-                          return t;
-                        },
-                        [&](int i, const Two& t) {
-                          if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.values, dp[0], 0, 0, 0);
-                          else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kf[i / 2], s[0], 0, 0, 0);
-                        });
-    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, r0 >= all_first && r0 + ROWS <= to_row, false};
+    const char* Os = Qs + HALF;
+    struct Two { Frag rows, own; };
+#pragma unroll 1
+    for (int k0 = 0; k0 < DH / 8; k0 += 8)                      // (all at once, the compiler reads all fragments before the first product)
+      in_a_row<8, 2>([&](int i) {
+                       Two t;
+                       t.rows = frag_rows<DH>(i % 2 ? Os : Qs, 0, (k0 + i) / 2);
+                       t.own = own[(k0 + i) * 64];
+                       return t;
+                     },
+                     [&](int i, const Two& t) {
+                       if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, dp[0], 0, 0, 0);
+                       else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, s[0], 0, 0, 0);
+                     });
+    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, {r0 >= all_first && r0 + ROWS <= to_row, false}, {}};
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       dp[0][x] *= s[0][x];
     }
-    if (!v.all) {
+    if (!v.all[0]) {
       asm volatile("");
 #pragma unroll
       for (int x = 0; x < 16; ++x)
@@ -837,11 +851,12 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
     }
     const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
     add_product<DH, 1>(dv, Os, p);
-    add_product<DH, 1>(dk, slot, ds);
+    add_product<DH, 1>(dk, Qs, ds);
   }
   if (!(all_finite(dk) && all_finite(dv))) {
     clear(dk); clear(dv);
-    Frag vf[DH / 16];
+    Frag kf[DH / 16], vf[DH / 16];
+    load_owned<DH>(kf, K);
     load_owned<DH>(vf, V);
 #pragma unroll 1
     for (int i = first; i < t1; i += 4) {
@@ -884,7 +899,7 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
     }
   }
 }
-template <int DH> constexpr int kSinkLds = 4 * 2 * 32 * DH * 2 + 32 * DH * 2;
+template <int DH> constexpr int kSinkLds = 4 * 2 * 32 * DH * 2 + 2 * 32 * DH * 2;
 template <int DH, int NW, int NS> constexpr int kKvLds = NS * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
 template <int DH> constexpr int kQLds = 4 * kTileBytes<DH>;
 constexpr int most(int x, int y) { return x > y ? x : y; }
@@ -932,8 +947,14 @@ __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinArgs a) {
 }
 
 // ---- host ----------------------------------------------------------------------------------
+// Waves of a workgroup of single tokens: rings of 128 KB, one workgroup to a CU, or of 64 KB where there is more than one to each.  us, 128 / 64 KB: a
+// token of 16 heads over 2 of 64 and 4000 keys, 4 sequences 18.2 / 37.9 (with the join's 4); 20 sequences of 8 heads of 128 and 2000 keys 32 / 40;
+// 32 of 32 over 8 of 128 and 4100 keys 100 / 99, 5.4 TB/s; 20 of 8 heads of 64 and 32000 keys 303 / 294.
+template <int DH, bool WIDE> constexpr int kTokenWaves = (DH == 128 ? 2 : 4) * (WIDE ? 2 : 1);
+constexpr int64_t kTokenGrid = 256;
+
 struct WinPlan {
-  bool token;                              // up to 32 rows to a key/value head
+  bool token, wide;                        // up to 32 rows to a key/value head; workgroups of more waves
   int R, Rp, fwd_parts, q_parts, kv_parts, sink_blocks, sink_parts;
   int window, sinks;                       // no more than the rows
   int at_once;                             // sequences
@@ -956,7 +977,12 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
     span = span < Sk ? span : Sk;
     return up(span, T) + (span + p.sinks <= Sk ? up(p.sinks, T) : 0);
   };
-  p.fwd_parts = p.token ? parts_for(U, tiles(R, TOKEN_KEYS), kTokenGrid, 8) : parts_for(U * up(R, OWN * 4), tiles(OWN * 4, TILE), 512, 4);
+  p.wide = U <= kTokenGrid;
+  if (p.token) {
+    // A step of a workgroup's waves takes 1.1 us, joining parts 4: parts of five steps or more, for more than ten.
+    const int64_t waves = (dh == 128 ? 2 : 4) * (p.wide ? 2 : 1), steps = up(tiles(R, TOKEN_KEYS), waves);
+    p.fwd_parts = steps > 10 ? parts_for(U, steps, kTokenGrid, 5) : 1;
+  } else p.fwd_parts = parts_for(U * up(R, OWN * 4), tiles(OWN * 4, TILE), 512, 4);
   p.q_parts = parts_for(U * up(R, OWN * 4), tiles(OWN * 4, TILE), 512, 4);
   const int64_t seen = (p.window + OWN * 4) * share < R ? (p.window + OWN * 4) * share : R;
   p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(seen, TILE), 256, 4);
@@ -973,7 +999,7 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
     threads = larger(threads, Hkv * p.Rp * (dh / 8));
     if (p.kv_parts > 1) threads = larger(threads, Hkv * Sk * (dh / 4));
   } else {
-    threads = 256 * (p.token ? dealt(1, p.fwd_parts) : dealt(up(R, OWN * 4), p.fwd_parts));
+    threads = p.token ? 512 * dealt(1, p.fwd_parts) : 256 * dealt(up(R, OWN * 4), p.fwd_parts);
     if (p.fwd_parts > 1) threads = larger(threads, Hkv * R * dh);
   }
   if (threads > kMostThreads) return false;
@@ -1015,18 +1041,26 @@ WinArgs sequences(WinArgs a, const WinPlan& p, int b0) {
   return a;
 }
 
+template <int DH, bool WIDE>
+rv_status tokens(WinArgs& a, const WinPlan& p, hipStream_t st) {
+  constexpr int waves = kTokenWaves<DH, WIDE>, ring = waves * kTokenRing<DH>, image = waves * (DH / 2 * 64 * 4 + 32 * 8);
+  const int64_t grid = deal(a.fwd, a, a.start || a.length, 1, p.fwd_parts);
+  return launch<window_token_kernel<DH, waves>>(a, grid, 64 * waves, ring > image ? ring : image, st);
+}
 template <int DH>
 rv_status forward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   const bool unequal = a.start || a.length;
   a.part = (float*)work; a.part_ml = (float2*)(work + p.fwd_ml);
   if (p.token) {
-    constexpr int waves = kTokenWaves<DH>, ring = waves * kTokenRing<DH>, image = waves * (DH / 2 * 64 * 4 + 32 * 8);
-    const int64_t grid = deal(a.fwd, a, unequal, 1, p.fwd_parts);
-    RV_TRY((launch<window_token_kernel<DH>>(a, grid, 64 * waves, ring > image ? ring : image, st)));
+    RV_TRY((p.wide ? tokens<DH, true>(a, p, st) : tokens<DH, false>(a, p, st)));
   } else {
     const int64_t grid = deal(a.fwd, a, unequal, up(a.R, OWN * 4), p.fwd_parts);
-    RV_TRY((launch<window_fwd_kernel<DH, 4, 2>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
+    // Narrow windows 32 keys at a time: what a wave's own tokens do not see is left out, and heads of 64 take 110 registers, four waves to a SIMD.  us, 32 / 64
+    // keys: 4 x 2000 tokens of 16 heads of 64, windows of 64 / 256 / 512 / 1024 / 1500: 20 / 26, 30 / 43, 41 / 54, 62 / 69, 83 / 79; heads of 128 37 / 38, 51 / 55,
+    // 68 / 68, 102 / 99, 125 / 119; 32768 tokens, 32 heads over 8 of 128, a window of 4096 2436 / 2269.
+    if (a.window <= (DH == 64 ? 1024 : 512)) RV_TRY((launch<window_fwd_kernel<DH, 4, 2, 1>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
+    else RV_TRY((launch<window_fwd_kernel<DH, 4, 2, 2>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
   }
   if (p.fwd_parts == 1) return RV_OK;
   if (p.fwd_parts > 4) RV_TRY((launch<window_join_kernel<DH, 8>>(a, up(U * a.R * (DH / 8), 32), 256, 0, st)));
