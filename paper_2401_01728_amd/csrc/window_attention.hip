@@ -33,7 +33,7 @@ struct WinArgs {
   float* part; float2* part_ml;          // forward: sums of the parts
   float* q_part; float* kv_part; float* sink_part;   // backward
   int B, Sq, Sk, share, Hkv, R, Rp, kv_grid, sink_grid;
-  int sink_blocks, sink_parts;           // workgroups that add up what tokens whose window has left the sinks leave to them
+  int sink_blocks, sink_parts;           // workgroups of the sinks, or 0: where no window leaves them they are keys like others
   int window, sinks, ring;               // sinks < Sk, ring = Sk - sinks
   Grid fwd, bq, bkv;
   float c2, scale;                       // log2(e) / sqrt(dh), 1 / sqrt(dh)
@@ -86,10 +86,10 @@ __device__ __forceinline__ Walk walk_of(const WinArgs& a, int start, int n, int 
   w.row0 = uniform((int)(key < (unsigned)a.Sk ? key : a.sinks + (key - a.sinks) % (unsigned)a.ring));
   return w;
 }
-// Which streamed rows, counted from the first, a lane sees: x <= up and (x > low or x < first).  all: every lane of the wave all of 32 of them, those from
-// 0 or 32 on; none: none.  The three are less 4 (lane / 32), so that the rows of a lane's registers (acc_row) are compared as constants: kept, they
+// Which streamed rows, counted from the first, a lane sees: x <= up and (x > low or x < first).  partly: not all lanes of the wave see all of 32 of them;
+// none: no lane sees any.  The three are less 4 (lane / 32), so that the rows of a lane's registers (acc_row) are compared as constants: kept, they
 // would be 16 registers or 32.
-struct Sees { int up, low, first; bool all[2], none[2]; };
+struct Sees { int up, low, first; int partly, none; };            // bit 0: the rows from 0 on, bit 1: from 32 on
 struct Tile { int row, keys; };                                   // its first key's row, and how many there are
 template <int T>
 __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) {
@@ -104,15 +104,17 @@ __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) 
 // of tile i, its keys from `at` on; a lane's token t; tokens first .. last are the wave's
 template <int T>
 __device__ __forceinline__ Sees sees_of(const WinArgs& a, const Walk& w, int i, int at, int t, int first, int last) {
-  Sees s;
+  Sees s{0, 0, 0, 0, 0};
   const bool sink = i < w.sink_tiles;
   const int off = (sink ? i : i - w.sink_tiles) * T + at, shift = w.shift - off, sinks = w.first - off;
 #pragma unroll
   for (int sub = 0; sub < 2; ++sub) {
     const int x = 32 * sub;
-    s.all[sub] = sink ? a.sinks - off >= x + 32 && w.start + first >= off + x + 31
-                      : x + 31 <= first + shift && (last + shift - a.window < x || x + 32 <= sinks);
-    s.none[sub] = sink ? off + x >= a.sinks : last + shift < x || (first + shift - a.window >= x + 31 && sinks <= x);
+    const bool all = sink ? a.sinks - off >= x + 32 && w.start + first >= off + x + 31
+                          : x + 31 <= first + shift && (last + shift - a.window < x || x + 32 <= sinks);
+    const bool none = sink ? off + x >= a.sinks : last + shift < x || (first + shift - a.window >= x + 31 && sinks <= x);
+    s.partly |= (int)!all << sub;
+    s.none |= (int)none << sub;
   }
   const int grp4 = (threadIdx.x & 32) >> 3;
   if (sink) {
@@ -124,25 +126,71 @@ __device__ __forceinline__ Sees sees_of(const WinArgs& a, const Walk& w, int i, 
   }
   return s;
 }
+// The tiles, from the first up to but not including the second, all of whose keys all of a wave's tokens see as far as the window goes: most of a long
+// walk, where nothing else is looked at.
+struct Span { int first, end; };
+template <int T>
+__device__ __forceinline__ Span whole_tiles(const WinArgs& a, const Walk& w, int first, int last) {
+  const int left = last + w.shift - a.window, right = first + w.shift + 1;     // keys up to `left` are behind a token, from `right` on ahead of one
+  return {uniform(w.sink_tiles + (left < 0 ? 0 : left / T + 1)), uniform(w.sink_tiles + (right < 0 ? 0 : right / T))};
+}
 __device__ __forceinline__ bool sees(const Sees& s, int x) { return x <= s.up && (x > s.low || x < s.first); }
 
-// Loads of a tile of keys from a matrix whose row 0 is the sequence's: the tile's rows are neighbours but for the end of the ring.
-template <int DH, int NW, int ROWS>
-__device__ __forceinline__ void load_keys(const TileLoads<DH, NW, ROWS>& loads, const WinArgs& a, const uint16_t* base, int64_t ld, const Tile& t, char* lds) {
-  if (t.row + t.keys <= a.Sk) {
-    loads.keys(base, ld, t.row, t.row + t.keys, lds);
-    return;
-  }
-  const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)lds + loads.wave * 1024);
-#pragma unroll
-  for (int i = 0; i < TileLoads<DH, NW, ROWS>::N; ++i) {
-    int r = loads.row + i * TileLoads<DH, NW, ROWS>::STEP;
-    r = t.row + (r < t.keys ? r : t.keys - 1);
-    if (r >= a.Sk) r -= a.ring;
-    const uint16_t* from = base + (int64_t)r * ld + loads.column(i);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(m0v + i * NW * 1024) : "memory", "m0");
-  }
+// One load of 64 lanes: 16 bytes each from base + off to LDS at lds + AT.
+template <int AT>
+__device__ __forceinline__ void load_at(const uint16_t* base, unsigned off, int lds) {
+  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(lds), "n"(AT) : "memory", "m0", "scc");
 }
+// N of them, OFFS lane offsets: one for each, or one for all, whose bases are `step` elements apart.  (More than that are spilled in some kernels, and the
+// wait for what was spilled is one for all loads on the way: backward of heads of 64 20 % slower.)
+template <int N, int OFFS, int TO, int I = 0>
+__device__ __forceinline__ void load_all(const uint16_t* base, int64_t step, const unsigned (&off)[OFFS], int lds) {
+  load_at<I * TO>(base, off[OFFS == 1 ? 0 : I], lds);
+  if constexpr (I + 1 < N) load_all<N, OFFS, TO, I + 1>(OFFS == 1 ? base + step : base, step, off, lds);
+}
+// Tiles of keys and values.  Whole ones whose rows are neighbours - all but the last of a range, a ring's end and few sinks - take lane offsets that are
+// formed once.
+template <int DH, int NW, int ROWS>
+struct KeyLoads {
+  typedef TileLoads<DH, NW, ROWS> Base;
+  static constexpr int N = Base::N, OFFS = Base::kOneColumn ? 1 : N, PER_TILE = 2 * N;
+  Base loads;
+  const uint16_t* K; const uint16_t* V;                // the sequence's row 0
+  unsigned off_k[OFFS], off_v[OFFS];
+  __device__ __forceinline__ KeyLoads(const WinArgs& a, const Where& w, int wave) : loads(wave) {
+    K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
+    V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
+#pragma unroll
+    for (int i = 0; i < OFFS; ++i) {
+      const unsigned r = loads.row + i * Base::STEP, c = loads.column(i) * 2;
+      off_k[i] = r * (unsigned)(a.ldk * 2) + c;
+      off_v[i] = r * (unsigned)(a.ldv * 2) + c;
+      asm volatile("" : "+v"(off_k[i]), "+v"(off_v[i]));   // (of 64-bit products the low halves: else both are kept)
+    }
+  }
+  // rows of the tile out of the ring's end, and repeats of the last one
+  __device__ __forceinline__ void pieces(const WinArgs& a, const uint16_t* base, int64_t ld, const Tile& t, int m0v) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int r = loads.row + i * Base::STEP;
+      r = t.row + (r < t.keys ? r : t.keys - 1);
+      if (r >= a.Sk) r -= a.ring;
+      const uint16_t* from = base + (int64_t)r * ld + loads.column(i);
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(m0v + i * NW * 1024) : "memory", "m0");
+    }
+  }
+  __device__ __forceinline__ void issue(const WinArgs& a, const Walk& w, int i, char* lds) const {
+    const Tile t = tile_of<ROWS>(a, w, i);
+    const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)lds + loads.wave * 1024);
+    if (t.keys == ROWS && t.row + ROWS <= a.Sk) {
+      load_all<N, OFFS, NW * 1024>(K + (int64_t)t.row * a.ldk, Base::STEP * a.ldk, off_k, m0v);
+      load_all<N, OFFS, NW * 1024>(V + (int64_t)t.row * a.ldv, Base::STEP * a.ldv, off_v, m0v + ROWS * DH * 2);
+    } else {
+      pieces(a, K, a.ldk, t, m0v);
+      pieces(a, V, a.ldv, t, m0v + ROWS * DH * 2);
+    }
+  }
+};
 
 // acc[dt] += tile^T p over SUBS x 32 streamed rows, which begin at lds
 template <int DH, int SUBS>
@@ -219,7 +267,7 @@ template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, const Sees& v, float& m, float& lsum) {
 #pragma unroll
   for (int sub = 0; sub < SUBS; ++sub)
-    if (!v.all[sub]) {                   // (wave-uniform)
+    if (v.partly >> sub & 1) {           // (wave-uniform)
       asm volatile("");
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -287,17 +335,10 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   const Rows<NW> own(a, w, a.fwd.blocks - 1 - w.block, wave);    // later rows see more keys: they come first
   const Walk walk = own.template walk<TILE>(a);
   const int t0 = (int)((int64_t)walk.tiles * w.part / parts), t1 = (int)((int64_t)walk.tiles * (w.part + 1) / parts);
-  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
-  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
-
-  const TileLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * TileLoads<DH, NW>::N;
-  auto issue = [&](int i) {
-    char* to = smem + (i - t0) % NS * SLOT;
-    const Tile tile = tile_of<TILE>(a, walk, i);
-    load_keys(loads, a, K, a.ldk, tile, to);
-    load_keys(loads, a, V, a.ldv, tile, to + kTileBytes<DH>);
-  };
+  const KeyLoads<DH, NW, TILE> loads(a, w, wave);
+  const Span whole = whole_tiles<TILE>(a, walk, own.first, own.last);
+  constexpr int LPT = loads.PER_TILE;
+  auto issue = [&](int i) { loads.issue(a, walk, i, smem + (i - t0) % NS * SLOT); };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
     if (t0 + i < t1) issue(t0 + i);
@@ -328,8 +369,9 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   auto tile = [&](int i, const char* Ks) {
 #pragma unroll 1
     for (int at = 0; at < TILE; at += 32 * SUBS) {
-      const Sees v = sees_of<TILE>(a, walk, i, at, own.t, own.first, own.last);
-      if (!(v.none[0] && (SUBS == 1 || v.none[1]))) some(Ks + at * DH * 2, v);
+      Sees v{0, 0, 0, 0, 0};
+      if (i < whole.first || i >= whole.end) v = sees_of<TILE>(a, walk, i, at, own.t, own.first, own.last);
+      if ((v.none & (SUBS == 1 ? 1 : 3)) != (SUBS == 1 ? 1 : 3)) some(Ks + at * DH * 2, v);
     }
   };
   for (int i = t0; i < t1; ++i) {
@@ -342,8 +384,8 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   if (own.active && !all_finite(o)) {
     clear(o);
     one_by_one<TILE>(a, walk, t0, t1, 1, own.t, own.first, own.last, [&](int row, bool seen) {
-      const float s = dot_row<DH>(qf, K + (int64_t)row * a.ldk);
-      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), V + (int64_t)row * a.ldv);
+      const float s = dot_row<DH>(qf, loads.K + (int64_t)row * a.ldk);
+      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), loads.V + (int64_t)row * a.ldv);
     });
   }
   if (own.r >= a.R) return;
@@ -375,17 +417,10 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
   const Walk walk = own.template walk<TOKEN_KEYS>(a);
   const int t0 = (int)((int64_t)walk.tiles * w.part / parts), t1 = (int)((int64_t)walk.tiles * (w.part + 1) / parts);
   char* ring = dtl_smem + wave * kTokenRing<DH>;
-  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
-  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
-  const TileLoads<DH, 1, TOKEN_KEYS> loads(0);
-  constexpr int LPT = 2 * TileLoads<DH, 1, TOKEN_KEYS>::N;
+  const KeyLoads<DH, 1, TOKEN_KEYS> loads(a, w, 0);
+  constexpr int LPT = loads.PER_TILE;
   const int mine = t1 - t0 > wave ? (t1 - t0 - wave + TOKEN_NW - 1) / TOKEN_NW : 0;      // tiles t0 + wave, + TOKEN_NW, ...
-  auto issue = [&](int i) {
-    char* to = ring + i % NS * SLOT;
-    const Tile tile = tile_of<TOKEN_KEYS>(a, walk, t0 + wave + i * TOKEN_NW);
-    load_keys(loads, a, K, a.ldk, tile, to);
-    load_keys(loads, a, V, a.ldv, tile, to + HALF);
-  };
+  auto issue = [&](int i) { loads.issue(a, walk, t0 + wave + i * TOKEN_NW, ring + i % NS * SLOT); };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
     if (i < mine) issue(i);
@@ -417,8 +452,8 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
   if (own.first != own.last && !all_finite(o)) {         // (one token: what is masked is a repeat of what it sees)
     clear(o);
     one_by_one<TOKEN_KEYS>(a, walk, t0 + wave, t1, TOKEN_NW, own.t, own.first, own.last, [&](int row, bool seen) {
-      const float s = dot_row<DH>(qf, K + (int64_t)row * a.ldk);
-      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), V + (int64_t)row * a.ldv);
+      const float s = dot_row<DH>(qf, loads.K + (int64_t)row * a.ldk);
+      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), loads.V + (int64_t)row * a.ldv);
     });
   }
   lsum += __shfl_xor(lsum, 32, 64);
@@ -558,18 +593,12 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   const Rows<NW> own(a, w, a.bq.blocks - 1 - w.block, wave);
   const Walk walk = own.template walk<TILE>(a);
   const int t0 = (int)((int64_t)walk.tiles * w.part / parts), t1 = (int)((int64_t)walk.tiles * (w.part + 1) / parts);
-  const uint16_t* K = a.k + (int64_t)w.b * a.Sk * a.ldk + w.h * DH;
-  const uint16_t* V = a.v + (int64_t)w.b * a.Sk * a.ldv + w.h * DH;
   f32x16 dq[DH / 32];
   clear(dq);
-  const TileLoads<DH, NW> loads(wave);
-  constexpr int LPT = 2 * TileLoads<DH, NW>::N;
-  auto issue = [&](int i) {
-    char* to = smem + (i - t0) % NS * SLOT;
-    const Tile tile = tile_of<TILE>(a, walk, i);
-    load_keys(loads, a, K, a.ldk, tile, to);
-    load_keys(loads, a, V, a.ldv, tile, to + kTileBytes<DH>);
-  };
+  const KeyLoads<DH, NW, TILE> loads(a, w, wave);
+  const Span whole = whole_tiles<TILE>(a, walk, own.first, own.last);
+  constexpr int LPT = loads.PER_TILE;
+  auto issue = [&](int i) { loads.issue(a, walk, i, smem + (i - t0) % NS * SLOT); };
 #pragma unroll
   for (int i = 0; i < NS - 1; ++i)
     if (t0 + i < t1) issue(t0 + i);
@@ -584,8 +613,9 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
     const char* Vs = Ks + kTileBytes<DH>;
 #pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
-      const Sees v = sees_of<TILE>(a, walk, i, sub * 32, own.t, own.first, own.last);
-      if (v.none[0]) continue;
+      Sees v{0, 0, 0, 0, 0};
+      if (i < whole.first || i >= whole.end) v = sees_of<TILE>(a, walk, i, sub * 32, own.t, own.first, own.last);
+      if (v.none & 1) continue;
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int x = 0; x < 16; ++x) { s[0][x] = lse; dp[0][x] = D; }
@@ -596,7 +626,7 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
                           });
 #pragma unroll
       for (int x = 0; x < 16; ++x) dp[0][x] *= __builtin_amdgcn_exp2f(s[0][x] * a.c2);
-      if (!v.all[0]) {
+      if (v.partly & 1) {
         asm volatile("");
 #pragma unroll
         for (int x = 0; x < 16; ++x)
@@ -616,8 +646,8 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   if (own.active && !all_finite(dq)) {
     clear(dq);
     one_by_one<TILE>(a, walk, t0, t1, 1, own.t, own.first, own.last, [&](int row, bool seen) {
-      const uint16_t* k = K + (int64_t)row * a.ldk;
-      const float p = __builtin_amdgcn_exp2f((lse + dot_row<DH>(qf, k)) * a.c2), dp = D + dot_row<DH>(of, V + (int64_t)row * a.ldv);
+      const uint16_t* k = loads.K + (int64_t)row * a.ldk;
+      const float p = __builtin_amdgcn_exp2f((lse + dot_row<DH>(qf, k)) * a.c2), dp = D + dot_row<DH>(of, loads.V + (int64_t)row * a.ldv);
       if (seen) add_row<DH>(dq, p * dp, k);
     });
   }
@@ -628,11 +658,44 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   else store_owned32<DH>(dq, a.q_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.R + own.r) * DH);
 }
 
+// Tiles of rows: queries and do.  Where a load's rows are whole tokens, lane offsets are formed once.
+template <int DH, int NW, int ROWS>
+struct RowLoads {
+  typedef TileLoads<DH, NW, ROWS> Base;
+  static constexpr int N = Base::N;
+  Base loads;
+  int tokens;                                          // of a load's step, or 0
+  unsigned off_q[1], off_o[1];
+  __device__ __forceinline__ RowLoads(const WinArgs& a, int wave) : loads(wave) {
+    tokens = Base::kOneColumn && Base::STEP % a.share == 0 ? Base::STEP / a.share : 0;
+    const unsigned t = loads.row / a.share, c = ((loads.row - t * a.share) * DH + loads.column(0)) * 2;
+    off_q[0] = t * (unsigned)(a.ldq * 2) + c;
+    off_o[0] = t * (unsigned)(a.lddo * 2) + c;
+    asm volatile("" : "+v"(off_q[0]), "+v"(off_o[0]));
+  }
+  // tile i of the rows of (b, h) from token t0 on, no further than row `end`
+  __device__ __forceinline__ void issue(const WinArgs& a, int b, int h, int t0, int i, int end, char* lds) const {
+    const int r0 = t0 * a.share + i * ROWS;
+    if (tokens && r0 + ROWS <= end) {
+      const int64_t tok = (int64_t)b * a.Sq + t0 + i * N * tokens;
+      const int m0v = __builtin_amdgcn_readfirstlane((int)(size_t)lds + loads.wave * 1024);
+      load_all<N, 1, NW * 1024>(a.q + tok * a.ldq + h * a.share * DH, tokens * a.ldq, off_q, m0v);
+      load_all<N, 1, NW * 1024>(a.dout + tok * a.lddo + h * a.share * DH, tokens * a.lddo, off_o, m0v + ROWS * DH * 2);
+      return;
+    }
+    loads.rows([&](int r, int64_t& tok, int& c) {
+      const int t = r / a.share, g = r - t * a.share;
+      tok = (int64_t)b * a.Sq + t;
+      c = (h * a.share + g) * DH;
+    }, end, a.q, a.ldq, a.dout, a.lddo, r0, lds, lds + ROWS * DH * 2);
+  }
+};
+
 // dK, dV of the window: a wave owns 32 keys, the rows (queries and do) of the tokens whose windows hold any of a workgroup's keys stream.
-template <int DH, int NW, int NS>
+template <int DH, int NW, int NS, int ROWS>
 __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) {
   char* smem = dtl_smem;
-  constexpr int SLOT = 2 * kTileBytes<DH> + 2 * TILE * 4;   // queries, do, lse, D
+  constexpr int HALF = ROWS * DH * 2, SLOT = 2 * HALF + 2 * 64 * 4;   // queries, do, lse, D
   const int parts = a.bkv.parts;
   Where w;
   if (!where(a, a.bkv, id, grid, w)) return;
@@ -643,55 +706,49 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
   auto end = [&](int x) { return (n - x < a.window ? n : x + a.window) * a.share; };
   const int jl = (j0 + OWN * NW < n ? j0 + OWN * NW : n) - 1;                 // the workgroup's last key
   const int from = j0 * a.share, to_row = j0 < n ? end(jl) : from;
-  const int nt = (to_row - from + TILE - 1) / TILE;         // keys behind the sequence: zeros
+  const int nt = (to_row - from + ROWS - 1) / ROWS;         // keys behind the sequence: zeros
   const int t0 = (int)((int64_t)nt * w.part / parts), t1 = (int)((int64_t)nt * (w.part + 1) / parts);
   const bool active = j0 + wave * OWN < n;
   const int jc = j < n ? j : n > 0 ? n - 1 : 0, w0 = __builtin_amdgcn_readfirstlane(jc), w1 = __builtin_amdgcn_readlane(jc, 31);
   const int my_first = jc * a.share, my_end = end(jc);
   const int all_first = w1 * a.share, all_end = end(w0), any_first = w0 * a.share, any_end = end(w1);
-  // Heads of 128: keys, values, their two gradients and the scores are 256 registers by themselves; the values stay in LDS
-  constexpr bool kValuesInLds = DH == 128;
+  // Keys, values, their two gradients and the scores are 256 registers by themselves (heads of 64: 144 of 168): the values stay in LDS
   Frag* vl = reinterpret_cast<Frag*>(smem + NS * SLOT + wave * OWN * DH * 2) + l;
   Frag kf[DH / 16], vf[DH / 16];
   f32x16 dk[DH / 32], dv[DH / 32];
   clear(dk); clear(dv);
-  const TileLoads<DH, NW> loads(wave);
+  const RowLoads<DH, NW, ROWS> loads(a, wave);
+  constexpr int LPT = 2 * RowLoads<DH, NW, ROWS>::N + 1;
   const float* stat = (wave & 1 ? a.stat_d : a.stat_lse) + (int64_t)w.unit * a.Rp;   // (even waves bring the lse, odd ones D)
   auto issue = [&](int i) {
     char* to = smem + (i - t0) % NS * SLOT;
-    loads.rows([&](int r, int64_t& tok, int& c) {
-      const int t = r / a.share, g = r - t * a.share;
-      tok = (int64_t)w.b * a.Sq + t;
-      c = (w.h * a.share + g) * DH;
-    }, to_row, a.q, a.ldq, a.dout, a.lddo, from + i * TILE, to, to + kTileBytes<DH>);
-    load_floats(stat + from + i * TILE, to + 2 * kTileBytes<DH> + (wave & 1) * TILE * 4);
+    loads.issue(a, w.b, w.h, j0, i, to_row, to);
+    load_floats(stat + from + i * ROWS, to + 2 * HALF + (wave & 1) * 64 * 4);
   };
-  // One slot: the next tile is asked for when everyone has left this one.  The first tile goes out ahead of the wave's own keys: with few
-  // rows a workgroup is one chain of round trips.
-  static_assert(NS == 1 || NS == 2, "slots");
-  if (t0 < t1) issue(t0);
+  // The first tiles go out ahead of the wave's own keys: with few rows a workgroup is one chain of round trips.
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i)
+    if (t0 + i < t1) issue(t0 + i);
   if (active) {
     load_owned<DH>(kf, a.k + ((int64_t)w.b * a.Sk + jc) * a.ldk + w.h * DH);
     load_owned<DH>(vf, a.v + ((int64_t)w.b * a.Sk + jc) * a.ldv + w.h * DH);
     settle(kf); settle(vf);
-    if (kValuesInLds) {
 #pragma unroll
-      for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
-    }
+    for (int kk = 0; kk < DH / 16; ++kk) vl[kk * 64] = vf[kk];
   }
   auto tile = [&](int i, const char* Qs) {
-    const char* Os = Qs + kTileBytes<DH>;
-    const float* lse = reinterpret_cast<const float*>(Os + kTileBytes<DH>);
+    const char* Os = Qs + HALF;
+    const float* lse = reinterpret_cast<const float*>(Os + HALF);
 #pragma unroll(DH == 128 ? 1 : 2)
-    for (int sub = 0; sub < 2; ++sub) {
-      const int r0 = from + i * TILE + sub * 32;
+    for (int sub = 0; sub < ROWS / 32; ++sub) {
+      const int r0 = from + i * ROWS + sub * 32;
       if (r0 + 31 < any_first || r0 >= any_end) continue;
-      const Sees v{my_end - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, 0 - 4 * grp, {r0 >= all_first && r0 + 32 <= all_end, false}, {}};
+      const Sees v{my_end - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, 0 - 4 * grp, !(r0 >= all_first && r0 + 32 <= all_end), 0};
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const f32x4 ls = *reinterpret_cast<const f32x4*>(lse + sub * 32 + 8 * q + 4 * grp);
-        const f32x4 D = *reinterpret_cast<const f32x4*>(lse + TILE + sub * 32 + 8 * q + 4 * grp);
+        const f32x4 D = *reinterpret_cast<const f32x4*>(lse + 64 + sub * 32 + 8 * q + 4 * grp);
 #pragma unroll
         for (int x = 0; x < 4; ++x) { s[0][4 * q + x] = ls[x]; dp[0][4 * q + x] = D[x]; }
       }
@@ -699,11 +756,11 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
       in_a_row<DH / 8, DH == 128 ? 4 : 2>([&](int i) {
                             Two t;
                             t.rows = frag_rows<DH>(i % 2 ? Os : Qs, sub * 32, i / 2);
-                            if (kValuesInLds && i % 2) t.values = vl[i / 2 * 64];
+                            if (i % 2) t.values = vl[i / 2 * 64];
                             return t;
                           },
                           [&](int i, const Two& t) {
-                            if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kValuesInLds ? t.values : vf[i / 2], dp[0], 0, 0, 0);
+                            if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.values, dp[0], 0, 0, 0);
                             else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, kf[i / 2], s[0], 0, 0, 0);
                           });
 #pragma unroll
@@ -711,7 +768,7 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
         s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
         dp[0][x] *= s[0][x];
       }
-      if (!v.all[0]) {
+      if (v.partly) {
         asm volatile("");
 #pragma unroll
         for (int x = 0; x < 16; ++x)
@@ -730,23 +787,20 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
     }
   };
   for (int i = t0; i < t1; ++i) {
-    wait_loads<0>();                                         // (at most one tile is on the way)
+    if (i + NS - 2 < t1) wait_loads<LPT * (NS - 2)>();
+    else wait_loads<0>();
     __syncthreads();
-    if (NS == 2 && i + 1 < t1) issue(i + 1);
+    if (i + NS - 1 < t1) issue(i + NS - 1);
     if (active) tile(i, smem + (i - t0) % NS * SLOT);
-    if (NS == 1 && i + 1 < t1) {
-      __syncthreads();
-      issue(i + 1);
-    }
   }
   if (active && !(all_finite(dk) && all_finite(dv))) {
     clear(dk); clear(dv);
     load_owned<DH>(vf, a.v + ((int64_t)w.b * a.Sk + jc) * a.ldv + w.h * DH);
-    const int r1 = from + t1 * TILE < to_row ? from + t1 * TILE : to_row;
+    const int r1 = from + t1 * ROWS < to_row ? from + t1 * ROWS : to_row;
     const float* lse = a.stat_lse + (int64_t)w.unit * a.Rp;
     const float* D = a.stat_d + (int64_t)w.unit * a.Rp;
 #pragma unroll 1
-    for (int r = from + t0 * TILE; r < r1; ++r) {
+    for (int r = from + t0 * ROWS; r < r1; ++r) {
       const uint16_t* q = a.q + row_at<DH>(a, w.b, w.h, r, a.ldq);
       const uint16_t* d = a.dout + row_at<DH>(a, w.b, w.h, r, a.lddo);
       const float p = __builtin_amdgcn_exp2f((lse[r] + dot_row<DH>(kf, q)) * a.c2), dp = D[r] + dot_row<DH>(vf, d);
@@ -758,20 +812,20 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
   if (j >= a.Sk) return;
   if (one_key(a, n)) of_one_key(dk);
   if (j >= n) { clear(dk); clear(dv); }                     // (repeats of the last key)
-  const bool more = a.sink_parts && j < a.sinks;            // rows behind the window see it, too
-  if (parts == 1 && !more) {
+  if (a.sink_parts && j < a.sinks) return;                  // bwd_sink_body's
+  if (parts == 1) {
     store_owned<DH>(dk, a.scale, a.dk + ((int64_t)w.b * a.Sk + j) * a.lddk + w.h * DH);
     store_owned<DH>(dv, 1.0f, a.dv + ((int64_t)w.b * a.Sk + j) * a.lddv + w.h * DH);
   } else {
-    float* to = a.kv_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * (parts == 1 ? a.sinks : a.Sk) + j) * 2 * DH;
+    float* to = a.kv_part + (((int64_t)w.part * a.B * a.Hkv + w.unit) * a.Sk + j) * 2 * DH;
     store_owned32<DH>(dk, to);
     store_owned32<DH>(dv, to + DH);
   }
 }
 
-// dK, dV of the sinks from the tokens whose windows have left them: 32 keys, thousands of rows.  The four waves of a workgroup own the same keys and
-// walk over 32 rows each in turn, in slots of their own and without barriers; their sums meet in LDS and leave as a part of the workgroup's own.
-// (The first block of keys had all the rows at first, one workgroup's walk: 4 x 4096 tokens, 16 heads over 2 of 128, a window of 1024, 1568 us.)
+// dK, dV of the sinks, which all rows behind them see: 32 keys, thousands of rows.  The four waves of a workgroup own the same keys and walk over 32 rows
+// each in turn, in slots of their own and without barriers; their sums meet in LDS and are the result, or a part of it.
+// (The first block of keys had all the rows at first, one workgroup's walk: 4 x 4096 tokens, 16 heads over 2 of 128, a window of 1024, 1568 us, 523 without.)
 template <int DH>
 __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
   constexpr int ROWS = 32, HALF = ROWS * DH * 2, SLOT = 2 * HALF;
@@ -780,10 +834,10 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, grp = l >> 5;
   const int n = live_of(a, b), j0 = block * OWN, j = j0 + (l & 31);
   const int last = a.sinks - 1 < n - 1 ? a.sinks - 1 : n - 1, jc = j < last ? j : last > 0 ? last : 0;
-  const int from = (n - j0 < a.window ? n : j0 + a.window) * a.share, to_row = n * a.share;
+  const int from_token = j0 < n ? j0 : n, from = from_token * a.share, to_row = n * a.share;
   const int nt = (to_row - from + ROWS - 1) / ROWS;
   const int t0 = (int)((int64_t)nt * part / a.sink_parts), t1 = (int)((int64_t)nt * (part + 1) / a.sink_parts);
-  const int my_first = (n - jc < a.window ? n : jc + a.window) * a.share, all_first = __builtin_amdgcn_readlane(my_first, 31);
+  const int my_first = jc * a.share, all_first = __builtin_amdgcn_readlane(my_first, 31);
   char* slot = dtl_smem + wave * SLOT;
   // keys and values in LDS, one copy for all waves: with both gradients and the scores they are too many registers
   Frag* own = reinterpret_cast<Frag*>(dtl_smem + 4 * SLOT) + l;
@@ -798,7 +852,7 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
   __syncthreads();
   f32x16 dk[DH / 32], dv[DH / 32];
   clear(dk); clear(dv);
-  const TileLoads<DH, 1, ROWS> loads(0);
+  const RowLoads<DH, 1, ROWS> loads(a, 0);
   const float* stat_lse = a.stat_lse + (int64_t)unit * a.Rp;
   const float* stat_d = a.stat_d + (int64_t)unit * a.Rp;
   const int first = t0 + wave;
@@ -809,11 +863,7 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
     int same = 0;
     asm volatile("" : "+s"(same));                            // (fragments' addresses are not kept over the loop: there are no registers for them)
     char* Qs = slot + same;
-    loads.rows([&](int r, int64_t& tok, int& c) {
-      const int t = r / a.share, g = r - t * a.share;
-      tok = (int64_t)b * a.Sq + t;
-      c = (h * a.share + g) * DH;
-    }, to_row, a.q, a.ldq, a.dout, a.lddo, r0, Qs, Qs + HALF);
+    loads.issue(a, b, h, from_token, i, to_row, Qs);
     f32x16 s[1], dp[1];
 #pragma unroll
     for (int q = 0; q < 4; ++q)
@@ -837,13 +887,13 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
                        if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, dp[0], 0, 0, 0);
                        else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, s[0], 0, 0, 0);
                      });
-    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, {r0 >= all_first && r0 + ROWS <= to_row, false}, {}};
+    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, !(r0 >= all_first && r0 + ROWS <= to_row), 0};
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       dp[0][x] *= s[0][x];
     }
-    if (!v.all[0]) {
+    if (v.partly) {
       asm volatile("");
 #pragma unroll
       for (int x = 0; x < 16; ++x)
@@ -872,6 +922,8 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
       }
     }
   }
+  if (n == 1) of_one_key(dk);
+  if (j >= n) { clear(dk); clear(dv); }                       // (repeats of the last key)
   // the waves' sums, dk's and then dv's: registers through LDS, an equal share of them to each wave
   float* image = reinterpret_cast<float*>(dtl_smem);          // [4][DH / 2][64]: the slots
   float* to = a.sink_part + (((int64_t)part * a.B * a.Hkv + unit) * a.sinks + j) * 2 * DH;
@@ -883,61 +935,56 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
 #pragma unroll
       for (int x = 0; x < 16; ++x) image[(wave * (DH / 2) + dt * 16 + x) * 64 + l] = what ? dv[dt][x] : dk[dt][x];
     __syncthreads();
-    if (j < a.sinks) {
+    if (j >= a.sinks) continue;
+    uint16_t* out = what ? a.dv + ((int64_t)b * a.Sk + j) * a.lddv + h * DH : a.dk + ((int64_t)b * a.Sk + j) * a.lddk + h * DH;
+    const float mul = what ? 1.0f : a.scale;
 #pragma unroll
-      for (int x = 0; x < DH / 8; x += 4) {
-        const int reg = wave * (DH / 8) + x;
-        f32x4 v;
+    for (int x = 0; x < DH / 8; x += 4) {
+      const int reg = wave * (DH / 8) + x, col = (reg >> 4) * 32 + acc_row(reg & 15, grp);
+      f32x4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = 0.f;
+      for (int e = 0; e < 4; ++e) {
+        v[e] = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[e] += image[(i * (DH / 2) + reg + e) * 64 + l];
-        }
-        *reinterpret_cast<f32x4*>(to + what * DH + (reg >> 4) * 32 + acc_row(reg & 15, grp)) = v;
+        for (int i = 0; i < 4; ++i) v[e] += image[(i * (DH / 2) + reg + e) * 64 + l];
       }
+      if (a.sink_parts > 1) *reinterpret_cast<f32x4*>(to + what * DH + col) = v;
+      else *reinterpret_cast<u32x2*>(out + col) = u32x2{rv_pack_bf16x2(v.x * mul, v.y * mul), rv_pack_bf16x2(v.z * mul, v.w * mul)};
     }
   }
 }
 template <int DH> constexpr int kSinkLds = 4 * 2 * 32 * DH * 2 + 2 * 32 * DH * 2;
-template <int DH, int NW, int NS> constexpr int kKvLds = NS * (2 * kTileBytes<DH> + 2 * TILE * 4) + (DH == 128 ? NW * OWN * DH * 2 : 0);
-template <int DH> constexpr int kQLds = 4 * kTileBytes<DH>;
+template <int DH, int NW, int NS, int ROWS> constexpr int kKvLds = NS * (2 * ROWS * DH * 2 + 2 * 64 * 4) + NW * OWN * DH * 2;
+template <int DH, int NS> constexpr int kQLds = NS * 2 * kTileBytes<DH>;
 constexpr int most(int x, int y) { return x > y ? x : y; }
-template <int DH, int NW, int NS> constexpr int kBwdLds = most(kKvLds<DH, NW, NS>, most(kQLds<DH>, kSinkLds<DH>));
+template <int DH, int NW, int NS, int ROWS, int NS_Q> constexpr int kBwdLds = most(kKvLds<DH, NW, NS, ROWS>, most(kQLds<DH, NS_Q>, kSinkLds<DH>));
 // All in one launch, the longer workgroups (dK and dV: four products to dQ's three) first.
-template <int DH, int NW, int NS>
+template <int DH, int NW, int NS, int ROWS, int NS_Q>
 __global__ __launch_bounds__(64 * NW, DH == 128 ? 2 : 3) void window_bwd_kernel(WinArgs a) {
   static_assert(NW == 4, "bwd_sink_body");
   const int id = blockIdx.x, others = a.kv_grid + a.sink_grid;
-  if (id < a.kv_grid) bwd_kv_body<DH, NW, NS>(a, id, a.kv_grid);
+  if (id < a.kv_grid) bwd_kv_body<DH, NW, NS, ROWS>(a, id, a.kv_grid);
   else if (id < others) bwd_sink_body<DH>(a, id - a.kv_grid);
-  else bwd_q_body<DH, NW, 2>(a, id - others, gridDim.x - others);
+  else bwd_q_body<DH, NW, NS_Q>(a, id - others, gridDim.x - others);
 }
-// parts -> dq (KV false), or dk and dv (of the sinks alone where the others' are no parts)
+// parts -> dq (KV false), or dk and dv, of the sinks alone where the others' are no parts
 template <int DH, bool KV>
 __global__ __launch_bounds__(256) void window_bwd_join_kernel(WinArgs a) {
   constexpr int W = KV ? 2 * DH : DH;
-  const int parts = KV ? a.bkv.parts : a.bq.parts, per = !KV ? a.R : parts > 1 ? a.Sk : a.sinks;
-  const float* sums = KV ? a.kv_part : a.q_part;
-  const int64_t rows = (int64_t)a.B * a.Hkv * per;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
+  const int per = !KV ? a.R : a.bkv.parts > 1 ? a.Sk : a.sinks;
+  const int64_t units = (int64_t)a.B * a.Hkv, i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / (W / 8);
   const int c = (int)(i % (W / 8)) * 8;
-  if (row >= rows) return;
+  if (row >= units * per) return;
+  const int unit = (int)(row / per), r = (int)(row - (int64_t)unit * per), b = unit / a.Hkv, h = unit % a.Hkv;
+  const bool sink = KV && a.sink_parts && r < a.sinks;
+  if (sink && a.sink_parts == 1) return;                    // there already
+  const int parts = !KV ? a.bq.parts : sink ? a.sink_parts : a.bkv.parts, rows = !KV ? a.R : sink ? a.sinks : a.Sk;
+  const float* from = (!KV ? a.q_part : sink ? a.sink_part : a.kv_part) + ((int64_t)unit * rows + r) * W + c;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll 4
   for (int s = 0; s < parts; ++s) {
-    const f32x4* p = reinterpret_cast<const f32x4*>(sums + (s * rows + row) * W + c);
+    const f32x4* p = reinterpret_cast<const f32x4*>(from + s * units * rows * W);
     v[0] += p[0]; v[1] += p[1];
-  }
-  const int unit = (int)(row / per), r = (int)(row - (int64_t)unit * per), b = unit / a.Hkv, h = unit % a.Hkv;
-  if (KV && r < a.sinks) {
-    const int64_t step = (int64_t)a.B * a.Hkv * a.sinks * W;
-    const float* from = a.sink_part + ((int64_t)unit * a.sinks + r) * W + c;
-#pragma unroll 4
-    for (int s = 0; s < a.sink_parts; ++s) {
-      const f32x4* p = reinterpret_cast<const f32x4*>(from + s * step);
-      v[0] += p[0]; v[1] += p[1];
-    }
   }
   const bool values = KV && c >= DH;
   if (!values) { v[0] *= a.scale; v[1] *= a.scale; }
@@ -959,7 +1006,7 @@ struct WinPlan {
   int window, sinks;                       // no more than the rows
   int at_once;                             // sequences
   size_t fwd_ml, fwd_bytes;                // forward: [sums][pairs]
-  size_t d, part, kv_part, sink_part, bwd_bytes;   // backward: [lse][D][sums of dq][of dk and dv][of the sinks' from behind the window]
+  size_t d, part, kv_part, sink_part, bwd_bytes;   // backward: [lse][D][sums of dq][of dk and dv][of the sinks']
 };
 bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t Hkv, int64_t dh, int64_t window, int64_t sinks, bool backward) {
   if (B < 1 || Sq < 1 || Sk < 1 || H < 1 || Hkv < 1 || H % Hkv || (dh != 64 && dh != 128) || window < 1 || sinks < 0) return false;
@@ -986,10 +1033,9 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   p.q_parts = parts_for(U * up(R, OWN * 4), tiles(OWN * 4, TILE), 512, 4);
   const int64_t seen = (p.window + OWN * 4) * share < R ? (p.window + OWN * 4) * share : R;
   p.kv_parts = parts_for(U * up(Sk, OWN * 4), up(seen, TILE), 256, 4);
-  // tokens whose window leaves sinks: 512 workgroups, each with 8 rounds of its waves' 32 rows or more
-  const int64_t behind = p.sinks && p.window < Sk ? (Sk - p.window) * share : 0;
-  p.sink_blocks = behind ? (int)up(p.sinks, OWN) : 0;
-  p.sink_parts = behind ? parts_for(U * p.sink_blocks, up(behind, 4 * OWN), 512, 8) : 0;
+  // sinks that windows leave: 512 workgroups, each with 8 rounds of its waves' 32 rows or more
+  p.sink_blocks = p.sinks && p.window < Sk ? (int)up(p.sinks, OWN) : 0;
+  p.sink_parts = p.sink_blocks ? parts_for(U * p.sink_blocks, up(R, 4 * OWN), 512, 8) : 0;
   // threads of the largest launch, a sequence; of blocks that are dealt out in groups (deal) up to eight for seven more
   auto dealt = [&](int64_t blocks, int parts) { const int64_t n = blocks * parts; return Hkv * (n + (n < 8 ? n : 8) - 1); };
   auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
@@ -1011,8 +1057,8 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   p.d = round((size_t)4 * U * p.Rp);
   p.part = 2 * p.d;
   p.kv_part = p.part + (p.q_parts > 1 ? round((size_t)4 * p.q_parts * U * R * dh) : 0);
-  p.sink_part = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : p.sink_parts ? round((size_t)8 * U * p.sinks * dh) : 0);
-  p.bwd_bytes = p.sink_part + round((size_t)8 * p.sink_parts * U * p.sinks * dh);
+  p.sink_part = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : 0);
+  p.bwd_bytes = p.sink_part + (p.sink_parts > 1 ? round((size_t)8 * p.sink_parts * U * p.sinks * dh) : 0);
   return true;
 }
 
@@ -1067,7 +1113,7 @@ rv_status forward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
   else RV_TRY((launch<window_join_kernel<DH, 1>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
   return RV_OK;
 }
-template <int DH, int NW, int NS>
+template <int DH, int NW, int NS, int ROWS, int NS_Q>
 rv_status backward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
   const int64_t U = (int64_t)a.B * a.Hkv;
   a.stat_lse = (float*)work; a.stat_d = (float*)(work + p.d); a.q_part = (float*)(work + p.part); a.kv_part = (float*)(work + p.kv_part);
@@ -1076,9 +1122,9 @@ rv_status backward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
   const int64_t kv = deal(a.bkv, a, a.length != nullptr, up(a.Sk, OWN * NW), p.kv_parts);
   const int64_t q = deal(a.bq, a, a.length != nullptr, up(a.R, OWN * NW), p.q_parts);
   a.kv_grid = (int)kv; a.sink_grid = (int)(U * p.sink_blocks * p.sink_parts);
-  RV_TRY((launch<window_bwd_kernel<DH, NW, NS>>(a, kv + a.sink_grid + q, 64 * NW, kBwdLds<DH, NW, NS>, st)));
+  RV_TRY((launch<window_bwd_kernel<DH, NW, NS, ROWS, NS_Q>>(a, kv + a.sink_grid + q, 64 * NW, kBwdLds<DH, NW, NS, ROWS, NS_Q>, st)));
   if (p.q_parts > 1) RV_TRY((launch<window_bwd_join_kernel<DH, false>>(a, up(U * a.R * (DH / 8), 256), 256, 0, st)));
-  if (p.kv_parts > 1 || p.sink_parts) RV_TRY((launch<window_bwd_join_kernel<DH, true>>(a, up(U * (p.kv_parts > 1 ? a.Sk : a.sinks) * (DH / 4), 256), 256, 0, st)));
+  if (p.kv_parts > 1 || p.sink_parts > 1) RV_TRY((launch<window_bwd_join_kernel<DH, true>>(a, up(U * (p.kv_parts > 1 ? a.Sk : a.sinks) * (DH / 4), 256), 256, 0, st)));
   return RV_OK;
 }
 
@@ -1127,7 +1173,8 @@ extern "C" rv_status rv_k_window_attention_bwd(const void* q, int64_t ldq, const
   a.dq = (uint16_t*)dq; a.lddq = lddq; a.dk = (uint16_t*)dk; a.lddk = lddk; a.dv = (uint16_t*)dv; a.lddv = lddv;
   for (int b = 0; b < B; b += p.at_once) {
     const WinArgs some = sequences(a, p, b);
-    RV_TRY(d_head == 64 ? (backward<64, 4, 2>(some, p, (char*)work, (hipStream_t)stream)) : (backward<128, 4, 1>(some, p, (char*)work, (hipStream_t)stream)));
+    RV_TRY(d_head == 64 ? (backward<64, 4, 2, 64, 2>(some, p, (char*)work, (hipStream_t)stream))
+                        : (backward<128, 4, 2, 32, 2>(some, p, (char*)work, (hipStream_t)stream)));
   }
   return RV_OK;
 }
