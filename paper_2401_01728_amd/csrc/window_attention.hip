@@ -86,10 +86,6 @@ __device__ __forceinline__ Walk walk_of(const WinArgs& a, int start, int n, int 
   w.row0 = uniform((int)(key < (unsigned)a.Sk ? key : a.sinks + (key - a.sinks) % (unsigned)a.ring));
   return w;
 }
-// Which streamed rows, counted from the first, a lane sees: x <= up and (x > low or x < first).  partly: not all lanes of the wave see all of 32 of them;
-// none: no lane sees any.  The three are less 4 (lane / 32), so that the rows of a lane's registers (acc_row) are compared as constants: kept, they
-// would be 16 registers or 32.
-struct Sees { int up, low, first; int partly, none; };            // bit 0: the rows from 0 on, bit 1: from 32 on
 struct Tile { int row, keys; };                                   // its first key's row, and how many there are
 template <int T>
 __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) {
@@ -101,32 +97,75 @@ __device__ __forceinline__ Tile tile_of(const WinArgs& a, const Walk& w, int i) 
   t.keys = left < T ? left : T;
   return t;
 }
-// of tile i, its keys from `at` on; a lane's token t; tokens first .. last are the wave's
+// What a wave sees of the tile's keys from one on: numbers that are the wave's, so that a tile of which all of it sees all costs comparisons alone.
+struct Edge {
+  int at;                                // that key, counted as the others are: in the range (or among the sinks)
+  int up_first, up_last;                 // the last key that the wave's first token sees, and its last one
+  int reach;                             // keys that a token sees up to its last one
+  int sinks;                             // keys in front of this one are seen from everywhere
+  bool sink;
+};
 template <int T>
-__device__ __forceinline__ Sees sees_of(const WinArgs& a, const Walk& w, int i, int at, int t, int first, int last) {
-  Sees s{0, 0, 0, 0, 0};
-  const bool sink = i < w.sink_tiles;
-  const int off = (sink ? i : i - w.sink_tiles) * T + at, shift = w.shift - off, sinks = w.first - off;
-#pragma unroll
-  for (int sub = 0; sub < 2; ++sub) {
-    const int x = 32 * sub;
-    const bool all = sink ? a.sinks - off >= x + 32 && w.start + first >= off + x + 31
-                          : x + 31 <= first + shift && (last + shift - a.window < x || x + 32 <= sinks);
-    const bool none = sink ? off + x >= a.sinks : last + shift < x || (first + shift - a.window >= x + 31 && sinks <= x);
-    s.partly |= (int)!all << sub;
-    s.none |= (int)none << sub;
-  }
-  const int grp4 = (threadIdx.x & 32) >> 3;
-  if (sink) {
-    // (a token in front of the last sink has the range apart where its own row has been taken)
-    const int top = w.start + t < a.sinks ? w.start + t : a.sinks - 1;
-    s.up = top - off - grp4; s.low = -5; s.first = 0;
-  } else {
-    s.up = t + shift - grp4; s.low = s.up - a.window; s.first = sinks - grp4;
-  }
-  return s;
+__device__ __forceinline__ Edge edge_of(const WinArgs& a, const Walk& w, int i, int at, int first, int last) {
+  Edge e;
+  e.sink = i < w.sink_tiles;
+  e.at = (e.sink ? i : i - w.sink_tiles) * T + at;
+  // (a token in front of the last sink has the range apart where its own row has been taken)
+  const int top = a.sinks - 1;
+  e.up_first = e.sink ? (w.start + first < top ? w.start + first : top) : first + w.shift;
+  e.up_last = e.sink ? (w.start + last < top ? w.start + last : top) : last + w.shift;
+  e.reach = e.sink ? a.sinks : a.window;
+  e.sinks = e.sink ? 0 : w.first;
+  return e;
 }
-// The tiles, from the first up to but not including the second, all of whose keys all of a wave's tokens see as far as the window goes: most of a long
+// of the 32 keys from AT on: nobody sees any; some are ahead of a token; some are behind one
+template <int AT>
+__device__ __forceinline__ bool none(const Edge& e) {
+  return e.at + AT > e.up_last || (e.at + AT + 31 <= e.up_first - e.reach && e.at + AT >= e.sinks);
+}
+template <int AT>
+__device__ __forceinline__ bool ahead(const Edge& e) { return e.at + AT + 31 > e.up_first; }
+template <int AT>
+__device__ __forceinline__ bool behind(const Edge& e) { return e.at + AT <= e.up_last - e.reach && e.at + AT + 32 > e.sinks; }
+// Which rows, counted from a tile's first, a lane sees: x <= up and (x > low or x < first).  The three are less 4 (lane / 32), so that the rows of a lane's
+// registers (acc_row) are compared as constants: kept, they would be 16 registers or 32.
+struct Limits { int up, low, first; };
+__device__ __forceinline__ Limits limits(const WinArgs& a, const Walk& w, const Edge& e, int t) {
+  const int from = e.at + ((threadIdx.x & 32) >> 3), top = a.sinks - 1;
+  const int up = (e.sink ? (w.start + t < top ? w.start + t : top) : t + w.shift) - from;
+  return {up, up - e.reach, e.sinks - from};
+}
+__device__ __forceinline__ bool sees(const Limits& s, int x) { return x <= s.up && (x > s.low || x < s.first); }
+// hide(register) for what a lane does not see of 32 rows.  The empty asm keeps it behind its branch: as selects, the compiler has every tile pay for it.
+template <int AT, typename Hide>
+__device__ __forceinline__ void mask(const Limits& s, Hide hide) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (!sees(s, AT + acc_row(r, 0))) hide(r);
+    if (r % 2) __builtin_amdgcn_sched_barrier(0);           // (all comparisons first would take the scalar registers that the walk is kept in)
+  }
+}
+// and where nothing is behind
+template <int AT, typename Hide>
+__device__ __forceinline__ void mask_ahead(const Limits& s, Hide hide) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (AT + acc_row(r, 0) > s.up) hide(r);
+    if (r % 2) __builtin_amdgcn_sched_barrier(0);
+  }
+}
+template <int AT, typename Hide>
+__device__ __forceinline__ void mask_edge(const WinArgs& a, const Walk& w, const Edge& e, int t, Hide hide) {
+  if (behind<AT>(e)) {                   // (wave-uniform)
+    asm volatile("");
+    mask<AT>(limits(a, w, e, t), hide);
+  } else if (ahead<AT>(e)) {
+    asm volatile("");
+    mask_ahead<AT>(limits(a, w, e, t), hide);
+  }
+}
+
+// The tiles, from the first up to but not including the second, of which all of a wave's tokens see all as far as the window goes: most of a long
 // walk, where nothing else is looked at.
 struct Span { int first, end; };
 template <int T>
@@ -134,8 +173,6 @@ __device__ __forceinline__ Span whole_tiles(const WinArgs& a, const Walk& w, int
   const int left = last + w.shift - a.window, right = first + w.shift + 1;     // keys up to `left` are behind a token, from `right` on ahead of one
   return {uniform(w.sink_tiles + (left < 0 ? 0 : left / T + 1)), uniform(w.sink_tiles + (right < 0 ? 0 : right / T))};
 }
-__device__ __forceinline__ bool sees(const Sees& s, int x) { return x <= s.up && (x > s.low || x < s.first); }
-
 // One load of 64 lanes: 16 bytes each from base + off to LDS at lds + AT.
 template <int AT>
 __device__ __forceinline__ void load_at(const uint16_t* base, unsigned off, int lds) {
@@ -256,7 +293,7 @@ __device__ __forceinline__ void one_by_one(const WinArgs& a, const Walk& w, int 
 #pragma unroll 1
   for (int i = t0; i < t1; i += step) {
     const Tile tile = tile_of<T>(a, w, i);
-    const Sees v = sees_of<T>(a, w, i, 0, t, first, last);
+    const Limits v = limits(a, w, edge_of<T>(a, w, i, 0, first, last), t);
 #pragma unroll 1
     for (int x = 0; x < tile.keys; ++x) use(tile.row + x < a.Sk ? tile.row + x : tile.row + x - a.ring, sees(v, x - grp4));
   }
@@ -264,15 +301,12 @@ __device__ __forceinline__ void one_by_one(const WinArgs& a, const Walk& w, int 
 
 // Softmax of a tile of scores as in cross_attention.hip: s becomes exp2(s c2 - m), the factor for what was summed before is returned.
 template <int SUBS>
-__device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], float c2, const Sees& v, float& m, float& lsum) {
-#pragma unroll
-  for (int sub = 0; sub < SUBS; ++sub)
-    if (v.partly >> sub & 1) {           // (wave-uniform)
-      asm volatile("");
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!sees(v, sub * 32 + acc_row(r, 0))) s[sub][r] = -INFINITY;
-    }
+__device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum) {
+  const float c2 = a.c2;
+  if (!whole) {
+    mask_edge<0>(a, w, e, t, [&](int r) { s[0][r] = -INFINITY; });
+    if constexpr (SUBS == 2) mask_edge<32>(a, w, e, t, [&](int r) { s[SUBS - 1][r] = -INFINITY; });
+  }
   float mx = s[0][0];
 #pragma unroll
   for (int sub = 0; sub < SUBS; ++sub)
@@ -336,7 +370,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   const Walk walk = own.template walk<TILE>(a);
   const int t0 = (int)((int64_t)walk.tiles * w.part / parts), t1 = (int)((int64_t)walk.tiles * (w.part + 1) / parts);
   const KeyLoads<DH, NW, TILE> loads(a, w, wave);
-  const Span whole = whole_tiles<TILE>(a, walk, own.first, own.last);
+  const Span span = whole_tiles<TILE>(a, walk, own.first, own.last);
   constexpr int LPT = loads.PER_TILE;
   auto issue = [&](int i) { loads.issue(a, walk, i, smem + (i - t0) % NS * SLOT); };
 #pragma unroll
@@ -349,13 +383,13 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   clear(o);
   float m = -INFINITY, lsum = 0.f;
   // SUBS x 32 keys of a tile
-  auto some = [&](const char* Ks, const Sees& v) {
+  auto some = [&](const char* Ks, bool whole, const Edge& e) {
     const char* Vs = Ks + kTileBytes<DH>;
     f32x16 s[SUBS];
     clear(s);
     in_a_row<SUBS * DH / 16, DH == 128 ? 6 : 3>([&](int i) { return frag_rows<DH>(Ks, i % SUBS * 32, i / SUBS); },
                         [&](int i, const Frag& f) { s[i % SUBS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / SUBS], s[i % SUBS], 0, 0, 0); });
-    const float alpha = softmax_tile(s, a.c2, v, m, lsum);
+    const float alpha = softmax_tile(s, a, walk, whole, e, own.t, m, lsum);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {    // maxima that have settled leave the sums as they are
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
@@ -369,9 +403,11 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
   auto tile = [&](int i, const char* Ks) {
 #pragma unroll 1
     for (int at = 0; at < TILE; at += 32 * SUBS) {
-      Sees v{0, 0, 0, 0, 0};
-      if (i < whole.first || i >= whole.end) v = sees_of<TILE>(a, walk, i, at, own.t, own.first, own.last);
-      if ((v.none & (SUBS == 1 ? 1 : 3)) != (SUBS == 1 ? 1 : 3)) some(Ks + at * DH * 2, v);
+      // (32 keys at a time the span costs more scalar registers than it saves comparisons: 4 x 2000 tokens of 16 heads, a window of 64 20.3 us, 19.3 without)
+      const bool whole = SUBS == 2 && i >= span.first && i < span.end;
+      Edge e{};
+      if (!whole) e = edge_of<TILE>(a, walk, i, at, own.first, own.last);
+      if (whole || !none<0>(e) || (SUBS == 2 && !none<32>(e))) some(Ks + at * DH * 2, whole, e);
     }
   };
   for (int i = t0; i < t1; ++i) {
@@ -436,12 +472,12 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
     if (i + NS - 1 < mine) { issue(i + NS - 1); wait_loads<LPT * (NS - 1)>(); }
     else wait_loads<0>();
     const char* Ks = ring + i % NS * SLOT;
-    const Sees v = sees_of<TOKEN_KEYS>(a, walk, t0 + wave + i * TOKEN_NW, 0, own.t, own.first, own.last);
+    const Edge e = edge_of<TOKEN_KEYS>(a, walk, t0 + wave + i * TOKEN_NW, 0, own.first, own.last);
     f32x16 s[1];
     clear(s);
     in_a_row<DH / 16, 4>([&](int i) { return frag_rows<DH>(Ks, 0, i); },
                          [&](int i, const Frag& f) { s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i], s[0], 0, 0, 0); });
-    const float alpha = softmax_tile(s, a.c2, v, m, lsum);
+    const float alpha = softmax_tile(s, a, walk, false, e, own.t, m, lsum);
     if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
 #pragma unroll
       for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
@@ -596,7 +632,6 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
   f32x16 dq[DH / 32];
   clear(dq);
   const KeyLoads<DH, NW, TILE> loads(a, w, wave);
-  const Span whole = whole_tiles<TILE>(a, walk, own.first, own.last);
   constexpr int LPT = loads.PER_TILE;
   auto issue = [&](int i) { loads.issue(a, walk, i, smem + (i - t0) % NS * SLOT); };
 #pragma unroll
@@ -613,9 +648,8 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
     const char* Vs = Ks + kTileBytes<DH>;
 #pragma unroll(DH == 128 ? 1 : 2)
     for (int sub = 0; sub < 2; ++sub) {
-      Sees v{0, 0, 0, 0, 0};
-      if (i < whole.first || i >= whole.end) v = sees_of<TILE>(a, walk, i, sub * 32, own.t, own.first, own.last);
-      if (v.none & 1) continue;
+      const Edge e = edge_of<TILE>(a, walk, i, sub * 32, own.first, own.last);
+      if (none<0>(e)) continue;
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int x = 0; x < 16; ++x) { s[0][x] = lse; dp[0][x] = D; }
@@ -626,12 +660,7 @@ __device__ __forceinline__ void bwd_q_body(const WinArgs& a, int id, int grid) {
                           });
 #pragma unroll
       for (int x = 0; x < 16; ++x) dp[0][x] *= __builtin_amdgcn_exp2f(s[0][x] * a.c2);
-      if (v.partly & 1) {
-        asm volatile("");
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (!sees(v, acc_row(x, 0))) dp[0][x] = 0.f;
-      }
+      mask_edge<0>(a, walk, e, own.t, [&](int r) { dp[0][r] = 0.f; });
       const Frag ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
       add_product<DH, 1>(dq, Ks + sub * 32 * DH * 2, ds);
     }
@@ -743,7 +772,6 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
     for (int sub = 0; sub < ROWS / 32; ++sub) {
       const int r0 = from + i * ROWS + sub * 32;
       if (r0 + 31 < any_first || r0 >= any_end) continue;
-      const Sees v{my_end - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, 0 - 4 * grp, !(r0 >= all_first && r0 + 32 <= all_end), 0};
       f32x16 s[1], dp[1];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -768,11 +796,10 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
         s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
         dp[0][x] *= s[0][x];
       }
-      if (v.partly) {
+      if (r0 < all_first || r0 + 32 > all_end) {           // (wave-uniform)
         asm volatile("");
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (!sees(v, acc_row(x, 0))) s[0][x] = dp[0][x] = 0.f;
+        const int from = r0 + 4 * grp;
+        mask<0>(Limits{my_end - 1 - from, my_first - 1 - from, -4 * grp}, [&](int r) { s[0][r] = dp[0][r] = 0.f; });
       }
       const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
       const char* O = Os + sub * 32 * DH * 2;
@@ -887,17 +914,15 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
                        if (i % 2) dp[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, dp[0], 0, 0, 0);
                        else s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t.rows, t.own, s[0], 0, 0, 0);
                      });
-    const Sees v{to_row - 1 - r0 - 4 * grp, my_first - 1 - r0 - 4 * grp, -4 * grp, !(r0 >= all_first && r0 + ROWS <= to_row), 0};
 #pragma unroll
     for (int x = 0; x < 16; ++x) {
       s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       dp[0][x] *= s[0][x];
     }
-    if (v.partly) {
+    if (r0 < all_first || r0 + ROWS > to_row) {
       asm volatile("");
-#pragma unroll
-      for (int x = 0; x < 16; ++x)
-        if (!sees(v, acc_row(x, 0))) s[0][x] = dp[0][x] = 0.f;
+      const int r1 = r0 + 4 * grp;
+      mask<0>(Limits{to_row - 1 - r1, my_first - 1 - r1, -4 * grp}, [&](int r) { s[0][r] = dp[0][r] = 0.f; });
     }
     const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
     add_product<DH, 1>(dv, Os, p);
