@@ -207,10 +207,11 @@ rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, in
  *                      sinks + (p - sinks) mod (rows - sinks); sinks counts as rows - 1 at most.  Of two tokens of a call with one row the
  *                      later is kept; no other row is touched.
  * Backward: dq_out, dk_out are the gradients of q_out and k_out (without a cache), dq, dk those of q and k, rows lddq_out .. apart; dq may be
- * dq_out and dk dk_out.  q and k are the forward's inputs, read with a norm only (NULL else; dq and dk may not be q and k unless
- * dq_out and dk_out are others).  dgamma_q, dgamma_k fp32 [d_head] or NULL.  v, *_out, rows, sinks are not looked at.
+ * dq_out or q, and dk dk_out or k, with its pitch.  q and k are the forward's inputs, read with a norm only (NULL else).
+ * dgamma_q, dgamma_k fp32 [d_head] or NULL.  v, *_out, rows, sinks are not looked at.
  *   work               of the backward with dgamma_q or dgamma_k: device, 256-byte aligned, rv_k_rotary_work bytes; calls that may run at one time
  *                      need one each.
+ * A head of zeros has no norm where eps is 0: NaN.
  * A result is computed in 32 bits and rounded once; an angle is off by less than 2^-24 turns.  No atomics: results do not vary.  d_head is 64 or 128;
  * B <= 2^20, S <= 2^24, B * S <= 2^30, up to 2^12 heads; pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (start, length, pos, dgamma:
  * 4, freq: 8).  Outputs must not share memory with inputs or one another but as said (columns of one matrix do not).

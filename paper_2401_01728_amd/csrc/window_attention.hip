@@ -136,32 +136,48 @@ __device__ __forceinline__ Limits limits(const WinArgs& a, const Walk& w, const 
   return {up, up - e.reach, e.sinks - from};
 }
 __device__ __forceinline__ bool sees(const Limits& s, int x) { return x <= s.up && (x > s.low || x < s.first); }
-// hide(register) for what a lane does not see of 32 rows.  The empty asm keeps it behind its branch: as selects, the compiler has every tile pay for it.
+// hide(register) for what a lane does not see of 32 rows: what is ahead of it, what is behind, both where sinks are among them.
+// (All comparisons first would take the scalar registers that the walk is kept in.)
 template <int AT, typename Hide>
-__device__ __forceinline__ void mask(const Limits& s, Hide hide) {
+__device__ __forceinline__ void mask_ahead(int up, Hide hide) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    if (!sees(s, AT + acc_row(r, 0))) hide(r);
-    if (r % 2) __builtin_amdgcn_sched_barrier(0);           // (all comparisons first would take the scalar registers that the walk is kept in)
-  }
-}
-// and where nothing is behind
-template <int AT, typename Hide>
-__device__ __forceinline__ void mask_ahead(const Limits& s, Hide hide) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    if (AT + acc_row(r, 0) > s.up) hide(r);
+    if (AT + acc_row(r, 0) > up) hide(r);
     if (r % 2) __builtin_amdgcn_sched_barrier(0);
   }
 }
 template <int AT, typename Hide>
+__device__ __forceinline__ void mask_behind(int low, Hide hide) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (AT + acc_row(r, 0) <= low) hide(r);
+    if (r % 2) __builtin_amdgcn_sched_barrier(0);
+  }
+}
+template <int AT, typename Hide>
+__device__ __forceinline__ void mask_all(const Limits& s, Hide hide) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    if (!sees(s, AT + acc_row(r, 0))) hide(r);
+    if (r % 2) __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// The empty asm keeps each behind its (wave-uniform) branch: as selects, the compiler has every tile pay for them.
+template <int AT, typename Hide>
 __device__ __forceinline__ void mask_edge(const WinArgs& a, const Walk& w, const Edge& e, int t, Hide hide) {
-  if (behind<AT>(e)) {                   // (wave-uniform)
+  const bool back = behind<AT>(e);
+  if (back && e.sinks > e.at + AT) {
     asm volatile("");
-    mask<AT>(limits(a, w, e, t), hide);
-  } else if (ahead<AT>(e)) {
+    mask_all<AT>(limits(a, w, e, t), hide);
+    return;
+  }
+  if (back) {
     asm volatile("");
-    mask_ahead<AT>(limits(a, w, e, t), hide);
+    mask_behind<AT>(limits(a, w, e, t).low, hide);
+  }
+  if (ahead<AT>(e)) {
+    asm volatile("");
+    mask_ahead<AT>(limits(a, w, e, t).up, hide);
   }
 }
 
@@ -796,10 +812,14 @@ __device__ __forceinline__ void bwd_kv_body(const WinArgs& a, int id, int grid) 
         s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
         dp[0][x] *= s[0][x];
       }
-      if (r0 < all_first || r0 + 32 > all_end) {           // (wave-uniform)
+      auto hide = [&](int r) { s[0][r] = dp[0][r] = 0.f; };
+      if (r0 < all_first) {                                // (wave-uniform)
         asm volatile("");
-        const int from = r0 + 4 * grp;
-        mask<0>(Limits{my_end - 1 - from, my_first - 1 - from, -4 * grp}, [&](int r) { s[0][r] = dp[0][r] = 0.f; });
+        mask_behind<0>(my_first - 1 - r0 - 4 * grp, hide);
+      }
+      if (r0 + 32 > all_end) {
+        asm volatile("");
+        mask_ahead<0>(my_end - 1 - r0 - 4 * grp, hide);
       }
       const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
       const char* O = Os + sub * 32 * DH * 2;
@@ -919,10 +939,14 @@ __device__ __forceinline__ void bwd_sink_body(const WinArgs& a, int id) {
       s[0][x] = __builtin_amdgcn_exp2f(s[0][x] * a.c2);
       dp[0][x] *= s[0][x];
     }
-    if (r0 < all_first || r0 + ROWS > to_row) {
+    auto hide = [&](int r) { s[0][r] = dp[0][r] = 0.f; };
+    if (r0 < all_first) {
       asm volatile("");
-      const int r1 = r0 + 4 * grp;
-      mask<0>(Limits{to_row - 1 - r1, my_first - 1 - r1, -4 * grp}, [&](int r) { s[0][r] = dp[0][r] = 0.f; });
+      mask_behind<0>(my_first - 1 - r0 - 4 * grp, hide);
+    }
+    if (r0 + ROWS > to_row) {
+      asm volatile("");
+      mask_ahead<0>(to_row - 1 - r0 - 4 * grp, hide);
     }
     const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}}, ds[1][2] = {{pack_frag(dp[0], 0), pack_frag(dp[0], 1)}};
     add_product<DH, 1>(dv, Os, p);
