@@ -283,8 +283,8 @@ rv_status rv_k_rotary_bwd(const rv_rotary_desc* desc);
  *   start, length      device int32 [B] or NULL: 0 (Sk >= Sq then), Sq for all.  Taken as 0 below 0, and length as Sq above.
  *   lse2               fp32 [B, n_heads, Sq]: log2 of the softmax denominator in the scaled base-2 domain (kept for the backward).
  * A token behind a sequence's length, or one that sees no key (its own row taken, no sinks), gives out 0, lse2 -inf and dq 0; rows that no live token
- * sees are not read, and no value of a key reaches a token that does not see it, infinities and NaN included (a workgroup that meets them among what
- * others of its tokens see is slower).
+ * sees are not read, and no value of a key reaches a token that does not see it, infinities and NaN included.  (Where some of 32 neighbouring rows see one,
+ * the sums of all 32 are formed again in fp32 vector arithmetic: many times slower, and of probabilities that are not rounded to bf16.)
  * Backward: of a call whose keys are the tokens' own, without start: S rows of each.  It writes all of dq, dk and dv, zeros behind a sequence's
  * length; out and lse2 are the forward's.  Probabilities are formed from lse2: off by up to 2^-20 |lse2| of themselves.
  * A score of -inf is a probability of zero; a token with keys whose scores are all -inf, or one of +inf or NaN among them, has no softmax: out and lse2
