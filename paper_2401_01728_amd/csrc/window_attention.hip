@@ -315,6 +315,11 @@ __device__ __forceinline__ void one_by_one(const WinArgs& a, const Walk& w, int 
   }
 }
 
+// the larger of a lane's and of the lane 32 further on or back: a vector instruction, where __shfl_xor goes through LDS
+__device__ __forceinline__ float other_half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 // Softmax of a tile of scores as in cross_attention.hip: s becomes exp2(s c2 - m), the factor for what was summed before is returned.
 template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum) {
@@ -328,7 +333,7 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& 
   for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
-  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  mx = other_half_max(mx);
   const float mn = fmaxf(m, mx * c2), base = mn == -INFINITY ? 0.f : mn;
   const float alpha = __builtin_amdgcn_exp2f(m - base);
   m = mn;
