@@ -320,6 +320,8 @@ __device__ __forceinline__ float other_half_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
+// what scores of maximum m are formed from: of all -inf, as a part of a row's keys may be, 0, so that their probabilities are zero
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 // Softmax of a tile of scores as in cross_attention.hip: s becomes exp2(s c2 - m), the factor for what was summed before is returned.
 template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum) {
@@ -334,7 +336,7 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& 
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
   mx = other_half_max(mx);
-  const float mn = fmaxf(m, mx * c2), base = mn == -INFINITY ? 0.f : mn;
+  const float mn = fmaxf(m, mx * c2), base = base_of(mn);
   const float alpha = __builtin_amdgcn_exp2f(m - base);
   m = mn;
   float ps = 0.f;
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
     clear(o);
     one_by_one<TILE>(a, walk, t0, t1, 1, own.t, own.first, own.last, [&](int row, bool seen) {
       const float s = dot_row<DH>(qf, loads.K + (int64_t)row * a.ldk);
-      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), loads.V + (int64_t)row * a.ldv);
+      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -base_of(m))), loads.V + (int64_t)row * a.ldv);
     });
   }
   if (own.r >= a.R) return;
@@ -510,7 +512,7 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
     clear(o);
     one_by_one<TOKEN_KEYS>(a, walk, t0 + wave, t1, TOKEN_NW, own.t, own.first, own.last, [&](int row, bool seen) {
       const float s = dot_row<DH>(qf, loads.K + (int64_t)row * a.ldk);
-      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -m)), loads.V + (int64_t)row * a.ldv);
+      if (seen) add_row<DH>(o, __builtin_amdgcn_exp2f(__fmaf_rn(s, a.c2, -base_of(m))), loads.V + (int64_t)row * a.ldv);
     });
   }
   lsum += __shfl_xor(lsum, 32, 64);
@@ -528,7 +530,7 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
   float top = -INFINITY, tot = 0.f, f[TOKEN_NW];
 #pragma unroll
   for (int i = 0; i < TOKEN_NW; ++i) top = fmaxf(top, ml[i * 32 + r].x);
-  const float base = top == -INFINITY ? 0.f : top;
+  const float base = base_of(top);
 #pragma unroll
   for (int i = 0; i < TOKEN_NW; ++i) {
     f[i] = __builtin_amdgcn_exp2f(ml[i * 32 + r].x - base);
@@ -580,7 +582,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(WinArgs a) {
   float m = -INFINITY, tot = 0.f;
   f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
   auto add = [&](float2 ml, f32x4 x, f32x4 y) {
-    const float mn = fmaxf(m, ml.x), base = mn == -INFINITY ? 0.f : mn;
+    const float mn = fmaxf(m, ml.x), base = base_of(mn);
     const float was = __builtin_amdgcn_exp2f(m - base), f = __builtin_amdgcn_exp2f(ml.x - base);
     v[0] = v[0] * was + x * f;
     v[1] = v[1] * was + y * f;

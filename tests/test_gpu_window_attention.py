@@ -407,6 +407,24 @@ def test_a_row_of_scores_of_minus_infinity(B, S, H, Hkv, dh, window, sinks, leng
     assert bool(torch.isnan(got[1][0, 0, r]))
 
 
+@pytest.mark.parametrize("Sq,Sk,H,dh,broken", [(2, 300, 1, 64, 100), (3, 700, 2, 128, 65), (16, 90, 2, 64, 32), (40, 1200, 1, 64, 400), (33, 1300, 2, 128, 300)])
+def test_keys_of_scores_of_minus_infinity_beside_rows_without_numbers(Sq, Sk, H, dh, broken):
+    """The first keys' scores are -inf for even tokens, whose results are those without these keys, and +inf for odd ones, who have none."""
+    g = torch.Generator().manual_seed(7)
+    q, k, v = (torch.randn(1, n, cols, generator=g).to(torch.bfloat16) for n, cols in ((Sq, H * dh), (Sk, dh), (Sk, dh)))
+    for h in range(H):
+        q[0, 0::2, h * dh + 3], q[0, 1::2, h * dh + 3] = 1.0, -1.0
+    bad = k.clone()
+    bad[0, :broken, 3] = -math.inf
+    start = Sk - Sq
+    out, lse2 = kernels.window_attention_fwd(q.cuda(), bad.cuda(), v.cuda(), H, 1, Sk, 0, start=_ints([start]))
+    see = lambda b: ((torch.arange(Sk) <= torch.arange(Sq)[:, None] + start) & (torch.arange(Sk) >= broken), slice(0, Sk))  # noqa: E731
+    (ref, ref_lse, *_), (e_out, *_) = _reference(q, k, v, None, [Sq], H, 1, Sk, 0, see)
+    _near(out[:, 0::2], ref[:, 0::2], e_out[:, 0::2])
+    _near_lse(lse2[:, :, 0::2], ref_lse[:, :, 0::2])
+    assert bool(torch.isnan(out[:, 1::2]).all()) and bool(torch.isnan(lse2[:, :, 1::2]).all())
+
+
 @pytest.mark.parametrize("B,S,H,Hkv,dh,length", [(2, 200, 4, 2, 64, None), (2, 70, 2, 2, 128, [70, 1]), (1, 1, 2, 1, 64, None)])
 def test_a_window_of_one_token(B, S, H, Hkv, dh, length):
     """Its probability is 1 whatever the score: the value itself, dq and dk exactly zero, dv the sum over the heads."""
