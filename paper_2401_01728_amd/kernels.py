@@ -311,6 +311,11 @@ def rotary_bwd(dq_out, dk_out, freq, n_heads, n_kv_heads, *, q=None, k=None, lay
     return dq, dk, dgamma_q, dgamma_k
 
 
+def _c_int(x):
+    """A number of which any larger one means the same: ctypes would keep its low 32 bits."""
+    return max(-1, min(x, 2 ** 31 - 1))
+
+
 @lru_cache(maxsize=256)
 def _window_work(sizes, backward):
     n = ctypes.c_size_t(0)
@@ -322,7 +327,7 @@ def window_attention_fwd(q, k, v, n_heads, n_kv_heads, window, sinks=0, start=No
     """rv_k_window_attention_fwd: q bf16 [B, Sq, n_heads * d_head], k and v bf16 [B, Sk, n_kv_heads * d_head] (columns of a wider matrix or not), start and
     length int32 [B] or None -> (out like q, lse2 fp32 [B, n_heads, Sq])."""
     B, Sq, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
-    cols, kcols, sizes = H * dh, Hkv * dh, (B, Sq, Sk, H, Hkv, dh, window, sinks)
+    cols, kcols, sizes = H * dh, Hkv * dh, (B, Sq, Sk, H, Hkv, dh, _c_int(window), _c_int(sinks))
     handle, context = _handle(stream, q, k, v, start, length, out)
     with context:
         if out is None:
@@ -340,7 +345,7 @@ def window_attention_bwd(q, k, v, out, dout, lse2, n_heads, n_kv_heads, window, 
     """rv_k_window_attention_bwd: (dq, dk, dv) of the above without start; out and lse2 are the forward's."""
     B, S, Sk, H, Hkv, dh = _cross_sizes(q, k, n_heads, n_kv_heads)
     assert S == Sk, (S, Sk)
-    cols, kcols = H * dh, Hkv * dh
+    cols, kcols, window, sinks = H * dh, Hkv * dh, _c_int(window), _c_int(sinks)
     handle, context = _handle(stream, q, k, v, length, out, dout, lse2, dq, dk, dv)
     with context:
         dq = q.new_empty(B, S, cols) if dq is None else dq

@@ -425,6 +425,13 @@ def test_keys_of_scores_of_minus_infinity_beside_rows_without_numbers(Sq, Sk, H,
     assert bool(torch.isnan(out[:, 1::2]).all()) and bool(torch.isnan(lse2[:, :, 1::2]).all())
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 32 + 5, 0), (2 ** 63, 2 ** 32), (10, 2 ** 40)])
+def test_windows_and_sinks_behind_32_bits_see_all(window, sinks):
+    qkv, do, _ = _inputs(2, 1, 100, 2, 2, 64)
+    for a, b in zip(_both(qkv.cuda(), do.cuda(), 2, 2, 64, window, sinks), _both(qkv.cuda(), do.cuda(), 2, 2, 64, 100 if window > 100 else window, 100 if sinks else 0)):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("B,S,H,Hkv,dh,length", [(2, 200, 4, 2, 64, None), (2, 70, 2, 2, 128, [70, 1]), (1, 1, 2, 1, 64, None)])
 def test_a_window_of_one_token(B, S, H, Hkv, dh, length):
     """Its probability is 1 whatever the score: the value itself, dq and dk exactly zero, dv the sum over the heads."""
