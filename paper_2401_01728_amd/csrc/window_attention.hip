@@ -322,7 +322,9 @@ __device__ __forceinline__ float other_half_max(float v) {
 }
 // what scores of maximum m are formed from: of all -inf, as a part of a row's keys may be, 0, so that their probabilities are zero
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// Softmax of a tile of scores as in cross_attention.hip: s becomes exp2(s c2 - m), the factor for what was summed before is returned.
+// Softmax of a tile of scores: s becomes exp2(s c2 - m), the factor for what was summed before is returned.  m follows a row's maximum where that is kStay
+// ahead of it: up to 2^8 in place of 1 loses nothing, and most tiles have a new maximum for one of a wave's 32 rows, which had all its sums multiplied.
+constexpr float kStay = 8.0f;
 template <int SUBS>
 __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum) {
   const float c2 = a.c2;
@@ -336,7 +338,7 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& 
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
   mx = other_half_max(mx);
-  const float mn = fmaxf(m, mx * c2), base = base_of(mn);
+  const float mn = mx * c2 > m + kStay ? mx * c2 : m, base = base_of(mn);
   const float alpha = __builtin_amdgcn_exp2f(m - base);
   m = mn;
   float ps = 0.f;
