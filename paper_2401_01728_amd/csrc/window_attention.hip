@@ -322,11 +322,11 @@ __device__ __forceinline__ float other_half_max(float v) {
 }
 // what scores of maximum m are formed from: of all -inf, as a part of a row's keys may be, 0, so that their probabilities are zero
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
-// Softmax of a tile of scores: s becomes exp2(s c2 - m), the factor for what was summed before is returned.  m follows a row's maximum where that is kStay
+// Softmax of a tile of scores: s becomes exp2(s c2 - m), o is what was summed before.  m follows a row's maximum where that is kStay
 // ahead of it: up to 2^8 in place of 1 loses nothing, and most tiles have a new maximum for one of a wave's 32 rows, which had all its sums multiplied.
 constexpr float kStay = 8.0f;
-template <int SUBS>
-__device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum) {
+template <int SUBS, int N>
+__device__ __forceinline__ void softmax_tile(f32x16 (&s)[SUBS], const WinArgs& a, const Walk& w, bool whole, const Edge& e, int t, float& m, float& lsum, f32x16 (&o)[N]) {
   const float c2 = a.c2;
   if (!whole) {
     mask_edge<0>(a, w, e, t, [&](int r) { s[0][r] = -INFINITY; });
@@ -338,9 +338,15 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& 
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[sub][r]);
   mx = other_half_max(mx);
-  const float mn = mx * c2 > m + kStay ? mx * c2 : m, base = base_of(mn);
-  const float alpha = __builtin_amdgcn_exp2f(m - base);
-  m = mn;
+  const bool ahead_of = mx * c2 > m + kStay;
+  if (__builtin_amdgcn_ballot_w64(ahead_of)) {
+    const float alpha = ahead_of ? __builtin_amdgcn_exp2f(m - mx * c2) : 1.0f;
+    if (ahead_of) m = mx * c2;
+    lsum *= alpha;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] *= alpha;
+  }
+  const float base = base_of(m);
   float ps = 0.f;
 #pragma unroll
   for (int sub = 0; sub < SUBS; ++sub)
@@ -350,8 +356,7 @@ __device__ __forceinline__ float softmax_tile(f32x16 (&s)[SUBS], const WinArgs& 
       s[sub][r] = p;
       ps += p;
     }
-  lsum = lsum * alpha + ps;
-  return alpha;
+  lsum += ps;
 }
 // what a live row's sums end with: keys whose scores are all -inf have no softmax
 __device__ __forceinline__ float log2_sum(float m, float tot) { return tot == 0.f ? NAN : m + __builtin_amdgcn_logf(tot); }
@@ -414,11 +419,7 @@ __global__ __launch_bounds__(64 * NW, NW / 4) void window_fwd_kernel(WinArgs a) 
     clear(s);
     in_a_row<SUBS * DH / 16, DH == 128 ? 6 : 3>([&](int i) { return frag_rows<DH>(Ks, i % SUBS * 32, i / SUBS); },
                         [&](int i, const Frag& f) { s[i % SUBS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i / SUBS], s[i % SUBS], 0, 0, 0); });
-    const float alpha = softmax_tile(s, a, walk, whole, e, own.t, m, lsum);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {    // maxima that have settled leave the sums as they are
-#pragma unroll
-      for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
-    }
+    softmax_tile(s, a, walk, whole, e, own.t, m, lsum, o);
 #pragma unroll
     for (int sub = 0; sub < SUBS; ++sub) {
       const Frag p[1][2] = {{pack_frag(s[sub], 0), pack_frag(s[sub], 1)}};
@@ -502,11 +503,7 @@ __global__ __launch_bounds__(64 * TOKEN_NW) void window_token_kernel(WinArgs a) 
     clear(s);
     in_a_row<DH / 16, 4>([&](int i) { return frag_rows<DH>(Ks, 0, i); },
                          [&](int i, const Frag& f) { s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[i], s[0], 0, 0, 0); });
-    const float alpha = softmax_tile(s, a, walk, false, e, own.t, m, lsum);
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
-#pragma unroll
-      for (int dt = 0; dt < DH / 32; ++dt) o[dt] *= alpha;
-    }
+    softmax_tile(s, a, walk, false, e, own.t, m, lsum, o);
     const Frag p[1][2] = {{pack_frag(s[0], 0), pack_frag(s[0], 1)}};
     add_product<DH, 1>(o, Ks + HALF, p);
   }
