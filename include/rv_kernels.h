@@ -289,6 +289,7 @@ rv_status rv_k_rotary_bwd(const rv_rotary_desc* desc);
  * length; out and lse2 are the forward's.  Probabilities are formed from lse2: off by up to 2^-20 |lse2| of themselves.
  * A score of -inf is a probability of zero; a token with keys whose scores are all -inf, or one of +inf or NaN among them, has no softmax: out and lse2
  * are NaN, and so is what the backward forms with them.  With an infinite operand a result that is infinite by definition may be NaN.
+ * Sums are kept up to 2^8 times their probabilities: values of less than 2^120 / Sk do not overflow.
  * d_head is 64 or 128; the scale is 1 / sqrt(d_head); window is at least 1, any larger number sees all, sinks at least 0; B, Sq, Sk are at least 1, of
  * any size (B <= 2^20, Sq and Sk <= 2^24, n_heads <= 2^16, n_heads / n_kv_heads * Sq < 2^30 - 64, of a sequence's q and k up to 2^34 elements).  Pitches are
  * multiples of 8 up to 2^24, pointers 16-byte aligned (lse2, start, length: 4).  Outputs must not share memory with inputs or one another (but they may

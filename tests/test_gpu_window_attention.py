@@ -425,6 +425,39 @@ def test_keys_of_scores_of_minus_infinity_beside_rows_without_numbers(Sq, Sk, H,
     assert bool(torch.isnan(out[:, 1::2]).all()) and bool(torch.isnan(lse2[:, :, 1::2]).all())
 
 
+@pytest.mark.parametrize("rise", [0.02, 0.05, 0.12, -0.05])
+@pytest.mark.parametrize("S,dh,window", [(700, 64, 500), (700, 64, 650), (1400, 64, 1300), (600, 128, 300), (900, 128, 700)])
+def test_scores_that_rise_from_key_to_key(S, dh, window, rise):
+    """By 1 to 11 powers of two in 64 keys, and falling: a row's largest score is another one in each tile."""
+    qkv, do, n = _inputs(11, 1, S, 2, 1, dh)
+    q, k, _ = _split(qkv, 2, 1, dh)
+    q[..., 0] = q[..., dh] = math.sqrt(dh)
+    k[..., 0] = torch.arange(S) * rise
+    (out, lse2, dq, dk, dv), (e_out, e_dq, e_dk, e_dv) = _reference(*_split(qkv, 2, 1, dh), do, n, 2, 1, window, 2)
+    got = _both(qkv.cuda(), do.cuda(), 2, 1, dh, window, 2)
+    _near(got[0], out, e_out)
+    _near_lse(got[1], lse2)
+    for a, ref, bound in zip(got[2:], (dq, dk, dv), (e_dq, e_dk, e_dv)):
+        _near(a, ref, bound)
+
+
+@pytest.mark.parametrize("Sq,dh", [(1, 64), (1, 128), (3, 64), (40, 128)])
+@pytest.mark.parametrize("rise", [0.03, -0.03])
+def test_scores_that_rise_in_a_cache(Sq, dh, rise):
+    """Likewise for single tokens, whose waves and parts have references of their own, and for parts of more rows."""
+    Sk = 3000
+    g = torch.Generator().manual_seed(12)
+    q, k, v = (torch.randn(1, rows, cols, generator=g).to(torch.bfloat16) for rows, cols in ((Sq, 2 * dh), (Sk, dh), (Sk, dh)))
+    q[..., 0] = q[..., dh] = math.sqrt(dh)
+    k[..., 0] = torch.arange(Sk) * rise
+    start = Sk - Sq
+    out, lse2 = kernels.window_attention_fwd(q.cuda(), k.cuda(), v.cuda(), 2, 1, Sk, 0, start=_ints([start]))
+    see = lambda b: (torch.arange(Sk) <= torch.arange(Sq)[:, None] + start, slice(0, Sk))  # noqa: E731
+    (ref, ref_lse, *_), (e_out, *_) = _reference(q, k, v, None, [Sq], 2, 1, Sk, 0, see)
+    _near(out, ref, e_out)
+    _near_lse(lse2, ref_lse)
+
+
 @pytest.mark.parametrize("window,sinks", [(2 ** 32 + 5, 0), (2 ** 63, 2 ** 32), (10, 2 ** 40)])
 def test_windows_and_sinks_behind_32_bits_see_all(window, sinks):
     qkv, do, _ = _inputs(2, 1, 100, 2, 2, 64)
