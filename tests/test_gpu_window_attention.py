@@ -387,6 +387,54 @@ def test_a_broken_row_of_a_cache(B, Sq, Sk, H, Hkv, dh, window, sinks, start, le
     assert bool(((got.double() - ref.double()).abs() <= 2.0 ** -6 * 6.0).all()) and bool(torch.isfinite(got).all())
 
 
+# chunks whose own keys lie on both sides of the ring's end, `before` of the first sequence's in front of it, rings gone round 1 to 50 times; in one walk and in
+# parts, by few rows and by workgroups of 128; with sinks and without, windows as long as the ring allows and shorter
+WRAPPED = [(2, 40, 104, 4, 2, 64, 60, 4, 20), (2, 3, 68, 8, 1, 64, 60, 4, 2), (3, 16, 333, 2, 1, 128, 300, 0, 5), (2, 100, 1507, 4, 2, 128, 1400, 4, 37),
+           (1, 4, 3000, 8, 2, 64, 2900, 7, 3), (2, 130, 2003, 1, 1, 64, 1800, 3, 65), (1, 300, 700, 8, 2, 128, 350, 0, 150), (2, 33, 45, 3, 3, 64, 10, 2, 1)]
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh,window,sinks,before", WRAPPED)
+@pytest.mark.parametrize("which", ["key", "value"])
+def test_a_broken_row_where_the_ring_has_wrapped(B, Sq, Sk, H, Hkv, dh, window, sinks, before, which):
+    """One of the last keys of a call, or its value, is no number.  Tokens in front of it, and behind its window, have
+    what the definition gives without it.  Keys in the rows next to the ring's end, on both of its sides, have a score of 4 more: one of them left out or taken
+    twice is several times the bound."""
+    ring = Sk - sinks
+    start = [sinks + (1, 50, 7)[b] * ring + ring - before - 9 * b for b in range(B)]
+    end = [s + Sq for s in start]
+    g = torch.Generator().manual_seed(25)
+    k, v = (torch.randn(B, max(end), Hkv * dh, generator=g).to(torch.bfloat16) for _ in range(2))
+    q = (torch.randn(B, Sq, H * dh, generator=g) * 1.3).to(torch.bfloat16)
+    q[..., ::dh] = math.sqrt(dh)
+    k[..., ::dh] = 0.0
+    for b in range(B):
+        phase = (torch.arange(end[b]) - sinks) % ring
+        k[b, :end[b], ::dh] = torch.where((phase >= ring - 10) | (phase < 10), 4.0, 0.0).to(torch.bfloat16)[:, None]
+    kc, vc, holds = _cache(k, v, end, Sk, sinks)
+
+    def see(b):
+        p, j = start[b] + torch.arange(Sq)[:, None], torch.arange(end[b])[None, :]
+        still = torch.zeros(end[b], dtype=torch.bool)
+        still[holds[b][holds[b] >= 0]] = True
+        return (j <= p) & ((j > p - window) | (j < sinks)) & still, slice(0, end[b])
+
+    (out, lse2, *_), (e_out, *_) = _reference(q, k, v, None, [Sq] * B, H, Hkv, window, sinks, see)
+    whole = torch.zeros(B, Sq, dtype=torch.bool)
+    for b in range(B):
+        at = end[b] - 1 - Sq // 8
+        (kc if which == "key" else vc)[b, sinks + (at - sinks) % ring] = math.nan
+        whole[b] = ~see(b)[0][:, at]
+    assert bool(whole.any()) and not bool(whole.all())
+    got, lse = kernels.window_attention_fwd(q.cuda(), kc.cuda(), vc.cuda(), H, Hkv, window, sinks, _ints(start))
+    got = got.cpu()
+    _near(got[whole], out[whole], e_out[whole])
+    assert bool(torch.isnan(got[~whole]).all())
+    by_token = lambda t: t.cpu().double().transpose(1, 2)  # noqa: E731
+    clear = whole if which == "key" else torch.ones_like(whole)
+    _near_lse(by_token(lse)[clear], by_token(lse2)[clear])
+    assert bool(torch.isnan(by_token(lse)[~clear]).all())
+
+
 @pytest.mark.parametrize("B,S,H,Hkv,dh,window,sinks,length", [(2, 100, 4, 2, 64, 20, 0, [100, 60]), (1, 300, 2, 1, 128, 300, 2, None)])
 def test_a_row_of_scores_of_minus_infinity(B, S, H, Hkv, dh, window, sinks, length):
     """It has no softmax: NaN, for itself and, in the backward, for the keys it shares with others; other rows and heads are what they were."""
