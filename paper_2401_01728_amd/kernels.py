@@ -220,6 +220,11 @@ def _matrix(t, B, S, cols):
     return (0, 0) if t is None else (t.data_ptr(), _tokens(t, B, S, cols))
 
 
+def _c_int(x):
+    """A number of which any larger one means the same: ctypes would keep its low 32 bits, and struct refuse it."""
+    return max(-1, min(x, 2 ** 31 - 1))
+
+
 ROT_LAYOUT = {"half": 0, "pairs": 1}
 FREQ_RULE = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 # rv_rotary_desc as C lays it out: one call of pack() is a third of the time of filling in a ctypes structure
@@ -275,7 +280,7 @@ def rotary_fwd(q, k, freq, n_heads, n_kv_heads, *, v=None, layout="half", amplit
         _check(_lib.lib().rv_k_rotary_fwd(_ROTARY_DESC.pack(
             *_rotary_head(B, S, n_heads, n_kv_heads, dh, freq, layout, amplitude, gamma_q, gamma_k, eps, pos, start, length), *_matrix(q, B, S, qcols),
             *_matrix(k, B, S, kcols), *_matrix(v, B, S, kcols), *_matrix(q_out, B, S, qcols), *_matrix(k_out, B, rows or S, kcols),
-            *_matrix(v_out, B, rows or S, kcols), rows, sinks, *_NONE, *_NONE, *_NONE, *_NONE, 0, 0, 0, 0, handle)))
+            *_matrix(v_out, B, rows or S, kcols), rows, _c_int(sinks), *_NONE, *_NONE, *_NONE, *_NONE, 0, 0, 0, 0, handle)))
     return (q_out, k_out) if v is None else (q_out, k_out, v_out)
 
 
@@ -309,11 +314,6 @@ def rotary_bwd(dq_out, dk_out, freq, n_heads, n_kv_heads, *, q=None, k=None, lay
             *_matrix(k, B, S, kcols), *_NONE, *_NONE, *_NONE, *_NONE, 0, 0, *_matrix(dq_out, B, S, qcols), *_matrix(dk_out, B, S, kcols), *_matrix(dq, B, S, qcols),
             *_matrix(dk, B, S, kcols), address(dgamma_q), address(dgamma_k), address(work), n, handle)))
     return dq, dk, dgamma_q, dgamma_k
-
-
-def _c_int(x):
-    """A number of which any larger one means the same: ctypes would keep its low 32 bits."""
-    return max(-1, min(x, 2 ** 31 - 1))
 
 
 @lru_cache(maxsize=256)

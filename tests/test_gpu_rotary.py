@@ -244,6 +244,19 @@ def test_cache(rows, sinks, S, start, length, values):
         assert got[2] is cache[1] and torch.equal(cache[1].cpu(), held)
 
 
+@pytest.mark.parametrize("sinks", [2 ** 31, 2 ** 32, 2 ** 40 + 1])
+def test_sinks_behind_32_bits(sinks):
+    """Any number of sinks counts as rows - 1 at most, as the attention that reads the cache takes it."""
+    q, k, v, *_ = _gpu(*_inputs(16, 2, 6, 2, 2, 64))
+    freq = kernels.rotary_frequencies(64)[0].cuda()
+    out = []
+    for n in (sinks, 3):
+        cache = [torch.zeros(2, 4, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        out.append(kernels.rotary_fwd(q, k, freq, 2, 2, v=v, cache=cache, sinks=n, start=_ints([0, 70])))
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+
+
 def test_a_cache_of_lengths_out_of_range():
     """Lengths above S and below 0 are S and 0, for the rows too."""
     q, k, v, *_ = _gpu(*_inputs(8, 2, 6, 2, 2, 64))
