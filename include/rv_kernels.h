@@ -212,9 +212,9 @@ rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, in
  *   work               of the backward with dgamma_q or dgamma_k: device, 256-byte aligned, rv_k_rotary_work bytes; calls that may run at one time
  *                      need one each.
  * A head of zeros has no norm where eps is 0: NaN.
- * A result is computed in 32 bits and rounded once; an angle is off by less than 2^-24 turns.  No atomics: results do not vary.  d_head is 64 or 128;
- * B <= 2^20, S <= 2^24, B * S <= 2^30, up to 2^12 heads; pitches are multiples of 8 up to 2^24, pointers 16-byte aligned (start, length, pos, dgamma:
- * 4, freq: 8).  Outputs must not share memory with inputs or one another but as said (columns of one matrix do not).
+ * A result is computed in 32 bits and rounded once; an angle is off by less than 2^-25 turns, for frequencies of up to 2^40 in size.  No atomics: results do
+ * not vary.  d_head is 64 or 128; B <= 2^20, S <= 2^24, B * S <= 2^30, up to 2^12 heads; pitches are multiples of 8 up to 2^24, pointers 16-byte aligned
+ * (start, length, pos, dgamma: 4, freq: 8).  Outputs must not share memory with inputs or one another but as said (columns of one matrix do not).
  */
 enum { RV_ROT_HALF = 0, RV_ROT_PAIRS = 1 };
 typedef struct {

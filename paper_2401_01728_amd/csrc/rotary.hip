@@ -7,7 +7,7 @@
 // Bound by memory: every element is read and written once (backward with a norm: read twice as much), 16 bytes to an access.  A lane holds
 // 16 columns of a head, two chunks of eight that contain the pairs of one another, so a head is 4 or 8 neighbouring lanes and its norm a sum
 // over them.  Cosines and sines are formed once for each (token, frequency) of a workgroup's tokens and reach the heads through LDS.
-// An angle is formed in 64 bits, as turns, and leaves them as a fraction of a turn: at position 2^31 it is off by 2^-24 turns.
+// An angle is formed as a fraction of a turn of which a product of 64-bit numbers keeps all its bits, and is rounded to 32 bits once (angles).
 #include <math.h>
 #include "../../include/rv_kernels.h"
 #include "common.h"
@@ -96,6 +96,16 @@ __device__ __forceinline__ void turn(float (&x)[16], const float2* cs, int j, in
   }
 }
 
+// p f / (2 pi) less a whole number: f / (2 pi) as the sum of two 64-bit numbers (2^-104 of itself off), whole turns taken out of the exact product with the
+// first.  For |p| <= 2^31 + 2^24 and |f| <= 2^40 the fraction is off by 2^-34 turns at most, and by 2^-26 when it is rounded to 32 bits.  (One product
+// of 64 bits was off by 2^-53 of all the turns: 2^-24 of one at f = 1 and position 2^31.)
+__device__ __forceinline__ float turn_fraction(double p, double f) {
+  constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;      // 1 / (2 pi)
+  const double h = f * kTurn, rest = fma(f, kTurnRest, fma(f, kTurn, -h));
+  const double t = fma(p, rest, fma(p, h, -rint(p * h)));
+  return (float)(t - rint(t));
+}
+
 // What a workgroup's tokens t0 .. share: where they go and their angles.
 __device__ __forceinline__ void angles(const RotArgs& a, int64_t t0, int tw, bool in_cache, bool turned, Token* token, float2* cs) {
   const int half = a.rot / 2;
@@ -130,9 +140,8 @@ __device__ __forceinline__ void angles(const RotArgs& a, int64_t t0, int tw, boo
       p = a.start ? a.start[b] : 0;
       p = (p < 0 ? 0 : p) + (t - (int64_t)b * a.S);
     }
-    const double turns = (double)p * (a.freq[f] * 0.15915494309189535);       // 1 / (2 pi)
     float s, c;
-    sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+    sincospif(2.0f * turn_fraction((double)p, a.freq[f]), &s, &c);
     cs[w * half + f] = float2{c * a.amplitude, s * a.amplitude};
   }
   __syncthreads();

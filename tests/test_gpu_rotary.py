@@ -11,6 +11,7 @@ Tolerances, element by element; u = 2^-24 is half a step of fp32, and the result
           sum e |xh| + (2 normed + (T heads / 32 + 80) u) sum |dn xh|
 """
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -175,6 +176,51 @@ def test_positions_of_their_own(layout, dh, rot):
     pos[0, 30:60] = torch.arange(30)
     pos[1, 0], pos[1, 1] = 2 ** 31 - 1, -2 ** 31
     _check(2, 77, 3, 1, dh, rot, layout, "qk", length=[77, 50], start=[3, 9], pos=pos, amplitude=1.35, base=500000.0, seed=2)
+
+
+def _turns(freq, pos):
+    """freq pos / (2 pi) less the nearest whole number, [positions, frequencies], in whole numbers with 1 / (2 pi) to 75 digits."""
+    turn = Fraction(10 ** 75, 6283185307179586476925286766559005768394338798750211641949889184615632812572)
+    t = [[Fraction(f) * p * turn for f in freq] for p in pos]
+    return torch.tensor([[float(x - round(x)) for x in row] for row in t], dtype=torch.float64)
+
+
+@pytest.mark.parametrize("layout,dh,amplitude", [("half", 64, 1.0), ("pairs", 128, -1.5)])
+def test_angles_of_far_positions_and_fast_frequencies(layout, dh, amplitude):
+    """Frequencies up to 2^40 and the ends of 32-bit positions.  Every pair is one that its angle turns to nearly (0, r) or, going back, (r, 0): the small
+    result, next to which a bf16 rounding is nothing, is off by the angle, 2^-25 turns, by a cosine and a sine (4 u, of which a step next to 1 is one),
+    their products with the amplitude (u) and the pair's product (u), times the pair's own size."""
+    g = torch.Generator().manual_seed(17)
+    half, S = dh // 2, 40
+    freq = torch.exp2(torch.linspace(-20.0, 40.0, half, dtype=torch.float64)) * (1.0 - 0.5 * torch.rand(half, generator=g, dtype=torch.float64))
+    freq[half // 2] = 500000.0 ** (-2.0 / 128)
+    freq[3] = -freq[3]
+    pos = torch.randint(-2 ** 31, 2 ** 31, (S,), generator=g, dtype=torch.int64)
+    pos[:6] = torch.tensor([0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2147311945])
+    turns = _turns(freq.tolist(), pos.tolist())
+    c, s = torch.cos(2 * math.pi * turns), torch.sin(2 * math.pi * turns)
+    # whole numbers of 8 bits (bf16) whose quotient is nearest to the angle's tangent
+    size = torch.arange(128, 256, dtype=torch.float64)[:, None, None]
+    a, b = torch.round(size * s), torch.round(size * c)
+    best = (a * c - b * s).abs().argmin(0, keepdim=True)
+    a, b = a.gather(0, best)[0], b.gather(0, best)[0]
+    first, second = _halves(dh, layout)
+    at = pos.to(torch.int32)[None].cuda()
+
+    def matrix(x, y):
+        m = torch.zeros(1, S, dh, dtype=torch.bfloat16)
+        m[0, :, first], m[0, :, second] = x.to(torch.bfloat16), y.to(torch.bfloat16)
+        return m.cuda()
+
+    how = dict(layout=layout, amplitude=amplitude, pos=at)
+    # in front: (a c - b s, b c + a s); back: (b c + a s, a c - b s) of (b, a)
+    there = kernels.rotary_fwd(matrix(a, b), None, freq.cuda(), 1, 0, **how)[0]
+    back = kernels.rotary_bwd(matrix(b, a), None, freq.cuda(), 1, 0, **how)[0]
+    bound = (2 * math.pi * 2.0 ** -25 + 6 * U) * abs(amplitude) * (a.abs() + b.abs())
+    for got, columns, ref in ((there, first, a * c - b * s), (there, second, b * c + a * s), (back, first, b * c + a * s), (back, second, a * c - b * s)):
+        got, ref = got[0].cpu().double()[:, columns], amplitude * ref
+        over = (got - ref).abs() / (bound + 2.0 ** -8 * ref.abs() + 1e-30)
+        assert bool((over <= 1.0).all()), "off by %.3g of the bound at (position, frequency) %d" % (float(over.max()), int(over.argmax()))
 
 
 def test_zeros_and_extremes():
