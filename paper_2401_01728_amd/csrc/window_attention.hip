@@ -1071,7 +1071,7 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   if (U * R * dh / 8 > (1ll << 38) || U * Sk * dh / 8 > (1ll << 38)) return false;
   p.window = (int)(window < Sk ? window : Sk);
   p.sinks = (int)(sinks < Sk ? sinks : Sk - 1);
-  p.R = (int)R; p.Rp = (int)(up(R, TILE) * TILE + TILE);      // (a tile of rows may begin anywhere)
+  p.R = (int)R; p.Rp = (int)(up(R + TILE - 1, TILE) * TILE);  // (a tile of rows may begin at any of them)
   p.token = R <= OWN;
   // tiles that a workgroup of `rows` walks over at most
   auto tiles = [&](int64_t rows, int64_t T) {
@@ -1107,13 +1107,14 @@ bool make_plan(WinPlan& p, int64_t B, int64_t Sq, int64_t Sk, int64_t H, int64_t
   p.at_once = (int)(B < kMostThreads / threads ? B : kMostThreads / threads);
   auto round = [](size_t b) { return (b + 255) / 256 * 256; };
   const bool parts = p.fwd_parts > 1;
-  p.fwd_ml = parts ? round((size_t)4 * p.fwd_parts * U * R * dh) : 0;
-  p.fwd_bytes = parts ? p.fwd_ml + round((size_t)8 * p.fwd_parts * U * R) : 0;
-  p.d = round((size_t)4 * U * p.Rp);
+  const size_t units = (size_t)p.at_once * Hkv;             // the next launch's sequences have the memory of those before
+  p.fwd_ml = parts ? round(4 * p.fwd_parts * units * R * dh) : 0;
+  p.fwd_bytes = parts ? p.fwd_ml + round(8 * p.fwd_parts * units * R) : 0;
+  p.d = round(4 * units * p.Rp);
   p.part = 2 * p.d;
-  p.kv_part = p.part + (p.q_parts > 1 ? round((size_t)4 * p.q_parts * U * R * dh) : 0);
-  p.sink_part = p.kv_part + (p.kv_parts > 1 ? round((size_t)8 * p.kv_parts * U * Sk * dh) : 0);
-  p.bwd_bytes = p.sink_part + (p.sink_parts > 1 ? round((size_t)8 * p.sink_parts * U * p.sinks * dh) : 0);
+  p.kv_part = p.part + (p.q_parts > 1 ? round(4 * p.q_parts * units * R * dh) : 0);
+  p.sink_part = p.kv_part + (p.kv_parts > 1 ? round(8 * p.kv_parts * units * Sk * dh) : 0);
+  p.bwd_bytes = p.sink_part + (p.sink_parts > 1 ? round(8 * p.sink_parts * units * p.sinks * dh) : 0);
   return true;
 }
 

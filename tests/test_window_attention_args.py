@@ -69,3 +69,13 @@ def test_too_little_work_memory():
     assert _fwd(dict(token, start=1 << 16, work=None)) == INVAL
     need = _work(backward=1)[1]
     assert _bwd(dict(bytes=need - 1)) == INVAL
+
+
+def test_work_memory_of_many_sequences():
+    """What does not go into one launch is made in several that use the same memory: no more for 2^20 sequences than for those of one launch."""
+    one = dict(Sq=1, Sk=1, H=16, Hkv=16, dh=64, window=7, sinks=1, backward=1)
+    status, most = _work(B=1 << 20, **one)
+    assert status == OK and most == _work(B=1 << 19, **one)[1]
+    assert _work(B=1 << 10, **one)[1] < most < _work(B=1, **one)[1] * (1 << 19)
+    # two statistics of 32 bits for 64 rows, a tile that may begin at the last of them, of 16 heads
+    assert _work(B=1, **one)[1] == 2 * 64 * 4 * 16
