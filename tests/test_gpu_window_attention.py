@@ -368,6 +368,21 @@ def test_an_output_gradient_that_is_not_a_number(B, S, H, Hkv, dh, window, sinks
         assert bool(((t - ref).abs() <= bound)[where].all()) and bool(torch.isnan(t[~where]).all())
 
 
+# sinks that fill whole workgroups of the backward, and one that does not
+MANY_SINKS = [(1, 400, 2, 2, 64, 30, 128, None, 5), (1, 500, 4, 1, 128, 70, 200, None, 140), (2, 600, 2, 1, 64, 100, 260, [600, 300], 259), (1, 450, 3, 3, 128, 1, 130, None, 300)]
+
+
+@pytest.mark.parametrize("B,S,H,Hkv,dh,window,sinks,length,at", MANY_SINKS)
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_a_broken_key_of_many_sinks(B, S, H, Hkv, dh, window, sinks, length, at, value):
+    test_a_key_that_is_not_a_number_reaches_who_sees_it(B, S, H, Hkv, dh, window, sinks, length, at, value)
+
+
+@pytest.mark.parametrize("B,S,H,Hkv,dh,window,sinks,length,at", MANY_SINKS)
+def test_a_broken_output_gradient_over_many_sinks(B, S, H, Hkv, dh, window, sinks, length, at):
+    test_an_output_gradient_that_is_not_a_number(B, S, H, Hkv, dh, window, sinks, length, at)
+
+
 @pytest.mark.parametrize("B,Sq,Sk,H,Hkv,dh,window,sinks,start,length", [c for c in CACHES if c[1] > 1])
 def test_a_broken_row_of_a_cache(B, Sq, Sk, H, Hkv, dh, window, sinks, start, length):
     """The newest key's value is no number: the tokens in front of it do not see it."""
