@@ -352,14 +352,12 @@ bool sizes_ok(int64_t B, int64_t S, int64_t H, int64_t Hkv, int64_t dh) {
   return B <= (1 << 20) && S <= (1 << 24) && B * S <= (1 << 30) && H <= (1 << 12) && Hkv <= (1 << 12);
 }
 
-// Workgroups and tokens of a side: up to 1024 items of 16 columns to a workgroup at one time, fewer while that leaves less than 2048 workgroups, but 1024
-// where there are 512 (the kernel on 8 x 511 tokens of 25 + 25 heads of 64 with one token's 100 14 us, 9.6).
+// Workgroups and tokens of a side: up to 1024 items of 16 columns to a workgroup at one time, fewer where that leaves less than 512 workgroups (8 x 511 tokens of
+// 25 + 25 heads of 64, a token of which is 100 items of either side: 14 us with one token to a workgroup, 9.6 with the seven of this rule).
 void deal(Side& d, int64_t tokens, int dh, int64_t most) {
   const int items = d.heads * (dh / 16);
   if (!items) return;
-  const int64_t few = 1024 / items < tokens / 512 ? 1024 / items : tokens / 512;
-  int64_t w = 1024 / items < tokens / 2048 ? 1024 / items : tokens / 2048;
-  w = w < few ? few : w;
+  const int64_t w = 1024 / items < tokens / 512 ? 1024 / items : tokens / 512;
   d.tw = (int)(w < 1 ? 1 : w > kMostTokens ? kMostTokens : w);
   const int64_t groups = (tokens + d.tw - 1) / d.tw;
   d.groups = (int)(groups < most ? groups : most);
