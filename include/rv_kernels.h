@@ -205,7 +205,7 @@ rv_status rv_k_cross_attention_bwd(const void* q, int64_t ldq, const void* k, in
  *   rows, sinks        rows > 0: k_out and v_out are a cache of `rows` rows for each sequence (sequence b's begin at row b * rows), a ring
  *                      behind its first `sinks` rows: position p (start[b] + i, whatever pos says) is row p below sinks, else
  *                      sinks + (p - sinks) mod (rows - sinks); sinks counts as rows - 1 at most.  Of two tokens of a call with one row the
- *                      later is kept; no other row is touched.
+ *                      later is kept; no other row is touched.  Who wants a prompt's keys in a matrix and its last ones in a cache calls twice.
  * Backward: dq_out, dk_out are the gradients of q_out and k_out (without a cache), dq, dk those of q and k, rows lddq_out .. apart; dq may be
  * dq_out or q, and dk dk_out or k, with its pitch.  q and k are the forward's inputs, read with a norm only (NULL else).
  * dgamma_q, dgamma_k fp32 [d_head] or NULL.  v, *_out, rows, sinks are not looked at.
@@ -261,7 +261,8 @@ typedef struct {
  *   RV_FREQ_LINEAR  positions closer together: divided by factor.
  *   RV_FREQ_BASE    the base times factor^(rot / (rot - 2)): the fastest stays, the slowest is divided by factor.
  *   RV_FREQ_PARTS   by the turns that a pair makes within `context` positions: `high` and more stay, `low` and less are divided by factor, linear in
- *                   the turns between; the amplitude is 1 + 0.1 ln factor.
+ *                   the turns between (not in the pair's index, as the code of some models has it: whoever needs that passes a freq of their own);
+ *                   the amplitude is 1 + 0.1 ln factor.
  */
 enum { RV_FREQ_PLAIN = 0, RV_FREQ_LINEAR = 1, RV_FREQ_BASE = 2, RV_FREQ_PARTS = 3 };
 rv_status rv_k_rotary_frequencies(int rot, double base, int rule, double factor, double context, double low, double high,

@@ -1160,8 +1160,9 @@ rv_status forward(WinArgs a, const WinPlan& p, char* work, hipStream_t st) {
     const int64_t grid = deal(a.fwd, a, unequal, up(a.R, OWN * 4), p.fwd_parts);
     // Narrow windows 32 keys at a time: what a wave's own tokens do not see is left out, and heads of 64 take 117 registers, four waves to a SIMD.  us, 32 / 64
     // keys: 4 x 2000 tokens of 16 heads of 64, windows of 64 / 256 / 512 / 1024 / 1500: 18 / 21, 25 / 32, 35 / 42, 53 / 55, 70 / 63; of 128 34 / 34, 45 / 44,
-    // 58 / 57, 85 / 82, 105 / 98; 4 x 4000 of 16 heads over 2 of 128, windows of 64 / 256 / 512 / 1024: 47 / 50, 77 / 80, 104 / 103, 154 / 148.  (Tiles of 32 in
-    // rings of 3 and 4 in place of 64 in two: 3 to 10 % slower, by their barriers.)
+    // 58 / 57, 85 / 82, 105 / 98; 4 x 4000 of 16 heads over 2 of 128, windows of 64 / 256 / 512 / 1024: 47 / 50, 77 / 80, 104 / 103, 154 / 148.  Heads of 128 gain 6 %
+    // at a window of 64 and lose 4 at 1024; between 256 and 512 the two are within 4 % of each other either way, and the border could be anywhere there.  (Tiles
+    // of 32 in rings of 3 and 4 in place of 64 in two: 3 to 10 % slower, by their barriers.)
     if (a.window <= (DH == 64 ? 1024 : 512)) RV_TRY((launch<window_fwd_kernel<DH, 4, 2, 1>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
     else RV_TRY((launch<window_fwd_kernel<DH, 4, 2, 2>>(a, grid, 256, 2 * 2 * kTileBytes<DH>, st)));
   }
